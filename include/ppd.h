@@ -18,6 +18,9 @@
  *   ppd_next_tree        device: the next step's candidate tree from this
  *                        step's outputs (Section 3, step (1))
  *
+ * ppd_accept_sample takes ppd_accept's place for decoding at a temperature, and
+ * the ppd_kvq calls that of the bf16 cache for one held in 4 bits.
+ *
  * Conventions shared by every call
  * --------------------------------
  * Tree.  Nodes 0..T-1 in topological order: parent[0] = -1 (node 0 is the
@@ -333,6 +336,198 @@ ppd_status ppd_next_tree(int32_t T, const int32_t *parent, const int32_t *ids, i
                          const int32_t *n_path, const int32_t *next_tok, int32_t tpl_T,
                          const int32_t *tpl_parent, const int32_t *tpl_kind, int32_t *next_ids,
                          void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * A KV cache held in 4 bits (bf16 models, head_dim 128): 144 bytes a token,
+ * layer and kv head instead of 512.  Tree nodes stay bfloat16 until they are
+ * accepted, in a staging cache of their own:
+ *   verify   ppd_verify_step_kvq   tree rows to `tail`, attention over both
+ *   accept   ppd_accept or ppd_accept_sample
+ *   score    ppd_kvq_score         (only for eviction) attention weights
+ *   commit   ppd_kvq_commit        accepted rows of `tail` into 4 bits
+ *   evict    ppd_kvq_evict         when the cache is to be cut
+ * Rows.  A key row (after RoPE) and a value row are held as two groups of 64
+ *   dims (the two RoPE halves): zero z = the group's minimum, scale s =
+ *   bf16((maximum - minimum) / 15), codes c = min(15, rint((x - z) / s)),
+ *   every operation in float32, roundings to nearest even; s = 0 gives c = 0.
+ *   The held value is s c + z (float32).  A group with a NaN or an infinity,
+ *   or whose range passes the largest float, stands for 64 NaNs.
+ * Layout.  blocks [n_layers][n_kv_heads][capacity / 32][PPD_KVQ_BLOCK_BYTES],
+ *   a block holding positions 32 b .. 32 b + 31 of one head in the operand
+ *   order of the attention's matrix instructions (16-row tiles of 64 lanes):
+ *     [0, 2048)     key codes, 32-bit words [t 2][lane 64][w 4]: position
+ *                   8 (lane % 16 / 4) + 4 t + lane % 4, dims 32 w + 8 (lane /
+ *                   16) + e, e < 8
+ *     [2048, 4096)  value codes, words [h 2][lane 64][w 4]: dim 64 h + 16 w +
+ *                   lane % 16, positions 8 (lane / 16) + e
+ *     [4096, 4352)  per position the keys' two (scale, zero) bfloat16 pairs
+ *     [4352, 4608)  the same of the values
+ *   Element e of a word is its bits 4 (e / 2) + 16 (e % 2) .. + 3.
+ * Positions [0, L) of every head hold the cached prefix; what the positions
+ * behind hold is never used, and a call leaves every position that it does
+ * not write as it was.
+ */
+#define PPD_KVQ_BLOCK 32
+#define PPD_KVQ_BLOCK_BYTES 4608
+typedef struct {
+  void *blocks;      /* device, 16-byte aligned */
+  int32_t n_layers, n_kv_heads;
+  int32_t capacity;  /* positions per head: a multiple of 32, at most PPD_CAPACITY_MAX */
+  ppd_kv tail;       /* bfloat16 staging of the tree's rows: node i at position i of
+                        [n_layers][n_kv_heads][tail.capacity][128] keys and [..][128][tail.capacity]
+                        values, tail.capacity >= T and a multiple of 8; may be all zero for calls that
+                        name no tail.  tail.len_dev, if set, receives L + n from ppd_kvq_commit */
+} ppd_kvq;
+
+/* Bytes of `blocks`; 0 on invalid sizes. */
+size_t ppd_kvq_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t capacity);
+
+/*
+ * bf16 rows into 4 bits and back, every layer and head of kv (src and dst
+ * caches have the same layers and heads; their layouts are ppd_kv's):
+ * positions [src_pos, src_pos + n) to [dst_pos, dst_pos + n).
+ * ppd_kvq_dequantize rounds the held values to bfloat16.  n = 0 does nothing.
+ * PPD_ECAPACITY where a range leaves its cache.
+ */
+ppd_status ppd_kvq_quantize(const ppd_kvq *dst, int32_t dst_pos, const ppd_kv *src, int32_t src_pos, int32_t n,
+                            void *stream);
+ppd_status ppd_kvq_dequantize(const ppd_kvq *src, int32_t src_pos, const ppd_kv *dst, int32_t dst_pos, int32_t n,
+                              void *stream);
+
+/*
+ * Commit accepted rows: position L + k of kv <- tail row path[k], k < *n_path,
+ * every layer and head.  path, path_len, n_path as for ppd_kv_compact (the
+ * count is clamped to [0, min(path_len, capacity - L)], path entries to the
+ * tail); the tail is not changed.
+ */
+ppd_status ppd_kvq_commit(const ppd_kvq *kv, int32_t L, const int32_t *path, int32_t path_len,
+                          const int32_t *n_path, void *stream);
+
+/*
+ * Tree attention of one layer over B 4-bit caches (the attention inside
+ * ppd_verify_step_kvq, for callers with a forward pass of their own).
+ * Sequences, trees and rows are packed as for ppd_verify_batch: sequence s has
+ * rows [t0_s, t0_s + T[s]) of q, mask, out and lse.  Row t of head h attends
+ * to positions [0, L[s]) of kv head h / (n_heads / n_kv_heads) and to the tree
+ * rows of the tail (positions [0, T[s]), written before) whose mask bit is
+ * set, with scale 1 / sqrt(128).  Sums are float32, probabilities enter the
+ * value product with about 16 significant bits.  A row that sees nothing (L =
+ * 0 and an empty mask) gets zeros, and minus infinity in lse; one that sees a
+ * NaN or an infinity gets NaN where these enter, and no other row does.
+ *   q     device bfloat16 [T[0] + .. ][n_heads][128], 16-byte aligned
+ *   out   device bfloat16, the same shape and alignment (not q itself)
+ *   lse   device float32 [T[0] + ..][n_heads]: ln sum exp of the row's scores,
+ *         or NULL
+ *   ws    device workspace, 16-byte aligned, of
+ *         ppd_kvq_attention_workspace_bytes(n_heads, n_kv_heads, T[0] + ..),
+ *         one for each stream that calls may overlap on
+ */
+size_t ppd_kvq_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t t_max);
+ppd_status ppd_kvq_attention(int32_t n_heads, int32_t B, const ppd_kvq *kvs, int32_t layer, const int32_t *L,
+                             const int32_t *T, const void *q, const uint64_t *mask, void *out, float *lse, void *ws,
+                             size_t ws_bytes, void *stream);
+
+/*
+ * ppd_verify_step and ppd_verify_batch on 4-bit caches.  pos[s] is the
+ * position of sequence s's root (its node i sits at pos[s] + depth[i]): L[s]
+ * as long as nothing was evicted, else the number of tokens so far.  The tree's
+ * rows go to kvs[s].tail, whose capacity has to hold T[s]; L[s] <=
+ * kvs[s].capacity.  ws: ppd_kvq_workspace_bytes(model, all tree tokens).
+ *   q_out    device float32 [n_layers][all tree tokens][n_heads][128]: the
+ *            queries after RoPE, or NULL
+ *   lse_out  device float32 [n_layers][all tree tokens][n_heads], or NULL
+ * q_out and lse_out are what ppd_kvq_score reads.
+ */
+size_t ppd_kvq_workspace_bytes(const ppd_model *model, int32_t t_max);
+ppd_status ppd_verify_batch_kvq(const ppd_model *model, int32_t B, const ppd_kvq *kvs, const int32_t *L,
+                                const int32_t *pos, const int32_t *T, const int32_t *ids, const int32_t *depth,
+                                const uint64_t *mask, void *ws, size_t ws_bytes, float *logits, int32_t *pred,
+                                float *q_out, float *lse_out, void *stream);
+ppd_status ppd_verify_step_kvq(const ppd_model *model, const ppd_kvq *kv, int32_t L, int32_t pos, int32_t T,
+                               const int32_t *ids, const int32_t *depth, const uint64_t *mask, void *ws,
+                               size_t ws_bytes, float *logits, int32_t *pred, float *q_out, float *lse_out,
+                               void *stream);
+
+/*
+ * Accumulated attention weights (what ppd_kvq_evict ranks by): the weight
+ * that each cached position has in the attention of the accepted nodes, added
+ * up over the nodes and over the heads that share a kv head.  With n = *n_path
+ * (clamped as in ppd_kvq_commit), for every layer l and kv head g:
+ *   j < L       score_out[l][g][j] = score_in[l][g][j] + sum over i < n and
+ *               heads h of g of exp(q[l][path[i]][h] . key_j / sqrt(128) -
+ *               lse[l][path[i]][h])
+ *   j = L + k   (k < n, the position that ppd_kvq_commit gives path[k]) the
+ *               same sum over k <= i < n, with path[k]'s row of the tail as the
+ *               key and no score_in
+ * Called before the next step overwrites the tail.  A step adds n times the
+ * heads that share a kv head in all, since every weight of its rows is counted.
+ *   q        device [n_layers][rows][n_heads][128], q_dtype PPD_F32 or PPD_BF16,
+ *            16-byte aligned
+ *   lse      device float32 [n_layers][rows][n_heads]
+ *   rows     tree tokens of a layer in q and lse (>= T); a batch's sequence s
+ *            passes pointers to its row t0_s, T = T[s] and rows = all of them
+ *   path     device int32[path_len], n_path device int32 (path entries are
+ *            clamped to [0, T) and to the tail)
+ *   score_in, score_out   device float32 [n_layers][n_kv_heads][capacity];
+ *            may be the same buffer.  score_in NULL: zeros
+ */
+ppd_status ppd_kvq_score(const ppd_kvq *kv, int32_t L, int32_t n_heads, int32_t T, const void *q, int32_t q_dtype,
+                         const float *lse, int32_t rows, const int32_t *path, int32_t path_len,
+                         const int32_t *n_path, const float *score_in, float *score_out, void *stream);
+
+/*
+ * Cut a cache of L positions to n = min(L, budget): every layer and head keeps
+ * its first n_sink and its last n_recent positions and, of the others, those
+ * with the largest scores (equal scores: the smaller position; NaN after every
+ * number), moved up in order to positions [0, n) of dst.  Heads keep different
+ * positions.
+ *   src, dst   caches of the same layers and heads, either the same cache
+ *              (blocks and capacity alike) or apart; no tail is read
+ *   score      device float32 [n_layers][n_kv_heads][src capacity]
+ *   score_out  device float32 [n_layers][n_kv_heads][dst capacity]: the kept
+ *              positions' scores; may be score itself when src is dst
+ *   kept       device int32 [n_layers][n_kv_heads][budget]: the kept positions,
+ *              rising, in its first n entries
+ * 1 <= budget <= dst capacity, n_sink, n_recent >= 0, n_sink + n_recent <=
+ * budget, L <= src capacity.
+ */
+ppd_status ppd_kvq_evict(const ppd_kvq *src, const ppd_kvq *dst, int32_t L, int32_t budget, int32_t n_sink,
+                         int32_t n_recent, const float *score, float *score_out, int32_t *kept, void *stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities (beside
+ * ppd_accept's exact matching): sampling at a temperature whose emitted tokens
+ * follow the target's distribution, from given random numbers.
+ * At a node a (first the root) the target has weights w_i = exp((logits[a][i]
+ * - max) / temperature).  Start with the residual r = w and go through a's
+ * candidate children (ids < vocab) by node index; child c with token x is
+ * accepted iff
+ *     u[c] q_x Z < r_x,    Z = sum of r,
+ * and the walk goes on at c; else r = max(r - Z q, 0).  q is draft[a], the
+ * probabilities that a's children were drawn from, or without draft the
+ * certainty of x (children chosen without chance, as ppd_next_tree's): q_x =
+ * 1 and a rejected token leaves r.  Where no child is accepted the walk ends
+ * with the bonus token, the smallest i with r_0 + .. + r_i > u[0] (r_0 + r_1 +
+ * ..).  A residual that is left empty starts again at w.  Weights and sums are
+ * float64: of V tokens one's border is always near.
+ *   parent, ids   device int32[T], this step's tree
+ *   logits        device float32 [T][vocab]; temperature > 0
+ *   draft         device float32 [T][vocab], or NULL; entries that are negative
+ *                 or NaN count as 0
+ *   u             device float32[T], uniform in [0, 1): u[c] decides node c,
+ *                 u[0] the bonus token
+ *   path, n_path, next_tok   as ppd_accept gives them; path[n_path .. T) = -1
+ *   ws            device workspace, 16-byte aligned, of
+ *                 ppd_accept_sample_workspace_bytes(T, vocab)
+ * A NaN logit counts as minus infinity and, in a row on the path, sets
+ * PPD_DEV_NAN_LOGIT, as does a row without any weight (its bonus token is 0);
+ * a row with infinite logits divides all weight among these.  Parents outside
+ * [0, i) set PPD_DEV_BAD_PARENT and count as 0.
+ */
+size_t ppd_accept_sample_workspace_bytes(int32_t T, int32_t vocab);
+ppd_status ppd_accept_sample(int32_t T, const int32_t *parent, const int32_t *ids, int32_t vocab, const float *logits,
+                             float temperature, const float *draft, const float *u, int32_t *path, int32_t *n_path,
+                             int32_t *next_tok, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Tree sizing (Section 4.2, the hardware-aware tree size; Proposition 1 of

@@ -25,6 +25,7 @@ PPD_F32, PPD_BF16 = 0, 1
 PPD_T_MAX = 128
 PPD_MASK_WORDS = 2
 PPD_DEV_BAD_TOKEN, PPD_DEV_BAD_PARENT, PPD_DEV_NAN_LOGIT = 1, 2, 4
+PPD_KVQ_BLOCK, PPD_KVQ_BLOCK_BYTES = 32, 4608
 PPD_W_QKV, PPD_W_O, PPD_W_GATE_UP, PPD_W_DOWN, PPD_W_LM_HEAD = range(5)
 
 _STATUS_NAMES = {0: "PPD_OK", 1: "PPD_EINVAL", 2: "PPD_ETREE", 3: "PPD_ECAPACITY",
@@ -52,6 +53,11 @@ class ppd_model(C.Structure):
 class ppd_kv(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("capacity", C.c_int32),
                 ("len_dev", C.c_void_p)]
+
+
+class ppd_kvq(C.Structure):
+    _fields_ = [("blocks", C.c_void_p), ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("capacity", C.c_int32), ("tail", ppd_kv)]
 
 
 _lib = None
@@ -89,6 +95,26 @@ def lib() -> C.CDLL:
         L.ppd_packed_weight_bytes.restype = sz
         L.ppd_pack_weight.argtypes = [i32, i32, i32, vp, vp, vp]
         L.ppd_read_probe.argtypes = [vp, sz, vp, vp]
+        L.ppd_kvq_bytes.argtypes = [i32, i32, i32]
+        L.ppd_kvq_attention_workspace_bytes.argtypes = [i32, i32, i32]
+        L.ppd_kvq_workspace_bytes.argtypes = [P(ppd_model), i32]
+        L.ppd_accept_sample_workspace_bytes.argtypes = [i32, i32]
+        for f in ("ppd_kvq_bytes", "ppd_kvq_attention_workspace_bytes", "ppd_kvq_workspace_bytes",
+                  "ppd_accept_sample_workspace_bytes"):
+            getattr(L, f).restype = sz
+        L.ppd_kvq_quantize.argtypes = [P(ppd_kvq), i32, P(ppd_kv), i32, i32, vp]
+        L.ppd_kvq_dequantize.argtypes = [P(ppd_kvq), i32, P(ppd_kv), i32, i32, vp]
+        L.ppd_kvq_commit.argtypes = [P(ppd_kvq), i32, vp, i32, vp, vp]
+        L.ppd_kvq_attention.argtypes = [i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.ppd_verify_batch_kvq.argtypes = [P(ppd_model), i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp, vp, vp, vp]
+        L.ppd_verify_step_kvq.argtypes = [P(ppd_model), P(ppd_kvq), i32, i32, i32, vp, vp, vp, vp, sz, vp, vp, vp, vp,
+                                          vp]
+        L.ppd_kvq_score.argtypes = [P(ppd_kvq), i32, i32, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp]
+        L.ppd_kvq_evict.argtypes = [P(ppd_kvq), P(ppd_kvq), i32, i32, i32, i32, vp, vp, vp, vp]
+        L.ppd_accept_sample.argtypes = [i32, vp, vp, i32, vp, C.c_float, vp, vp, vp, vp, vp, vp, sz, vp]
+        for f in ("ppd_kvq_quantize", "ppd_kvq_dequantize", "ppd_kvq_commit", "ppd_kvq_attention",
+                  "ppd_verify_batch_kvq", "ppd_verify_step_kvq", "ppd_kvq_score", "ppd_kvq_evict", "ppd_accept_sample"):
+            getattr(L, f).restype = C.c_int
         for f in ("ppd_verify_step_static", "ppd_next_tree", "ppd_sparse_template", "ppd_verify_batch", "ppd_pack_weight", "ppd_workspace_init", "ppd_build_tree_mask", "ppd_verify_step", "ppd_accept",
                   "ppd_kv_compact", "ppd_device_status", "ppd_set_kernel_timer", "ppd_read_probe"):
             getattr(L, f).restype = C.c_int
@@ -256,6 +282,54 @@ class KVCache:
         self.desc = ppd_kv(_ptr(k), _ptr(v), self.capacity, _ptr(len_dev) or None)
 
 
+class KVQCache:
+    """4-bit cache: blocks uint8 [layers][kv_heads][capacity / 32][4608] (layout
+    in include/ppd.h) and, for the calls that read or write tree rows, their
+    bf16 staging cache `tail` (a KVCache of the same layers and heads)."""
+
+    def __init__(self, blocks, tail: Optional[KVCache] = None):
+        if blocks.dim() != 4 or blocks.shape[3] != PPD_KVQ_BLOCK_BYTES or blocks.element_size() != 1:
+            raise ValueError(f"blocks must be bytes [layers][kv_heads][capacity / 32][{PPD_KVQ_BLOCK_BYTES}]")
+        if not blocks.is_contiguous():
+            raise ValueError("blocks must be contiguous")
+        if tail is not None:
+            self._check_rows(tail, blocks.shape[:2], "tail")
+        self.blocks, self.tail = blocks, tail
+        self.n_layers, self.n_kv_heads = int(blocks.shape[0]), int(blocks.shape[1])
+        self.capacity = int(blocks.shape[2]) * PPD_KVQ_BLOCK
+        self.desc = ppd_kvq(_ptr(blocks), self.n_layers, self.n_kv_heads, self.capacity,
+                            tail.desc if tail is not None else ppd_kv())
+
+    @classmethod
+    def empty(cls, n_layers: int, n_kv_heads: int, capacity: int, tail_capacity: int = PPD_T_MAX, device="cuda"):
+        """A cache of `capacity` positions and its staging cache, uninitialised."""
+        import torch
+        if capacity < 1 or capacity % PPD_KVQ_BLOCK:
+            raise ValueError(f"capacity must be a positive multiple of {PPD_KVQ_BLOCK}")
+        k = torch.empty((n_layers, n_kv_heads, tail_capacity, 128), dtype=torch.bfloat16, device=device)
+        v = torch.empty((n_layers, n_kv_heads, 128, tail_capacity), dtype=torch.bfloat16, device=device)
+        blocks = torch.empty((n_layers, n_kv_heads, capacity // PPD_KVQ_BLOCK, PPD_KVQ_BLOCK_BYTES),
+                             dtype=torch.uint8, device=device)
+        return cls(blocks, KVCache(k, v))
+
+    @staticmethod
+    def _check_rows(kv: KVCache, heads, name):
+        """kv is a bf16 cache of [layers][kv_heads] = heads, head_dim 128."""
+        import torch
+        want = (heads[0], heads[1])
+        if (tuple(kv.k.shape) != (*want, kv.capacity, 128) or tuple(kv.v.shape) != (*want, 128, kv.capacity) or
+                kv.k.dtype != torch.bfloat16 or kv.v.dtype != torch.bfloat16):
+            raise ValueError(f"{name} must be a bf16 cache of {want[0]} layers, {want[1]} heads and 128 dims")
+        if not (kv.k.is_contiguous() and kv.v.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous")
+
+    def _on_device(self):
+        _dev(self.blocks, None, "blocks")
+        if self.tail is not None:
+            _dev(self.tail.k, None, "tail.k")
+            _dev(self.tail.v, None, "tail.v")
+
+
 # ---------------------------------------------------------------------------
 # the C ABI, one Python function per entry point
 
@@ -402,6 +476,199 @@ def ppd_kv_compact(model: Model, kv: KVCache, L: int, path, n_path, stream=None,
                                 _ptr(n_path), _stream(stream)))
 
 
+def _bytes(n: int) -> int:
+    if n == 0:
+        raise PPDError(PPD_EINVAL, ppd_last_error())
+    return int(n)
+
+
+def ppd_kvq_bytes(n_layers: int, n_kv_heads: int, capacity: int) -> int:
+    return _bytes(lib().ppd_kvq_bytes(int(n_layers), int(n_kv_heads), int(capacity)))
+
+
+def _rows_of(kv: KVQCache, other: KVCache, name: str):
+    kv._on_device()
+    KVQCache._check_rows(other, (kv.n_layers, kv.n_kv_heads), name)
+    _dev(other.k, None, name)
+    _dev(other.v, None, name)
+
+
+def ppd_kvq_quantize(kv: KVQCache, dst_pos: int, src: KVCache, src_pos: int, n: int, stream=None):
+    """n bf16 positions of src, from src_pos on, into kv from dst_pos on."""
+    _rows_of(kv, src, "src")
+    _check(lib().ppd_kvq_quantize(C.byref(kv.desc), int(dst_pos), C.byref(src.desc), int(src_pos), int(n),
+                                  _stream(stream)))
+
+
+def ppd_kvq_dequantize(kv: KVQCache, src_pos: int, dst: KVCache, dst_pos: int, n: int, stream=None):
+    """n positions of kv, from src_pos on, as bf16 into dst from dst_pos on."""
+    _rows_of(kv, dst, "dst")
+    _check(lib().ppd_kvq_dequantize(C.byref(kv.desc), int(src_pos), C.byref(dst.desc), int(dst_pos), int(n),
+                                    _stream(stream)))
+
+
+def ppd_kvq_commit(kv: KVQCache, L: int, path, n_path, stream=None, path_len: Optional[int] = None):
+    """Rows path[0], .., path[*n_path - 1] of kv.tail to positions L, L + 1, .. of kv."""
+    _i32(path=path, n_path=n_path)
+    kv._on_device()
+    n = int(path.numel()) if path_len is None else int(path_len)
+    _check(lib().ppd_kvq_commit(C.byref(kv.desc), int(L), _ptr(path), n, _ptr(n_path), _stream(stream)))
+
+
+def ppd_kvq_attention_workspace_bytes(n_heads: int, n_kv_heads: int, t_max: int) -> int:
+    return _bytes(lib().ppd_kvq_attention_workspace_bytes(int(n_heads), int(n_kv_heads), int(t_max)))
+
+
+def _kvq_batch(kvs, *counts):
+    """The sequences' descriptions and host int32 arrays of one entry each."""
+    B = len(kvs)
+    arrays = [_host_i32(a) for a in counts]
+    for a in arrays:
+        if a.shape != (B,):
+            raise ValueError("kvs and the sequences' counts differ in length")
+    for kv in kvs:
+        kv._on_device()
+    return (B, (ppd_kvq * max(B, 1))(*[kv.desc for kv in kvs]), *arrays)
+
+
+def ppd_kvq_attention(kvs: Sequence[KVQCache], layer: int, L: Sequence[int], T: Sequence[int], q, mask, out, ws,
+                      lse=None, stream=None):
+    """Tree attention of one layer: q, out bf16 [tokens][heads][128], lse float32
+    [tokens][heads] (optional), mask int64 / uint64 [tokens][2]."""
+    import torch
+    _dev(q, torch.bfloat16, "q")
+    _dev(out, torch.bfloat16, "out")
+    _dev(lse, torch.float32, "lse")
+    _dev(mask, None, "mask")
+    _dev(ws, None, "ws")
+    B, descs, Ls, Ts = _kvq_batch(kvs, L, T)
+    n = int(Ts.sum())
+    if q.dim() != 3 or tuple(q.shape) != (n, q.shape[1], 128) or out.shape != q.shape:
+        raise ValueError(f"q and out must be [{n}][heads][128]")
+    if lse is not None and tuple(lse.shape) != (n, q.shape[1]):
+        raise ValueError(f"lse must be [{n}][{q.shape[1]}]")
+    if mask.numel() * mask.element_size() < 16 * n:
+        raise ValueError(f"mask must be [{n}][2] words of 64 bits")
+    _check(lib().ppd_kvq_attention(int(q.shape[1]), B, C.cast(descs, C.c_void_p), int(layer), _np_ptr(Ls), _np_ptr(Ts),
+                                   _ptr(q), _ptr(mask), _ptr(out), _ptr(lse) or None, _ptr(ws),
+                                   ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def ppd_kvq_workspace_bytes(model: Model, t_max: int) -> int:
+    return _bytes(lib().ppd_kvq_workspace_bytes(C.byref(model.desc), int(t_max)))
+
+
+def _trace(model, n, q_out, lse_out):
+    import torch
+    sh = model.shape
+    _dev(q_out, torch.float32, "q_out")
+    _dev(lse_out, torch.float32, "lse_out")
+    if q_out is not None and tuple(q_out.shape) != (sh.n_layers, n, sh.n_heads, 128):
+        raise ValueError(f"q_out must be [{sh.n_layers}][{n}][{sh.n_heads}][128]")
+    if lse_out is not None and tuple(lse_out.shape) != (sh.n_layers, n, sh.n_heads):
+        raise ValueError(f"lse_out must be [{sh.n_layers}][{n}][{sh.n_heads}]")
+
+
+def ppd_verify_batch_kvq(model: Model, kvs: Sequence[KVQCache], L: Sequence[int], pos: Sequence[int], T: Sequence[int],
+                         ids, depth, mask, ws, logits, pred, q_out=None, lse_out=None, stream=None):
+    """ppd_verify_batch on 4-bit caches; pos: the roots' positions."""
+    import torch
+    _i32(ids=ids, depth=depth, pred=pred)
+    _dev(mask, None, "mask")
+    _dev(ws, None, "ws")
+    _dev(logits, torch.float32, "logits")
+    B, descs, Ls, ps, Ts = _kvq_batch(kvs, L, pos, T)
+    _trace(model, int(Ts.sum()), q_out, lse_out)
+    _check(lib().ppd_verify_batch_kvq(C.byref(model.desc), B, C.cast(descs, C.c_void_p), _np_ptr(Ls), _np_ptr(ps),
+                                      _np_ptr(Ts), _ptr(ids), _ptr(depth), _ptr(mask), _ptr(ws),
+                                      ws.numel() * ws.element_size(), _ptr(logits) or None, _ptr(pred),
+                                      _ptr(q_out) or None, _ptr(lse_out) or None, _stream(stream)))
+
+
+def ppd_verify_step_kvq(model: Model, kv: KVQCache, L: int, pos: int, T: int, ids, depth, mask, ws, logits, pred,
+                        q_out=None, lse_out=None, stream=None):
+    """ppd_verify_step on a 4-bit cache; pos: the root's position."""
+    import torch
+    _i32(ids=ids, depth=depth, pred=pred)
+    _dev(mask, None, "mask")
+    _dev(ws, None, "ws")
+    _dev(logits, torch.float32, "logits")
+    kv._on_device()
+    _trace(model, int(T), q_out, lse_out)
+    _check(lib().ppd_verify_step_kvq(C.byref(model.desc), C.byref(kv.desc), int(L), int(pos), int(T), _ptr(ids),
+                                     _ptr(depth), _ptr(mask), _ptr(ws), ws.numel() * ws.element_size(),
+                                     _ptr(logits) or None, _ptr(pred), _ptr(q_out) or None, _ptr(lse_out) or None,
+                                     _stream(stream)))
+
+
+def ppd_kvq_score(kv: KVQCache, L: int, q, lse, path, n_path, score_in, score_out, stream=None,
+                  path_len: Optional[int] = None):
+    """Attention weights of the accepted nodes added to score_in (None: zeros).
+    q float32 or bf16 [layers][T][heads][128], lse float32 [layers][T][heads]:
+    a tree's rows, which may be a slice [:, t0:t0 + T] of a batch's."""
+    import torch
+    _i32(path=path, n_path=n_path)
+    kv._on_device()
+    if q.dim() != 4 or q.shape[0] != kv.n_layers or q.shape[3] != 128 or tuple(lse.shape) != tuple(q.shape[:3]):
+        raise ValueError("q must be [layers][T][heads][128], lse [layers][T][heads]")
+    if q.dtype not in (torch.float32, torch.bfloat16) or lse.dtype != torch.float32:
+        raise ValueError("q must be float32 or bfloat16, lse float32")
+    nh, T = int(q.shape[2]), int(q.shape[1])
+    rows = T if kv.n_layers == 1 else q.stride(0) // (nh * 128)
+    for t, name, row in ((q, "q", nh * 128), (lse, "lse", nh)):
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if not t[0].is_contiguous() or (kv.n_layers > 1 and t.stride(0) != rows * row):
+            raise ValueError(f"{name} must be contiguous, or a slice of the rows of a contiguous tensor")
+    for t, name in ((score_in, "score_in"), (score_out, "score_out")):
+        _dev(t, torch.float32, name)
+        if t is not None and tuple(t.shape) != (kv.n_layers, kv.n_kv_heads, kv.capacity):
+            raise ValueError(f"{name} must be [{kv.n_layers}][{kv.n_kv_heads}][{kv.capacity}]")
+    n = int(path.numel()) if path_len is None else int(path_len)
+    _check(lib().ppd_kvq_score(C.byref(kv.desc), int(L), nh, T, _ptr(q), PPD_F32 if q.dtype == torch.float32 else PPD_BF16,
+                               _ptr(lse), int(rows), _ptr(path), n, _ptr(n_path), _ptr(score_in) or None,
+                               _ptr(score_out), _stream(stream)))
+
+
+def ppd_kvq_evict(src: KVQCache, dst: KVQCache, L: int, budget: int, n_sink: int, n_recent: int, score, score_out, kept,
+                  stream=None) -> int:
+    """The kept positions of src moved up into dst (which may be src); returns
+    how many stay, min(L, budget)."""
+    import torch
+    src._on_device()
+    dst._on_device()
+    _i32(kept=kept)
+    for t, name, kv in ((score, "score", src), (score_out, "score_out", dst)):
+        _dev(t, torch.float32, name)
+        if tuple(t.shape) != (kv.n_layers, kv.n_kv_heads, kv.capacity):
+            raise ValueError(f"{name} must be [{kv.n_layers}][{kv.n_kv_heads}][{kv.capacity}]")
+    if tuple(kept.shape) != (src.n_layers, src.n_kv_heads, budget):
+        raise ValueError(f"kept must be [{src.n_layers}][{src.n_kv_heads}][{budget}]")
+    _check(lib().ppd_kvq_evict(C.byref(src.desc), C.byref(dst.desc), int(L), int(budget), int(n_sink), int(n_recent),
+                               _ptr(score), _ptr(score_out), _ptr(kept), _stream(stream)))
+    return min(int(L), int(budget))
+
+
+def ppd_accept_sample_workspace_bytes(T: int, vocab: int) -> int:
+    return _bytes(lib().ppd_accept_sample_workspace_bytes(int(T), int(vocab)))
+
+
+def ppd_accept_sample(T: int, parent, ids, vocab: int, logits, temperature: float, draft, u, path, n_path, next_tok, ws,
+                      stream=None):
+    """ppd_accept's place at a temperature: children verified against the
+    target's probabilities with the draws u [T]; draft float32 [T][vocab] or
+    None (children chosen without chance)."""
+    import torch
+    _i32(parent=parent, ids=ids, path=path, n_path=n_path, next_tok=next_tok)
+    _dev(logits, torch.float32, "logits")
+    _dev(draft, torch.float32, "draft")
+    _dev(u, torch.float32, "u")
+    _dev(ws, None, "ws")
+    _check(lib().ppd_accept_sample(int(T), _ptr(parent), _ptr(ids), int(vocab), _ptr(logits), float(temperature),
+                                   _ptr(draft) or None, _ptr(u), _ptr(path), _ptr(n_path), _ptr(next_tok), _ptr(ws),
+                                   ws.numel() * ws.element_size(), _stream(stream)))
+
+
 def ppd_device_status(ws, clear: bool = False, stream=None) -> int:
     out = C.c_uint32(0)
     _check(lib().ppd_device_status(_ptr(ws), ws.numel() * ws.element_size(), C.byref(out),
@@ -441,4 +708,7 @@ def ppd_set_kernel_timer(kind, start_events=(), stop_events=()):
 
 __all__ = ["ppd_verify_step_static", "ppd_verify_batch", "ppd_next_tree", "ppd_sparse_template", "ppd_packed_weight_bytes", "ppd_pack_weight", "ppd_set_kernel_timer", "Model", "KVCache", "PPDError", "lib", "ppd_workspace_bytes", "ppd_workspace_init",
            "ppd_build_tree_mask", "ppd_verify_step", "ppd_accept", "ppd_kv_compact",
-           "ppd_device_status", "ppd_last_error", "ppd_read_probe"]
+           "ppd_device_status", "ppd_last_error", "ppd_read_probe", "KVQCache", "ppd_kvq_bytes", "ppd_kvq_quantize",
+           "ppd_kvq_dequantize", "ppd_kvq_commit", "ppd_kvq_attention_workspace_bytes", "ppd_kvq_attention",
+           "ppd_kvq_workspace_bytes", "ppd_verify_batch_kvq", "ppd_verify_step_kvq", "ppd_kvq_score", "ppd_kvq_evict",
+           "ppd_accept_sample_workspace_bytes", "ppd_accept_sample"]

@@ -68,23 +68,6 @@ __device__ __forceinline__ int row_of_key(int j) {
   return kt * 16 + a * 4 + e;
 }
 
-// Reductions over the four 16-lane groups of a wave (lanes l, l ^ 16,
-// l ^ 32, l ^ 48) with the gfx950 lane-swap instructions: swapping a value
-// with itself across 16-lane (32-lane) halves gives each lane its partner's
-// value in one of the two results and its own in the other.
-__device__ __forceinline__ float quad_max(float v) {
-  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
 // one 16-query tile of a wave
 struct QTile {
   u32x4 q[4][2];  // queries (B operand), dims 32 ds + 8 (lane / 16) .. + 7, parts hi, lo

@@ -1,0 +1,588 @@
+// Tree attention over a 4-bit prefix and the tree's bf16 rows, and the
+// accumulated attention weights of the accepted nodes.
+//
+// Rows.  The heads that share a kv head read the same keys, so a kv head's
+// rows are tree row x head, r = t G + a (a < G), in 16-row tiles.
+//
+// Products (v_mfma_f32_16x16x32_bf16; layouts as in the bf16 attention): S^T =
+// K Q^T with the 32 keys of a block as two 16-row A operands, O^T += V^T P^T
+// with 16 dims as the A operand.  A code word is one lane's 8 elements of an A
+// operand; it enters as x = (16 + c) / 2, exact in bfloat16 (kvq_expand), and
+// scale and zero are applied outside the products in float32:
+//   S[k][q] = sum_g 2 s_kg (sum_d x_kd q_d) + (z_kg - 16 s_kg) (sum_d q_d)
+//   O[d][q] = sum_k x_kd (2 s_kg P_kq) + sum_k (z_kg - 16 s_kg) P_kq
+// over the 64-dim groups g, so a held value is never rounded.  A block's
+// parameters go through a wave's own LDS, from which every lane reads those of
+// its 8 keys.
+#include <algorithm>
+
+#include "ppd_kvq.h"
+
+namespace {
+
+constexpr int NT = 512;              // eight waves
+constexpr int OROW = PPD_ATTN_OROW;  // partial row: 128 dims, m, l, padding (floats)
+constexpr int kGroupRows = 128;      // rows of a workgroup at most
+constexpr float kLn2 = 0.69314718055994531f;
+
+// what a wave keeps of one 16-row tile
+struct RTile {
+  u32x4 q[4][2];  // B operand, dims 32 ds + 8 (lane / 16) .. + 7, parts hi, lo
+  float qs[2];    // sums of q over the two groups' dims
+  uint64_t mk0, mk1;
+  floatx4 o[8];   // O^T: dims 16 dt + 4 (lane / 16) + e, row lane % 16
+  float pz[2];    // sums of P (z - 16 s), this lane's keys
+  float m_run, l_run;
+};
+
+__device__ __forceinline__ float sum8(u32x4 v) {
+  float s = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) s += __uint_as_float(v[w] << 16) + __uint_as_float(v[w] & 0xffff0000u);
+  return s;
+}
+
+// probabilities as two bf16 parts
+__device__ __forceinline__ void split8(const float (&v)[8], u32x4 &hi, u32x4 &lo) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = v[e] - bf16_to_f32(f32_to_bf16(v[e]));
+  hi = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  lo = u32x4{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]), pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7])};
+}
+
+// One block's scores (unscaled, hidden keys at -inf) into the running softmax:
+// the reference moves only when a maximum passes it by 8 (log2), P in pv.
+__device__ __forceinline__ void softmax_step(RTile &R, const float (&sv)[8], float c, float (&pv)[8]) {
+  const float lmax = c * fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])),
+                               fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+  if (__ballot(lmax > R.m_run + 8.f)) {
+    const float bmax = quad_max(lmax);
+    const bool need = bmax > R.m_run + 8.f;
+    const float alpha = need ? __builtin_amdgcn_exp2f(R.m_run - bmax) : 1.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) R.o[dt] *= alpha;
+    R.pz[0] *= alpha;
+    R.pz[1] *= alpha;
+    R.l_run *= alpha;
+    R.m_run = need ? bmax : R.m_run;
+  }
+  const float m_eff = R.m_run == -INFINITY ? 0.f : R.m_run;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    pv[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], c, -m_eff));
+    R.l_run += pv[e];
+  }
+}
+
+// NQ tiles a wave, QW waves side by side over tiles, PARS over blocks
+template <int NQ, int QW, int PARS, bool PLANES>
+__global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
+  static_assert(QW * PARS * 64 == NT && QW * NQ * 16 <= kGroupRows, "eight waves");
+  constexpr int RW = QW * NQ * 16;  // rows of the workgroup
+  __shared__ __attribute__((aligned(16))) float rows_s[PARS][RW][OROW];
+  __shared__ __attribute__((aligned(16))) floatx4 par_s[8][2 * kQB];  // per wave: affine pairs of 32 keys, 32 values
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qw = wave % QW, par = wave / QW;
+  const int lr = lane & 15, lg = lane >> 4;
+  // slot -> sequence, kv head, row group, split
+  int sq = 0;
+  for (int j = 1; j < p.sb.B; ++j) sq = (int)blockIdx.x >= p.slot0[j] ? j : sq;
+  const int t0 = p.sb.t0[sq], T = p.sb.t0[sq + 1] - t0, L = p.sb.L[sq];
+  const int G = p.nh / p.nkv, R = T * G, n_grp = (R + RW - 1) / RW;
+  const int KS = p.splits[sq];
+  int local = blockIdx.x - p.slot0[sq];
+  const int ks = local % KS;
+  local /= KS;
+  const int grp = local % n_grp, kvh = local / n_grp;
+  const int n4 = (L + kQB - 1) / kQB, nblk = n4 + (T + kQB - 1) / kQB;
+  const int b0 = min(nblk, ks * p.chunk[sq]), b1 = min(nblk, b0 + p.chunk[sq]);
+  const unsigned char *blocks = p.sb.blocks[sq] + (size_t)kvh * p.sb.nb[sq] * kQBytes;
+  const int tcap = p.sb.tcap[sq];
+  const bf16_t *tk = p.sb.tk[sq] + (size_t)kvh * tcap * 128, *tv = p.sb.tv[sq] + (size_t)kvh * 128 * tcap;
+  const int row0 = grp * RW;
+  const int MT = p.T_pad >> 4;
+
+  RTile rt[NQ];
+  const int n_live = min(NQ, ((min(R - row0, RW) + 15) / 16 - qw + QW - 1) / QW);
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int r = row0 + (qw + QW * i) * 16 + lr;
+    const bool live = r < R;
+    const int rc = min(r, R - 1);
+    const int tok = t0 + rc / G, head = kvh * G + rc % G;
+#pragma unroll
+    for (int ds = 0; ds < 4; ++ds) {
+      if constexpr (PLANES) {
+        const unsigned char *src = (const unsigned char *)p.q + plane_off(MT, tok, head * 128 + ds * 32 + lg * 8);
+        rt[i].q[ds][0] = *(const u32x4 *)src;
+        rt[i].q[ds][1] = *(const u32x4 *)(src + kPlaneLo);
+      } else {
+        rt[i].q[ds][0] = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + ds * 32 + lg * 8);
+        rt[i].q[ds][1] = u32x4{0u, 0u, 0u, 0u};
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+      rt[i].qs[g] = quad_sum((sum8(rt[i].q[2 * g][0]) + sum8(rt[i].q[2 * g + 1][0])) +
+                             (PLANES ? sum8(rt[i].q[2 * g][1]) + sum8(rt[i].q[2 * g + 1][1]) : 0.f));
+    if (PLANES && p.q_out && ks == 0 && par == 0 && live) {
+      float *dst = p.q_out + ((size_t)tok * p.nh + head) * 128 + lg * 8;
+#pragma unroll
+      for (int ds = 0; ds < 4; ++ds)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t a = rt[i].q[ds][0][w], b = rt[i].q[ds][1][w];
+          *(float2 *)(dst + ds * 32 + 2 * w) =
+              float2{__uint_as_float(a << 16) + __uint_as_float(b << 16),
+                     __uint_as_float(a & 0xffff0000u) + __uint_as_float(b & 0xffff0000u)};
+        }
+    }
+    rt[i].mk0 = live ? p.mask[2 * (size_t)tok] : 0ull;
+    rt[i].mk1 = live ? p.mask[2 * (size_t)tok + 1] : 0ull;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) rt[i].o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    rt[i].pz[0] = rt[i].pz[1] = 0.f;
+    rt[i].m_run = -INFINITY;
+    rt[i].l_run = 0.f;
+  }
+  const float c = p.scale_log2;
+
+  if (n_live > 0)
+    for (int blk = b0 + par; blk < b1; blk += PARS) {
+      if (blk < n4) {
+        const unsigned char *src = blocks + (size_t)blk * kQBytes;
+        u32x4 kw[2], vw[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          kw[t] = *(const u32x4 *)(src + (t * 64 + lane) * 16);
+          vw[t] = *(const u32x4 *)(src + kQV + (t * 64 + lane) * 16);
+        }
+        const u32x2 pr = *(const u32x2 *)(src + kQP + lane * 8);
+        const bool valid = blk * kQB + (lane & 31) < L;
+        const float2 a0 = kvq_affine(pr[0]), a1 = kvq_affine(pr[1]);
+        par_s[wave][lane] = valid ? floatx4{a0.x, a0.y, a1.x, a1.y} : floatx4{0.f, 0.f, 0.f, 0.f};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int vis = L - blk * kQB - 8 * lg;  // keys of the lane below it are in the prefix
+        float sv[NQ][8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          floatx4 acc[NQ][2];
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) acc[i][g] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+              const bf16x8 x = as_bf16x8(kvq_expand(kw[t][2 * g + d]));
+#pragma unroll
+              for (int part = PLANES ? 1 : 0; part >= 0; --part)
+#pragma unroll
+                for (int i = 0; i < NQ; ++i)
+                  acc[i][g] = mfma16x16x32(x, as_bf16x8(rt[i].q[2 * g + d][part]), acc[i][g]);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const floatx4 a = par_s[wave][8 * lg + 4 * t + e];
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+              float x = fmaf(a[0], acc[i][0][e], a[1] * rt[i].qs[0]);
+              x = fmaf(a[2], acc[i][1][e], fmaf(a[3], rt[i].qs[1], x));
+              sv[i][4 * t + e] = 4 * t + e < vis ? x : -INFINITY;
+            }
+          }
+        }
+        float pv[NQ][8];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) softmax_step(rt[i], sv[i], c, pv[i]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          u32x4 ph[NQ], pl[NQ];
+          float ps[NQ][8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float2 a = *((const float2 *)&par_s[wave][kQB + 8 * lg + u] + g);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+              ps[i][u] = pv[i][u] * a.x;
+              rt[i].pz[g] = fmaf(pv[i][u], a.y, rt[i].pz[g]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) split8(ps[i], ph[i], pl[i]);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const bf16x8 x = as_bf16x8(kvq_expand(vw[g][w]));
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) rt[i].o[4 * g + w] = mfma16x16x32(x, as_bf16x8(pl[i]), rt[i].o[4 * g + w]);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) rt[i].o[4 * g + w] = mfma16x16x32(x, as_bf16x8(ph[i]), rt[i].o[4 * g + w]);
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the parameters' LDS is written next
+      } else {
+        // tree rows: keys and values straight from the tail
+        const int k0 = (blk - n4) * kQB;
+        const int j0 = k0 + 8 * lg, keep_n = max(0, min(8, T - j0));  // keys of the lane that exist
+        float sv[NQ][8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bf16_t *kr = tk + (size_t)min(k0 + kvq_key_of(t, lr), tcap - 1) * 128 + lg * 8;
+          u32x4 kf[4];
+#pragma unroll
+          for (int ds = 0; ds < 4; ++ds) kf[ds] = *(const u32x4 *)(kr + ds * 32);
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) {
+            floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int part = PLANES ? 1 : 0; part >= 0; --part)
+#pragma unroll
+              for (int ds = 0; ds < 4; ++ds) acc = mfma16x16x32(as_bf16x8(kf[ds]), as_bf16x8(rt[i].q[ds][part]), acc);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sv[i][4 * t + e] = acc[e];
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        u32x4 ph[NQ], pl[NQ];
+        uint32_t seen[NQ];
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          const uint64_t win = j0 >= 128 ? 0ull : j0 >= 64 ? rt[i].mk1 >> (j0 - 64) : rt[i].mk0 >> j0;
+          const uint32_t vis = seen[i] = (uint32_t)win & ((1u << keep_n) - 1u);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) sv[i][u] = (vis >> u) & 1u ? sv[i][u] : -INFINITY;
+          float pv[8];
+          softmax_step(rt[i], sv[i], c, pv);
+          split8(pv, ph[i], pl[i]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          u32x4 vf = *(const u32x4 *)(tv + (size_t)(16 * dt + lr) * tcap + min(j0, tcap - 8));
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            vf[w] &= (2 * w < keep_n ? 0xffffu : 0u) | (2 * w + 1 < keep_n ? 0xffff0000u : 0u);
+          // infinities and NaN must not reach the rows that do not see them (0
+          // times them is NaN): they are taken out, and the rows that see one
+          // get NaN
+          u32x4 odd;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            odd[w] = ((vf[w] & 0x7f80u) == 0x7f80u ? 0x3f80u : 0u) | ((vf[w] & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0u);
+          if (__ballot(odd[0] | odd[1] | odd[2] | odd[3])) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) vf[w] &= (odd[w] & 0xffffu ? 0u : 0xffffu) | (odd[w] >> 16 ? 0u : 0xffff0000u);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+              u32x4 on;
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                on[w] = (seen[i] >> (2 * w) & 1u ? 0x3f80u : 0u) | (seen[i] >> (2 * w + 1) & 1u ? 0x3f800000u : 0u);
+              const floatx4 n = mfma16x16x32(as_bf16x8(odd), as_bf16x8(on), floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+              for (int e = 0; e < 4; ++e) rt[i].o[dt][e] = n[e] > 0.f ? NAN : rt[i].o[dt][e];
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) {
+            rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pl[i]), rt[i].o[dt]);
+            rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(ph[i]), rt[i].o[dt]);
+          }
+          if (dt & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+
+  // ---- the waves meet in LDS: thread -> row tid / 32 + 16 n, dims 4 (tid % 32) .. + 3
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const float l = quad_sum(rt[i].l_run), z0 = quad_sum(rt[i].pz[0]), z1 = quad_sum(rt[i].pz[1]);
+    if (i < n_live) {
+      float *row = rows_s[par][(qw + QW * i) * 16 + lr];
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) *(floatx4 *)(row + dt * 16 + lg * 4) = rt[i].o[dt] + (dt < 4 ? z0 : z1);
+      if (lg == 0) *(float2 *)(row + 128) = float2{rt[i].m_run, l};
+    }
+  }
+  __syncthreads();
+  const int d4 = (tid & 31) * 4;
+  for (int rl = tid >> 5; rl < min(R - row0, RW); rl += NT / 32) {
+    const int r = row0 + rl, tok = t0 + r / G, head = kvh * G + r % G;
+    float2 ml[PARS];
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) {
+      ml[w] = *(const float2 *)(rows_s[w][rl] + 128);
+      M = fmaxf(M, ml[w].x);
+    }
+    float l = 0.f;
+    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) {
+      const float f = ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - M);
+      l += f * ml[w].y;
+      o += f * *(const floatx4 *)(rows_s[w][rl] + d4);
+    }
+    const size_t at = (size_t)tok * p.nh + head;
+    if (KS == 1) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      if constexpr (PLANES)
+        store_plane4((unsigned char *)p.out, MT, tok, head * 128 + d4, {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
+      else
+        *(u32x2 *)((bf16_t *)p.out + at * 128 + d4) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+      if (p.lse && d4 == 0) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+    } else {
+      float *row = p.part + ((size_t)ks * p.sb.t0[p.sb.B] * p.nh + at) * OROW;
+      *(floatx4 *)(row + d4) = o;
+      if (d4 == 0) *(float2 *)(row + 128) = float2{M, l};
+    }
+  }
+}
+
+// the splits of a row, added in order; 32 threads a row
+template <bool PLANES>
+__global__ __launch_bounds__(NT) void kvq_merge_kernel(KvqAttnLaunch p) {
+  const int n_rows = p.sb.t0[p.sb.B] * p.nh;
+  const int at = blockIdx.x * (NT / 32) + (threadIdx.x >> 5), d4 = (threadIdx.x & 31) * 4;
+  if (at >= n_rows) return;
+  const int tok = at / p.nh, head = at % p.nh;
+  int sq = 0;
+  for (int j = 1; j < p.sb.B; ++j) sq = tok >= p.sb.t0[j] ? j : sq;
+  const int KS = p.splits[sq];
+  if (KS == 1) return;  // already final
+  float M = -INFINITY, l = 0.f;
+  floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < KS; ++s) {
+    const float *row = p.part + ((size_t)s * n_rows + at) * OROW;
+    const float2 ml = *(const float2 *)(row + 128);
+    const floatx4 x = *(const floatx4 *)(row + d4);
+    if (ml.x > M) {
+      const float f = exp2f(M - ml.x);
+      o *= f;
+      l *= f;
+      M = ml.x;
+    }
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+    l += f * ml.y;
+    o += f * x;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (PLANES)
+    store_plane4((unsigned char *)p.out, p.T_pad >> 4, tok, head * 128 + d4, {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
+  else
+    *(u32x2 *)((bf16_t *)p.out + (size_t)at * 128 + d4) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+  if (p.lse && d4 == 0) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------
+// Accumulated weights.  Here the rows are the A operand and the keys the B
+// operand, S = Q K^T: a lane then holds one key and four rows, and the sum over
+// rows is over its registers and four lane groups.  Rows: path node x head, r =
+// i G + a, in passes of kPassTiles tiles, whose queries lie in LDS as three
+// bf16 parts (a float32 to its last bits, so that a weight is exact to
+// float32's own rounding of its exponent).  Workgroup: (layer and kv head, run
+// of blocks), four waves, a block a wave.
+
+constexpr int kPassTiles = 2;
+struct ScoreRow {
+  float qs0, qs1, lse2;  // sums of q over the groups, ln sum exp in log2
+  int node;              // place on the path; rows that do not exist: -1
+};
+
+__global__ __launch_bounds__(256) void kvq_score_kernel(KvqScoreLaunch p) {
+  __shared__ u32x4 q_s[kPassTiles][4][3][64];
+  __shared__ ScoreRow row_s[kPassTiles * 16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int lh = blockIdx.x, layer = lh / p.nkv, kvh = lh % p.nkv;
+  const int n = max(0, min(*p.n_path, min(p.path_len, p.cap - p.L)));
+  const int G = p.nh / p.nkv, R = n * G;
+  const int n4 = (p.L + kQB - 1) / kQB, nblk = n4 + (n + kQB - 1) / kQB;
+  const unsigned char *blocks = p.blocks + (size_t)lh * p.nb * kQBytes;
+  const bf16_t *tk = p.tk + (size_t)lh * p.tcap * 128;
+  const float *in = p.in ? p.in + (size_t)lh * p.cap : nullptr;
+  float *out = p.out + (size_t)lh * p.cap;
+  const float c = p.scale_log2;
+  for (int r0 = 0; r0 == 0 || r0 < R; r0 += kPassTiles * 16) {
+    __syncthreads();
+    const int tiles = min(kPassTiles, (R - r0 + 15) / 16);
+    // row tid / 8 (of 32), dims 16 (tid % 8) .. + 15
+    {
+      const int r = r0 + tid / 8, rl = tid / 8;
+      const bool live = r < R;
+      const int i = live ? r / G : 0, head = kvh * G + (live ? r % G : 0);
+      const int node = n > 0 ? max(0, min(p.path[i], p.T - 1)) : 0;
+      const size_t at = ((size_t)layer * p.rows + node) * p.nh + head;
+      float sum = 0.f;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int d = 16 * (tid % 8) + 8 * b;
+        float v[8];
+        if (!live) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        } else if (p.q_bf16) {
+          const u32x4 w = *(const u32x4 *)((const bf16_t *)p.q + at * 128 + d);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = bf16_to_f32((w[e >> 1] >> (16 * (e & 1))) & 0xffffu);
+        } else {
+          const floatx4 x = *(const floatx4 *)((const float *)p.q + at * 128 + d);
+          const floatx4 y = *(const floatx4 *)((const float *)p.q + at * 128 + d + 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = x[e], v[4 + e] = y[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[e];
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+            v[2 * e] -= __uint_as_float(w[e] << 16);
+            v[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+          }
+          q_s[rl >> 4][d >> 5][part][(rl & 15) + 16 * ((d >> 3) & 3)] = w;
+        }
+      }
+      // the four threads of a group
+      sum += __shfl_xor(sum, 1, 64);
+      sum += __shfl_xor(sum, 2, 64);
+      const float other = __shfl_xor(sum, 4, 64);
+      if (tid % 8 == 0)
+        row_s[rl] = ScoreRow{sum, other, live ? p.lse[at] * 1.4426950408889634f : INFINITY, live ? i : -1};
+    }
+    __syncthreads();
+    for (int blk = blockIdx.y * 4 + wave; blk < nblk; blk += gridDim.y * 4) {
+      const bool tree = blk >= n4;
+      const int k0 = tree ? (blk - n4) * kQB : blk * kQB;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int j = kvq_key_of(t, lr);  // this lane's key of the block
+        u32x4 b[4];
+        float4 a = float4{1.f, 0.f, 1.f, 0.f};
+        if (!tree) {
+          const unsigned char *src = blocks + (size_t)blk * kQBytes;
+          const u32x4 w = *(const u32x4 *)(src + (t * 64 + lane) * 16);
+          const u32x2 pr = *(const u32x2 *)(src + kQP + j * 8);
+#pragma unroll
+          for (int ds = 0; ds < 4; ++ds) b[ds] = kvq_expand(w[ds]);
+          const float2 a0 = kvq_affine(pr[0]), a1 = kvq_affine(pr[1]);
+          a = float4{a0.x, a0.y, a1.x, a1.y};
+        } else {
+          const int node = max(0, min(p.path[min(k0 + j, n - 1)], min(p.T, p.tcap) - 1));
+#pragma unroll
+          for (int ds = 0; ds < 4; ++ds) b[ds] = *(const u32x4 *)(tk + (size_t)node * 128 + ds * 32 + lg * 8);
+        }
+        float w = 0.f;
+        for (int m = 0; m < tiles; ++m) {
+          floatx4 acc[2];
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            acc[g] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int part = 2; part >= 0; --part)
+#pragma unroll
+              for (int d = 0; d < 2; ++d)
+                acc[g] = mfma16x16x32(as_bf16x8(q_s[m][2 * g + d][part][lane]), as_bf16x8(b[2 * g + d]), acc[g]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const ScoreRow row = row_s[m * 16 + 4 * lg + e];
+            const float s = fmaf(a.x, acc[0][e], a.y * row.qs0) + fmaf(a.z, acc[1][e], a.w * row.qs1);
+            const bool seen = row.node >= 0 && (!tree || row.node >= k0 + j);
+            w += seen ? __builtin_amdgcn_exp2f(fmaf(s, c, -row.lse2)) : 0.f;
+          }
+        }
+        w = quad_sum(w);
+        const int pos = tree ? p.L + k0 + j : k0 + j;
+        if (lg == 0 && (tree ? k0 + j < n : pos < p.L)) {
+          const float base = r0 > 0 ? out[pos] : tree || !in ? 0.f : in[pos];
+          out[pos] = base + w;
+        }
+      }
+    }
+  }
+}
+
+}  // namespace
+
+// 16-row tiles a wave holds and waves side by side, by the most tiles a kv head has
+static void kvq_shape(int tiles, int *nq, int *qw) {
+  *nq = 1;
+  *qw = tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
+}
+
+int kvq_attn_max_splits(int nkv) { return std::max(1, std::min(64, 512 / nkv)); }
+
+size_t kvq_attn_part_bytes(int nh, int nkv, int T) {
+  return (size_t)kvq_attn_max_splits(nkv) * T * nh * OROW * sizeof(float);
+}
+
+void kvq_attn_plan(KvqAttnLaunch &a) {
+  const int B = a.sb.B, G = a.nh / a.nkv, cap = kvq_attn_max_splits(a.nkv);
+  a.max_splits = cap;
+  a.tiles = 1;
+  for (int j = 0; j < B; ++j) a.tiles = std::max(a.tiles, ((a.sb.t0[j + 1] - a.sb.t0[j]) * G + 15) / 16);
+  int nq, qw;
+  kvq_shape(a.tiles, &nq, &qw);
+  const int rw = 16 * nq * qw, pars = 8 / qw;
+  long total = 0;
+  int nblk[PPD_BATCH_MAX], units[PPD_BATCH_MAX];
+  for (int j = 0; j < B; ++j) {
+    const int T = a.sb.t0[j + 1] - a.sb.t0[j];
+    nblk[j] = (a.sb.L[j] + kQB - 1) / kQB + (T + kQB - 1) / kQB;
+    units[j] = a.nkv * ((T * G + rw - 1) / rw);
+    total += (long)units[j] * nblk[j];
+  }
+  const long share = std::max<long>(pars, (total + 255) / 256);
+  a.n_slots = 0;
+  for (int j = 0; j < B; ++j) {
+    a.splits[j] = (int)std::max<long>(1, std::min<long>(cap, nblk[j] / share));
+    const int per = (nblk[j] + a.splits[j] - 1) / a.splits[j];
+    a.chunk[j] = (per + pars - 1) / pars * pars;
+    a.splits[j] = (nblk[j] + a.chunk[j] - 1) / a.chunk[j];
+    a.slot0[j] = a.n_slots;
+    a.n_slots += units[j] * a.splits[j];
+  }
+}
+
+template <bool PLANES>
+static hipError_t launch_attn(const KvqAttnLaunch &a, hipStream_t s) {
+  auto kernel = a.tiles <= 1   ? kvq_attention_kernel<1, 1, 8, PLANES>
+                : a.tiles <= 2 ? kvq_attention_kernel<1, 2, 4, PLANES>
+                : a.tiles <= 4 ? kvq_attention_kernel<1, 4, 2, PLANES>
+                               : kvq_attention_kernel<1, 8, 1, PLANES>;
+  const bool merge = *std::max_element(a.splits, a.splits + a.sb.B) > 1;
+  const hipEvent_t ev0 = (hipEvent_t)a.ev_start, ev1 = (hipEvent_t)a.ev_stop;
+  if (ev0)
+    hipExtLaunchKernelGGL(kernel, dim3(a.n_slots), dim3(NT), 0, s, ev0, merge ? (hipEvent_t) nullptr : ev1, 0, a);
+  else
+    hipLaunchKernelGGL(kernel, dim3(a.n_slots), dim3(NT), 0, s, a);
+  if (merge) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const dim3 grid((a.sb.t0[a.sb.B] * a.nh + NT / 32 - 1) / (NT / 32));
+    if (ev1)
+      hipExtLaunchKernelGGL(kvq_merge_kernel<PLANES>, grid, dim3(NT), 0, s, (hipEvent_t) nullptr, ev1, 0, a);
+    else
+      hipLaunchKernelGGL(kvq_merge_kernel<PLANES>, grid, dim3(NT), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_kvq_attn(const KvqAttnLaunch &a, hipStream_t s) {
+  return a.planes ? launch_attn<true>(a, s) : launch_attn<false>(a, s);
+}
+
+hipError_t launch_kvq_score(const KvqScoreLaunch &p, hipStream_t s) {
+  const int heads = p.layers * p.nkv, nblk = (p.L + p.path_len + 2 * kQB - 2) / kQB;
+  const int want = std::max(1, 1024 / heads);
+  hipLaunchKernelGGL(kvq_score_kernel, dim3(heads, std::max(1, std::min(want, (nblk + 3) / 4))), dim3(256), 0, s, p);
+  return hipGetLastError();
+}

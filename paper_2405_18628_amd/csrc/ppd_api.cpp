@@ -5,13 +5,15 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
 #include <functional>
 #include <string>
 
-#include "ppd_internal.h"
+#include "ppd_kvq.h"
+#include "ppd_sample.h"
 
 namespace {
 
@@ -428,10 +430,12 @@ SeqBatch seq_batch(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t *
   return sb;
 }
 
+// the step on 4-bit caches (kvq set): the caches of `kvs` are the staging
+// caches, in which the trees start at position 0 (Ls = 0)
 ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t *Ls,
                      const int32_t *Ts, const int32_t *ids, const int32_t *depth,
                      const uint64_t *mask, void *ws, const WsLayout &w, float *logits,
-                     int32_t *pred, hipStream_t s) {
+                     int32_t *pred, hipStream_t s, const KvqStep *kvq = nullptr) {
   const int H = m->hidden, nh = m->n_heads, nkv = m->n_kv_heads;
   int T = 0;
   for (int j = 0; j < B; ++j) T += Ts[j];
@@ -475,7 +479,7 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
   // embedding, the first norm's operand and sums of squares (one partial per
   // row), rotary table, zeroed counters
   PPD_TRY_HIP(launch_embed(PPD_BF16, m->tok_emb, m->prompt_emb, ids, depth,
-                           seq_batch(m, B, kvs, Ls, Ts, 0), m->head_dim, m->rope_base, rope,
+                           seq_batch(m, B, kvs, kvq ? kvq->pos : Ls, Ts, 0), m->head_dim, m->rope_base, rope,
                            m->vocab, m->n_prompt, H, x, (const bf16_t *)m->attn_norm[0], xg, ss, ctr,
                            w.n_ctr, status, s));
   int n_ss = 1;
@@ -492,7 +496,22 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
   a.status = status;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt(128.0));
   a.sb = seq_batch(m, B, kvs, Ls, Ts, 0);
-  set_attn_plan(a, Ls, Ts, sync);
+  KvqAttnLaunch qa{};
+  if (kvq) {
+    qa.q = q;
+    qa.out = attn_o;
+    qa.planes = 1;
+    qa.T_pad = Tp;
+    qa.mask = mask;
+    qa.part = at<float>(ws, w.total);
+    qa.nh = nh;
+    qa.nkv = nkv;
+    qa.scale_log2 = a.scale_log2;
+    qa.sb = kvq_seqs(B, kvq->kvs, kvq->L, Ts, 0);
+    kvq_attn_plan(qa);
+  } else {
+    set_attn_plan(a, Ls, Ts, sync);
+  }
   uint32_t *attn_ctr = ctr + (size_t)(4 * m->n_layers + 1) * 256;
   const float inv_h = 1.0f / (float)H;
 
@@ -521,10 +540,18 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
     timer_events(TK_QKV, &qg.ev_start, &qg.ev_stop);
     PPD_TRY_HIP(launch_gemm_bf16(qg, s));
     // tree attention
-    a.sb = sb;
-    a.ctr = attn_ctr + (size_t)l * 256;
-    timer_events(TK_ATTN, &a.ev_start, &a.ev_stop);
-    PPD_TRY_HIP(launch_attn_bf16(a, s));
+    if (kvq) {
+      qa.sb = kvq_seqs(B, kvq->kvs, kvq->L, Ts, l);
+      qa.q_out = kvq->q_out ? kvq->q_out + (size_t)l * T * nh * 128 : nullptr;
+      qa.lse = kvq->lse_out ? kvq->lse_out + (size_t)l * T * nh : nullptr;
+      timer_events(TK_ATTN, &qa.ev_start, &qa.ev_stop);
+      PPD_TRY_HIP(launch_kvq_attn(qa, s));
+    } else {
+      a.sb = sb;
+      a.ctr = attn_ctr + (size_t)l * 256;
+      timer_events(TK_ATTN, &a.ev_start, &a.ev_stop);
+      PPD_TRY_HIP(launch_attn_bf16(a, s));
+    }
     // O projection + residual; the MLP norm's operand and sums of squares
     GemmLaunch o = g;
     setup(o, SH_O);
@@ -745,6 +772,53 @@ ppd_status ppd_verify_batch(const ppd_model *model, int32_t B, const ppd_kv *kvs
   return step_f32(model, &kvs[0], L[0], T[0], ids, depth, mask, ws, w, logits, pred, s);
 }
 
+size_t ppd_kvq_workspace_bytes(const ppd_model *model, int32_t t_max) {
+  if (check_model(model) != PPD_OK) return 0;
+  if (t_max < 1 || t_max > PPD_T_MAX || model->dtype != PPD_BF16) {
+    fail(PPD_EINVAL, "t_max must be in [1, %d], the model bf16", PPD_T_MAX);
+    return 0;
+  }
+  return layout_of(model, t_max).total + kvq_attn_part_bytes(model->n_heads, model->n_kv_heads, t_max);
+}
+
+ppd_status ppd_verify_batch_kvq(const ppd_model *model, int32_t B, const ppd_kvq *kvs, const int32_t *L,
+                                const int32_t *pos, const int32_t *T, const int32_t *ids, const int32_t *depth,
+                                const uint64_t *mask, void *ws, size_t ws_bytes, float *logits, int32_t *pred,
+                                float *q_out, float *lse_out, void *stream) {
+  ppd_status st = check_model(model);
+  if (st != PPD_OK) return st;
+  if (model->dtype != PPD_BF16) return fail(PPD_EUNSUPPORTED, "4-bit caches need a bf16 model");
+  int total = 0;
+  if ((st = kvq_check_seqs(B, kvs, L, T, &total)) != PPD_OK) return st;
+  if (!pos) return fail(PPD_EINVAL, "NULL sequence arrays");
+  ppd_kv tails[PPD_BATCH_MAX];
+  const int32_t zero[PPD_BATCH_MAX] = {0};
+  for (int j = 0; j < B; ++j) {
+    if (kvs[j].n_layers != model->n_layers || kvs[j].n_kv_heads != model->n_kv_heads)
+      return fail(PPD_EINVAL, "sequence %d: a cache of %d layers and %d heads, not the model's", j, kvs[j].n_layers,
+                  kvs[j].n_kv_heads);
+    if (pos[j] < 0) return fail(PPD_EINVAL, "pos[%d] must be >= 0", j);
+    tails[j] = kvs[j].tail;
+  }
+  if (!ids || !depth || !mask || !pred) return fail(PPD_EINVAL, "NULL tree or output pointer");
+  if ((uintptr_t)q_out % 16) return fail(PPD_EINVAL, "q_out must be 16-byte aligned");
+  const WsLayout w = layout_of(model, total);
+  const size_t need = w.total + kvq_attn_part_bytes(model->n_heads, model->n_kv_heads, total);
+  if (!ws || ws_bytes < need)
+    return fail(PPD_EWORKSPACE, "workspace of %zu bytes is smaller than the %zu required", ws_bytes, need);
+  g_timer.next = 0;
+  const KvqStep step{kvs, L, pos, q_out, lse_out};
+  return step_bf16(model, B, tails, zero, T, ids, depth, mask, ws, w, logits, pred, (hipStream_t)stream, &step);
+}
+
+ppd_status ppd_verify_step_kvq(const ppd_model *model, const ppd_kvq *kv, int32_t L, int32_t pos, int32_t T,
+                               const int32_t *ids, const int32_t *depth, const uint64_t *mask, void *ws,
+                               size_t ws_bytes, float *logits, int32_t *pred, float *q_out, float *lse_out,
+                               void *stream) {
+  return ppd_verify_batch_kvq(model, 1, kv, &L, &pos, &T, ids, depth, mask, ws, ws_bytes, logits, pred, q_out,
+                              lse_out, stream);
+}
+
 ppd_status ppd_verify_step(const ppd_model *model, const ppd_kv *kv, int32_t L, int32_t T,
                            const int32_t *ids, const int32_t *depth, const uint64_t *mask,
                            void *ws, size_t ws_bytes, float *logits, int32_t *pred,
@@ -765,6 +839,43 @@ ppd_status ppd_accept(int32_t T, const int32_t *parent, const int32_t *ids, cons
   if (!ws || ws_bytes < 16) return fail(PPD_EWORKSPACE, "workspace (status word) required");
   PPD_TRY_HIP(launch_accept(T, parent, ids, pred, vocab, path, n_path, next_tok, (uint32_t *)ws,
                             (hipStream_t)stream));
+  return PPD_OK;
+}
+
+size_t ppd_accept_sample_workspace_bytes(int32_t T, int32_t vocab) {
+  if (T < 1 || T > PPD_T_MAX || vocab < 1) {
+    fail(PPD_EINVAL, "T must be in [1, %d], vocab positive", PPD_T_MAX);
+    return 0;
+  }
+  return sample_workspace_bytes(T, vocab);
+}
+
+ppd_status ppd_accept_sample(int32_t T, const int32_t *parent, const int32_t *ids, int32_t vocab, const float *logits,
+                             float temperature, const float *draft, const float *u, int32_t *path, int32_t *n_path,
+                             int32_t *next_tok, void *ws, size_t ws_bytes, void *stream) {
+  const size_t need = ppd_accept_sample_workspace_bytes(T, vocab);
+  if (!need) return PPD_EINVAL;
+  if (!(temperature > 0.f) || !std::isfinite(temperature))
+    return fail(PPD_EINVAL, "temperature must be positive and finite (ppd_accept is the greedy form)");
+  if (!parent || !ids || !logits || !u || !path || !n_path || !next_tok) return fail(PPD_EINVAL, "NULL argument");
+  if (!ws || ws_bytes < need)
+    return fail(PPD_EWORKSPACE, "workspace of %zu bytes is smaller than the %zu required", ws_bytes, need);
+  if ((uintptr_t)ws % 16) return fail(PPD_EINVAL, "ws must be 16-byte aligned");
+  SampleLaunch p{};
+  p.parent = parent;
+  p.ids = ids;
+  p.T = T;
+  p.vocab = vocab;
+  p.logits = logits;
+  p.draft = draft;
+  p.u = u;
+  p.temperature = temperature;
+  p.path = path;
+  p.n_path = n_path;
+  p.next_tok = next_tok;
+  p.status = (uint32_t *)ws;
+  p.node = (SampleNode *)((char *)ws + 256);
+  PPD_TRY_HIP(launch_sample(p, (hipStream_t)stream));
   return PPD_OK;
 }
 

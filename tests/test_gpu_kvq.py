@@ -1,0 +1,487 @@
+"""The 4-bit cache on the GPU against plain 64-bit implementations
+(kvq_reference): storing and reading back, commit, attention, accumulated
+weights, eviction, and the step on it.
+
+Tolerances.  Storing is defined by float32 operations and compared bit for
+bit, whatever lies around the written positions included.
+Attention: a score's error is at most `ds` = 2^-24 (terms + 8) times the sum
+of its terms' magnitudes, scaled (float32 sums of 128 products; the operands
+2 s x and z - 16 s are larger than the held values, so the bound is taken from
+them); a probability is then off by 2 ds + 2^-16 (two bf16 parts) of itself
+and the output by twice that times the largest held value, plus half a bf16
+step, 2^-8 of it.  lse is off by ds + 2^-22 (1 + |lse|).
+Weights: each is off by ds + 2^-22 (1 + |s| + |lse|) of itself, and a sum of n
+of them and a start by 2^-24 n of it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import kvq_reference as R
+import paper_2405_18628_amd as ppd
+from gpu_cases import say
+
+pytestmark = pytest.mark.gpu
+
+
+def _gen(seed):
+    g = torch.Generator("cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _bf16(shape, g, scale=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(torch.bfloat16)
+
+
+def _rows(layers, heads, cap, g, spread=3.0):
+    """A bf16 cache whose dims differ in size and offset, as keys' do."""
+    w = torch.rand((layers, heads, 1, 128), generator=g, device="cuda") * spread
+    k = (_bf16((layers, heads, cap, 128), g).float() * w + (w - spread / 2)).to(torch.bfloat16)
+    v = _bf16((layers, heads, 128, cap), g)
+    return ppd.KVCache(k.contiguous(), v.contiguous())
+
+
+def _garbage(layers, heads, cap, g):
+    b = torch.randint(0, 256, (layers, heads, cap // 32, 4608), generator=g, device="cuda", dtype=torch.uint8)
+    b[..., 4096:].fill_(255)  # every scale and zero NaN
+    return b
+
+
+def _tail(layers, heads, T, cap, g):
+    """T rows, NaN behind them."""
+    kv = _rows(layers, heads, cap, g)
+    kv.k[:, :, T:].fill_(float("nan"))
+    kv.v[:, :, :, T:].fill_(float("nan"))
+    return kv
+
+
+def _cache(layers, heads, L, cap, T, tcap, seed):
+    """A 4-bit cache with L rows (stored by the library), and its rows."""
+    g = _gen(seed)
+    kv = ppd.KVQCache(_garbage(layers, heads, cap, g), _tail(layers, heads, T, tcap, g))
+    src = _rows(layers, heads, max(8, (L + 7) // 8 * 8), g)
+    if L:
+        ppd.ppd_kvq_quantize(kv, 0, src, 0, L)
+    torch.cuda.synchronize()
+    return kv, src
+
+
+def _f32(t):
+    return t.float().cpu().numpy()
+
+
+# ---------------------------------------------------------------------------
+# storing and reading back
+
+
+@pytest.mark.parametrize("layers,heads,n,src_pos,dst_pos,cap", [
+    (1, 1, 1, 0, 0, 32), (1, 2, 1, 5, 31, 32), (2, 1, 31, 1, 1, 64), (1, 2, 33, 0, 31, 96), (2, 2, 64, 3, 0, 64),
+    (1, 1, 70, 2, 61, 160), (3, 1, 32, 8, 32, 64), (1, 3, 97, 0, 7, 128)])
+def test_quantize_and_back_bit_exact(layers, heads, n, src_pos, dst_pos, cap):
+    g = _gen(n * 1000 + dst_pos)
+    scap = (src_pos + n + 7) // 8 * 8
+    src = _rows(layers, heads, scap, g)
+    src.k[0, 0, src_pos] = 1.5                            # even groups: scale 0
+    src.v[0, 0, :64, src_pos + n - 1] = -0.0
+    src.k[-1, -1, src_pos + n // 2, 70] = float("inf")    # groups without a value
+    src.v[-1, -1, 3, src_pos + n // 2] = float("nan")
+    src.v[0, 0, 64:, src_pos] *= 1e-39                    # subnormal numbers
+    src.k[-1, 0, src_pos, :64] = torch.linspace(-3e38, 3e38, 64).to(torch.bfloat16).cuda()  # a range past float32
+    blocks = torch.randint(0, 256, (layers, heads, cap // 32, 4608), generator=g, device="cuda", dtype=torch.uint8)
+    want = R.heads_of(blocks).copy()
+    kv = ppd.KVQCache(blocks)
+    say(f"[quantize] n={n} {src_pos}->{dst_pos}")
+    ppd.ppd_kvq_quantize(kv, dst_pos, src, src_pos, n)
+    torch.cuda.synchronize()
+    for l in range(layers):
+        for h in range(heads):
+            R.store(want[l, h], dst_pos, _f32(src.k[l, h, src_pos:src_pos + n]),
+                    _f32(src.v[l, h, :, src_pos:src_pos + n].t()))
+    assert np.array_equal(R.heads_of(blocks), want)
+    # back, to other positions, between rows that stay
+    back = ppd.KVCache(torch.full((layers, heads, scap + 16, 128), 7.0, dtype=torch.bfloat16, device="cuda"),
+                       torch.full((layers, heads, 128, scap + 16), 7.0, dtype=torch.bfloat16, device="cuda"))
+    ppd.ppd_kvq_dequantize(kv, dst_pos, back, 5, n)
+    torch.cuda.synchronize()
+    for l in range(layers):
+        for h in range(heads):
+            k, v = R.load(want[l, h], dst_pos + n, np.float32)
+            ek = np.full((scap + 16, 128), 7.0, np.float32)
+            ev = ek.copy()
+            ek[5:5 + n], ev[5:5 + n] = R.bf16(k[dst_pos:]), R.bf16(v[dst_pos:])
+            assert np.array_equal(_f32(back.k[l, h]), ek, equal_nan=True)
+            assert np.array_equal(_f32(back.v[l, h]).T, ev, equal_nan=True)
+
+
+@pytest.mark.parametrize("L,T,path,n", [(0, 1, [0], 1), (31, 8, [0, 3, 7], 3), (30, 128, [0, 5, 9, 60, 127], 5),
+                                        (5, 128, list(range(128)), 128), (64, 9, [0, 8, 2], 0), (63, 20, [0, 1], 9),
+                                        (90, 20, [0, 3, 4, 5, 6, 7, 8], 7)])
+def test_commit(L, T, path, n):
+    """Rows in path order; counts past the path or the cache are clamped, the
+    tail stays, len_dev follows."""
+    layers, heads, cap = 2, 2, 160 if n > 90 else 96
+    g = _gen(L)
+    tail = _tail(layers, heads, T, (T + 7) // 8 * 8, g)
+    tail.len_dev = torch.zeros(1, dtype=torch.int32, device="cuda")
+    tail = ppd.KVCache(tail.k, tail.v, tail.len_dev)
+    blocks = torch.randint(0, 256, (layers, heads, cap // 32, 4608), generator=g, device="cuda", dtype=torch.uint8)
+    want, k0 = R.heads_of(blocks).copy(), tail.k.clone()
+    ppd.ppd_kvq_commit(ppd.KVQCache(blocks, tail), L, torch.tensor(path, dtype=torch.int32, device="cuda"),
+                       torch.tensor([n], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    m = min(n, len(path), cap - L)
+    for l in range(layers):
+        for h in range(heads):
+            if m:
+                R.store(want[l, h], L, _f32(tail.k[l, h, path[:m]]), _f32(tail.v[l, h][:, path[:m]].t()))
+    assert np.array_equal(R.heads_of(blocks), want)
+    assert int(tail.len_dev.item()) == L + m and torch.equal(tail.k.view(torch.int16), k0.view(torch.int16))
+
+
+# ---------------------------------------------------------------------------
+# attention
+
+
+def _tree_mask(T, rng, kind):
+    if kind == "tree":
+        parent = [-1] + [int(rng.integers(max(0, i - 7), i)) for i in range(1, T)]
+        return ppd.ppd_build_tree_mask(parent)[1]
+    bits = rng.random((T, 128)) < 0.3
+    if kind == "empty":
+        bits[::3] = False          # rows that see no tree row
+    m = np.zeros((T, 2), np.uint64)
+    for j in range(128):           # bits past the tree are set as well: they mean nothing
+        m[:, j // 64] |= bits[:, j].astype(np.uint64) << np.uint64(j % 64)
+    return m
+
+
+def _score_bound(q, words, L, kt):
+    """ds for one head (see the module's docstring): float64 [T][L + T]."""
+    d = np.arange(128) // 64
+    k = np.zeros((L, 128))
+    if L:
+        pos = np.arange(L)
+        sz = words[(pos // 32)[:, None], 1024 + 2 * (pos % 32)[:, None] + np.arange(2)[None]]
+        s = (sz << np.uint32(16)).view(np.float32).astype(np.float64)
+        z = (sz & np.uint32(0xffff0000)).view(np.float32).astype(np.float64)
+        k = 31 * s[:, d] + np.abs(z - 16 * s)[:, d]
+    return 2.0 ** -24 * 136 / math.sqrt(128) * (np.abs(q) @ np.concatenate((k, np.abs(kt))).T)
+
+
+def _check_attention(nh, nkv, Ts, Ls, kind="tree", seed=0, extra=0, stream=None, layer=0, layers=1):
+    say(f"[attention] nh={nh} nkv={nkv} T={Ts} L={Ls} {kind}")
+    rng = np.random.default_rng(seed)
+    g = _gen(seed)
+    kvs = [_cache(layers, nkv, L, max(32, (L + extra + 31) // 32 * 32), T, (T + 7) // 8 * 8 + 8 * (i % 2), seed + i)[0]
+           for i, (T, L) in enumerate(zip(Ts, Ls))]
+    n = sum(Ts)
+    mask = np.concatenate([_tree_mask(T, rng, kind) for T in Ts])
+    q = _bf16((n, nh, 128), g, 1.0)
+    out = torch.full((n, nh, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((n, nh), float("nan"), device="cuda")
+    ws = torch.empty(ppd.ppd_kvq_attention_workspace_bytes(nh, nkv, n), dtype=torch.uint8, device="cuda").fill_(255)
+    ppd.ppd_workspace_init(ws)
+    dm = torch.from_numpy(mask.view(np.int64)).cuda()
+    torch.cuda.synchronize()
+    ppd.ppd_kvq_attention(kvs, layer, Ls, Ts, q, dm, out, ws, lse=lse, stream=stream)
+    torch.cuda.synchronize()
+    qf, got, got_lse = _f32(q).astype(np.float64), _f32(out), lse.cpu().numpy()
+    t0 = 0
+    for kv, T, L in zip(kvs, Ts, Ls):
+        words = R.heads_of(kv.blocks)[layer]
+        vis = R.mask_bits(mask[t0:t0 + T], T)
+        for a in range(nh):
+            h = a // (nh // nkv)
+            k, v = R.load(words[h], L)
+            kt, vt = _f32(kv.tail.k[layer, h, :T]).astype(np.float64), _f32(kv.tail.v[layer, h, :, :T]).T.astype(np.float64)
+            ref, rl = R.attention(qf[t0:t0 + T, a], k, v, kt, vt, vis)
+            ds = _score_bound(qf[t0:t0 + T, a], words[h], L, kt).max(1)
+            vmax = max(np.abs(v).max() if L else 0, np.abs(vt).max())
+            tol = 2.0 ** -8 * np.abs(ref) + (2 * (2 * ds + 2.0 ** -16) * vmax)[:, None] + 1e-30
+            err = np.abs(got[t0:t0 + T, a] - ref)
+            assert (err <= tol).all(), (a, float((err - tol).max()), np.argwhere(~(err <= tol))[:3])
+            on = np.isfinite(rl)
+            e = np.abs(got_lse[t0:t0 + T, a] - np.where(on, rl, 0.0))
+            assert np.array_equal(got_lse[t0:t0 + T, a][~on], rl[~on])
+            assert (e[on] <= ds[on] + 2.0 ** -22 * (1 + np.abs(rl[on]))).all(), (a, float(e[on].max()))
+        t0 += T
+    assert ppd.ppd_device_status(ws) == 0
+    return out, lse
+
+
+@pytest.mark.parametrize("nh,nkv", [(1, 1), (4, 4), (6, 2), (8, 1), (14, 2)])
+@pytest.mark.parametrize("T,L", [(1, 1), (1, 0), (16, 33), (17, 31), (33, 300), (64, 64), (65, 7), (128, 95)])
+def test_attention(nh, nkv, T, L):
+    _check_attention(nh, nkv, [T], [L], seed=T * 7 + L)
+
+
+@pytest.mark.parametrize("nh,nkv,T,L", [(4, 4, 1, 5000), (8, 2, 5, 2049), (32, 32, 64, 1023), (2, 1, 100, 3333)])
+def test_attention_split_over_keys(nh, nkv, T, L):
+    _check_attention(nh, nkv, [T], [L], seed=L, extra=100)
+
+
+@pytest.mark.parametrize("kind", ["random", "empty"])
+@pytest.mark.parametrize("Ts,Ls", [([5, 30], [0, 0]), ([1, 2, 3, 4], [0, 700, 32, 1]), ([128], [0]),
+                                   ([8] * 16, [50 * i for i in range(16)])])
+def test_attention_batches_and_masks(Ts, Ls, kind):
+    """Any mask, bits past a tree among them; rows that see nothing."""
+    _check_attention(6, 2, Ts, Ls, kind, seed=len(Ts))
+
+
+def test_attention_of_a_layer():
+    _check_attention(4, 2, [9], [40], seed=3, layer=2, layers=3)
+
+
+def test_attention_nan_rows_reach_only_those_who_see_them():
+    """A group without a value poisons its kv head, as a NaN in a bf16 cache
+    does; a hidden tree row that holds NaN reaches nobody."""
+    kv, _ = _cache(1, 2, 40, 64, 4, 8, 1)
+    src = _rows(1, 2, 8, _gen(2))
+    src.k[0, 1, 3, 5] = float("nan")
+    ppd.ppd_kvq_quantize(kv, 36, src, 0, 4)
+    kv.tail.v[0, 0, :, 2] = float("nan")
+    mask = np.array([[1, 0], [3, 0], [5, 0], [9, 0]], np.uint64)
+    q = _bf16((4, 2, 128), _gen(3))
+    out = torch.empty_like(q)
+    ws = torch.zeros(ppd.ppd_kvq_attention_workspace_bytes(2, 2, 4), dtype=torch.uint8, device="cuda")
+    ppd.ppd_kvq_attention([kv], 0, [40], [4], q, torch.from_numpy(mask.view(np.int64)).cuda(), out, ws)
+    bad = torch.isnan(out.float()).any(-1).cpu().numpy()
+    assert bad[:, 1].all() and bad[:, 0].tolist() == [False, False, True, False]
+
+
+def test_attention_same_bits_again_and_on_another_stream():
+    """The result does not depend on what ran before or on the stream."""
+    a = _check_attention(8, 2, [20, 33], [4000, 100], seed=9)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b = _check_attention(8, 2, [20, 33], [4000, 100], seed=9, stream=s)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_attention_captured():
+    """Two captured graphs with a workspace each, replayed in turn with eager work between."""
+    cases = []
+    for seed, (T, L) in enumerate(((7, 900), (40, 3000))):
+        kv, _ = _cache(1, 4, L, (L + 31) // 32 * 32, T, (T + 7) // 8 * 8, seed)
+        m = torch.from_numpy(_tree_mask(T, np.random.default_rng(seed), "tree").view(np.int64)).cuda()
+        q = _bf16((T, 8, 128), _gen(seed))
+        out = torch.empty_like(q)
+        ws = torch.empty(ppd.ppd_kvq_attention_workspace_bytes(8, 4, T), dtype=torch.uint8, device="cuda")
+        ppd.ppd_workspace_init(ws)
+        run = lambda kv=kv, m=m, q=q, out=out, ws=ws, T=T, L=L: ppd.ppd_kvq_attention([kv], 0, [L], [T], q, m, out, ws)
+        run()
+        torch.cuda.synchronize()
+        ref = out.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        cases.append((graph, out, ref, q, run))  # run holds the graph's inputs
+    for _ in range(3):
+        for graph, out, ref, q, _ in cases:
+            out.fill_(0)
+            graph.replay()
+            assert float(q.float().sum()) == float(q.float().sum())
+            torch.cuda.synchronize()
+            assert torch.equal(out, ref)
+
+
+def test_attention_offsets_past_32_bits():
+    """A head of 2^24 positions is 2.4 GB: rows behind the 2 GB mark, and the
+    second head's.  2^20 rows are stored 15 times over, so the sums over the
+    prefix are 15 times those of the rows themselves (and of the rest)."""
+    cap, chunk, rest, nh = 1 << 24, 1 << 20, 77, 2
+    g = _gen(0)
+    kv = ppd.KVQCache(torch.empty((1, 2, cap // 32, 4608), dtype=torch.uint8, device="cuda"), _tail(1, 2, 3, 8, g))
+    src = _rows(1, 2, chunk, g)
+    L = 15 * chunk + rest
+    for i in range(16):
+        ppd.ppd_kvq_quantize(kv, i * chunk, src, 0, min(chunk, L - i * chunk))
+    say("[attention] L past 15 million")
+    q = _bf16((3, nh, 128), g)
+    out, lse = torch.empty_like(q), torch.empty((3, nh), device="cuda")
+    ws = torch.empty(ppd.ppd_kvq_attention_workspace_bytes(nh, 2, 3), dtype=torch.uint8, device="cuda")
+    ppd.ppd_workspace_init(ws)
+    mask = torch.tensor([[1, 0], [3, 0], [7, 0]], dtype=torch.int64, device="cuda")
+    ppd.ppd_kvq_attention([kv], 0, [L], [3], q, mask, out, ws, lse=lse)
+    back = ppd.KVCache(torch.empty((1, 2, chunk, 128), dtype=torch.bfloat16, device="cuda"),
+                       torch.empty((1, 2, 128, chunk), dtype=torch.bfloat16, device="cuda"))
+    ppd.ppd_kvq_dequantize(kv, 14 * chunk, back, 0, chunk)
+    torch.cuda.synchronize()
+    for h in range(2):
+        # held values rounded to bf16 (2^-9 each): averaged over millions of keys
+        k, v = back.k[0, h].double(), back.v[0, h].double().t()
+        kt, vt = kv.tail.k[0, h, :3].double(), kv.tail.v[0, h, :, :3].double().t()
+        for t in range(3):
+            x = q[t, h].double()
+            s, st = k @ x / math.sqrt(128), kt[:t + 1] @ x / math.sqrt(128)
+            m = float(torch.maximum(s.max(), st.max()))
+            w = torch.exp(s - m) * torch.where(torch.arange(chunk, device="cuda") < rest, 16.0, 15.0)
+            wt = torch.exp(st - m)
+            tot = float(w.sum() + wt.sum())
+            ref = (w @ v + wt @ vt[:t + 1]) / tot
+            # scores off by |q| |k| 2^-9 / sqrt(128) at most, the weights by as much of themselves
+            ds = float(x.norm() * k.norm(dim=1).max()) * 2.0 ** -9 / math.sqrt(128)
+            assert abs(float(lse[t, h]) - (m + math.log(tot))) <= ds
+            assert float((out[t, h].double() - ref).abs().max()) <= (2 * ds + 2.0 ** -8) * float(v.abs().max())
+
+
+# ---------------------------------------------------------------------------
+# accumulated weights
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("layers,nh,nkv,L,T,path,n", [
+    (2, 4, 4, 33, 8, [0, 2, 5], 3), (1, 6, 2, 0, 4, [0, 1], 2), (3, 8, 1, 100, 20, list(range(20)), 20),
+    (2, 2, 2, 64, 8, [0, 1], 0), (1, 14, 2, 300, 128, list(range(0, 128, 2)), 64), (1, 2, 1, 31, 128, list(range(128)), 128),
+    (1, 2, 2, 95, 8, [0, 3, 4], 3), (2, 4, 2, 257, 3, [0], 9)])
+def test_score(layers, nh, nkv, L, T, path, n, dtype):
+    cap = (L + 1 + 31) // 32 * 32
+    say(f"[score] nh={nh} nkv={nkv} L={L} cap={cap} T={T} n={n} {dtype}")
+    g = _gen(L + T)
+    kv, _ = _cache(layers, nkv, L, cap, T, (T + 7) // 8 * 8, L)
+    rows, t0 = T + 5, 2                     # a sequence of a batch: a slice of its rows
+    q = (torch.randn((layers, rows, nh, 128), generator=g, device="cuda")).to(dtype)[:, t0:t0 + T]
+    lse = (math.log(L + 2) + torch.rand((layers, rows, nh), generator=g, device="cuda"))[:, t0:t0 + T]
+    base = torch.rand((layers, nkv, cap), generator=g, device="cuda")
+    out = torch.full_like(base, -5.0)
+    dp, dn = torch.tensor(path, dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    ppd.ppd_kvq_score(kv, L, q, lse, dp, dn, base, out)
+    again = base.clone()
+    ppd.ppd_kvq_score(kv, L, q, lse, dp, dn, again, again)          # in place
+    fresh = torch.full_like(base, -5.0)
+    ppd.ppd_kvq_score(kv, L, q, lse, dp, dn, None, fresh)
+    torch.cuda.synchronize()
+    m = min(n, len(path), cap - L)
+    G = nh // nkv
+    for l in range(layers):
+        words = R.heads_of(kv.blocks)[l]
+        for h in range(nkv):
+            k = R.load(words[h], L)[0]
+            kt = _f32(kv.tail.k[l, h, :T]).astype(np.float64)
+            qh = q[l, :, h * G:(h + 1) * G].double().cpu().numpy()
+            lh = lse[l, :, h * G:(h + 1) * G].double().cpu().numpy()
+            ref = R.score(qh, lh, k, kt, path[:m], base[l, h].double().cpu().numpy())
+            ds = max(_score_bound(qh[:, a], words[h], L, kt).max() for a in range(G))
+            s_max = (np.abs(qh).max(0).max(0) @ np.concatenate((np.abs(k), np.abs(kt))).max(0)) / math.sqrt(128)
+            tol = ref * (ds + 2.0 ** -22 * (1 + s_max + np.abs(lh).max()) + 2.0 ** -24 * (m * G + 1))
+            err = np.abs(out[l, h, :L + m].cpu().numpy() - ref)
+            assert (err <= tol).all(), (l, h, float((err - tol).max()))
+            zero = R.score(qh, lh, k, kt, path[:m], np.zeros(L))
+            err = np.abs(fresh[l, h, :L + m].cpu().numpy() - zero)
+            assert (err <= tol).all()
+    assert bool((out[..., L + m:] == -5.0).all()) and torch.equal(again[..., L + m:], base[..., L + m:])
+    assert torch.equal(again[..., :L + m], out[..., :L + m])
+
+
+def test_scores_add_up_to_the_rows():
+    """Weights from the attention's own lse: a path of n nodes adds n times
+    the heads of a kv head, to the bounds above (5e-5 here)."""
+    nh, nkv, L, T, path = 8, 2, 500, 30, [0, 4, 9, 17]
+    kv, _ = _cache(1, nkv, L, 544, T, 32, 4)
+    parent = [-1] * T
+    for a, b in zip(path, path[1:]):
+        parent[b] = a
+    for i in range(1, T):
+        parent[i] = 0 if parent[i] < 0 else parent[i]
+    mask = torch.from_numpy(ppd.ppd_build_tree_mask(parent)[1].view(np.int64)).cuda()
+    q = _bf16((T, nh, 128), _gen(8))
+    out, lse = torch.empty_like(q), torch.empty((T, nh), device="cuda")
+    ws = torch.zeros(ppd.ppd_kvq_attention_workspace_bytes(nh, nkv, T), dtype=torch.uint8, device="cuda")
+    ppd.ppd_kvq_attention([kv], 0, [L], [T], q, mask, out, ws, lse=lse)
+    score = torch.zeros((1, nkv, 544), device="cuda")
+    ppd.ppd_kvq_score(kv, L, q[None], lse[None], torch.tensor(path, dtype=torch.int32, device="cuda"),
+                      torch.tensor([4], dtype=torch.int32, device="cuda"), score, score)
+    total = score.double().sum(-1).cpu().numpy()
+    assert np.abs(total / (4 * nh // nkv) - 1).max() < 5e-5, total
+
+
+# ---------------------------------------------------------------------------
+# eviction
+
+
+def _scores(kind, shape, g):
+    u = torch.rand(shape, generator=g, device="cuda")
+    if kind == "equal":
+        return torch.full(shape, 0.25, device="cuda")
+    if kind == "few":                       # many equal values, signs and zeros of both signs
+        return torch.floor(u * 5) - 2.0 + torch.where(u < 0.5, -0.0, 0.0)
+    if kind == "odd":                       # infinities, NaN, subnormals
+        x = u * 1e-40
+        x[..., ::7] = float("nan")
+        x[..., 3::11] = float("inf")
+        x[..., 5::13] = -float("inf")
+        return x
+    return u ** 4
+
+
+@pytest.mark.parametrize("kind", ["plain", "equal", "few", "odd"])
+@pytest.mark.parametrize("L,budget,sink,recent", [(1, 1, 0, 0), (40, 33, 2, 5), (100, 100, 3, 8), (95, 31, 0, 31),
+                                                  (64, 200, 10, 10), (1500, 1, 1, 0), (2500, 1027, 4, 100), (70, 7, 0, 0),
+                                                  (10, 30, 8, 8)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict(kind, L, budget, sink, recent, in_place):
+    layers, heads = 2, 3
+    cap = (max(L, budget) + 31) // 32 * 32
+    say(f"[evict] L={L} budget={budget} {kind} in_place={in_place}")
+    g = _gen(L + budget)
+    kv, _ = _cache(layers, heads, L, cap, 1, 8, L)
+    score = _scores(kind, (layers, heads, cap), g)
+    before, sc = R.heads_of(kv.blocks).copy(), score.cpu().numpy()
+    n = min(L, budget)
+    dst = kv if in_place else ppd.KVQCache(torch.randint(0, 256, (layers, heads, (budget + 31) // 32, 4608), generator=g,
+                                                         device="cuda", dtype=torch.uint8))
+    held = R.heads_of(dst.blocks).copy()
+    out = score if in_place else torch.full((layers, heads, dst.capacity), -5.0, device="cuda")
+    out0 = out.clone()
+    kept = torch.full((layers, heads, budget), -7, dtype=torch.int32, device="cuda")
+    assert ppd.ppd_kvq_evict(kv, dst, L, budget, sink, recent, score, out, kept) == n
+    torch.cuda.synchronize()
+    after = R.heads_of(dst.blocks)
+    for l in range(layers):
+        for h in range(heads):
+            at = R.keep(sc[l, h], L, budget, sink, recent)
+            assert kept[l, h].cpu().tolist() == at + [-7] * (budget - n)
+            assert np.array_equal(out[l, h, :n].cpu().numpy(), sc[l, h, at], equal_nan=True)
+            assert torch.equal(out[l, h, n:].view(torch.int32), out0[l, h, n:].view(torch.int32))
+            for got, rows in zip(R.load(after[l, h], n), R.load(before[l, h], L)):
+                assert np.array_equal(got, rows[at], equal_nan=True)
+            # positions behind the kept ones are as they were
+            for got, rows in zip(R.load(after[l, h], dst.capacity), R.load(held[l, h], dst.capacity)):
+                assert np.array_equal(got[n:], rows[n:], equal_nan=True)
+
+
+def test_evict_captured_after_score():
+    """score -> evict, in place, captured and replayed from the same start."""
+    kv, _ = _cache(2, 2, 300, 320, 4, 8, 6)
+    q, lse = _bf16((2, 4, 4, 128), _gen(1)), torch.full((2, 4, 4), 6.0, device="cuda")
+    path = torch.tensor([0, 2, 3, 0], dtype=torch.int32, device="cuda")
+    n_path = torch.tensor([3], dtype=torch.int32, device="cuda")
+    score = torch.rand((2, 2, 320), generator=_gen(2), device="cuda")
+    kept = torch.zeros((2, 2, 200), dtype=torch.int32, device="cuda")
+    b0, s0 = kv.blocks.clone(), score.clone()
+
+    def step():
+        ppd.ppd_kvq_score(kv, 300, q, lse, path, n_path, score, score)
+        ppd.ppd_kvq_commit(kv, 300, path, n_path)
+        ppd.ppd_kvq_evict(kv, kv, 303, 200, 4, 20, score, score, kept)
+
+    def restore():
+        kv.blocks.copy_(b0)
+        score.copy_(s0)
+        kept.zero_()
+        torch.cuda.synchronize()
+    step()
+    torch.cuda.synchronize()
+    ref = [t.clone() for t in (kv.blocks, score, kept)]
+    restore()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        restore()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip((kv.blocks, score, kept), ref):
+            assert torch.equal(got, want)
