@@ -875,6 +875,7 @@ ppd_status ppd_accept_sample(int32_t T, const int32_t *parent, const int32_t *id
   p.next_tok = next_tok;
   p.status = (uint32_t *)ws;
   p.node = (SampleNode *)((char *)ws + 256);
+  p.part = (SamplePart *)((char *)ws + 256);
   PPD_TRY_HIP(launch_sample(p, (hipStream_t)stream));
   return PPD_OK;
 }

@@ -3,6 +3,12 @@
 
 #include "ppd_internal.h"
 
+struct SamplePart {
+  float m;       // the largest logit of the part (NaN left out)
+  uint32_t nan;  // it holds a NaN
+  double rest;   // sum of exp((l - m) / temperature) without the node's drafted tokens
+};
+
 struct SampleNode {
   int taken;  // the accepted child, or -1
   int bonus;  // then the bonus token
@@ -17,7 +23,8 @@ struct SampleLaunch {
   float temperature;
   int32_t *path, *n_path, *next_tok;
   uint32_t *status;
-  SampleNode *node;  // [T]
+  SamplePart *part;  // without draft: [T][parts]
+  SampleNode *node;  // with draft: [T]
 };
 size_t sample_workspace_bytes(int T, int vocab);
 hipError_t launch_sample(const SampleLaunch &p, hipStream_t s);

@@ -167,12 +167,12 @@ def accept_sample(parent, ids, vocab, logits, temperature, draft, u):
                 took = c
                 break
             r = np.where(q == 1.0, 0.0, r) if draft is None else np.maximum(r - r.sum() * q, 0.0)
-            if not r.sum() > 0:
-                r = w.copy()
         if took < 0:
             break
         node = took
         path.append(node)
+    if not r.sum() > 0:
+        r = w
     if not r.any():
         return path, 0, flagged
     over = np.cumsum(r) > float(u[0]) * r.sum()

@@ -113,7 +113,7 @@ def test_borders_of_the_draws():
         assert got == ([0], bonus, 0), (u0, got)
     assert _call([-1, 0], [0, 31], V, logits, 1.0, None, np.array([0.0, 0.0], np.float32))[0] == [0]      # no weight
     assert _call([-1, 0], [0, 29], V, logits, 1.0, None, np.array([0.0, 0.0], np.float32))[0] == [0, 1]
-    # all weight on a token that is rejected by a draw of 1: the residual is empty and starts again
+    # all weight on a token that is rejected by a draw of 1: the residual is empty, the bonus token drawn from the weights
     logits[:] = -np.inf
     logits[:, 7] = 1.0
     for draft in (None, np.eye(V, dtype=np.float32)[[7, 7]]):
