@@ -8,8 +8,9 @@
 //
 // Weights and sums are float64: with V tokens V borders compete for one draw,
 // and float32's rounding moves each by about 1e-7 of the whole.  exp is
-// table-driven (Tang, 1989): e^x = 2^(n / 64) e^r, |r| <= ln 2 / 128, from 64
-// table entries and five terms of e^r's series, 14 operations.
+// table-driven (Tang, 1989): e^x = 2^(k / 64) e^r, |r| <= ln 2 / 128, from 64
+// table entries and five terms of e^r's series (4e-14 of a weight), eleven
+// float64 operations.
 //
 // Without draft probabilities a rejected token leaves the residual whole, so a
 // node needs one sum over its row, that of the tokens none of its children
@@ -24,7 +25,7 @@
 // max(w - a - b, 0): one row of weights, one of probabilities and a number, but
 // a sum over the row for each rejection, the next depending on it.  A workgroup
 // settles a node alone: weights in registers, probabilities in LDS.
-#include <algorithm>
+#include <cfloat>
 
 #include "ppd_sample.h"
 
@@ -42,10 +43,31 @@ __device__ __forceinline__ int parent_of(const SampleLaunch &p, int t) {
   return t == 0 ? -1 : up >= 0 && up < t ? up : 0;
 }
 
+// sum over the wave in every lane, by lane permutations in the vector unit
+// (pairs, quads, halves of 16, 16, then the row and half swaps)
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double join64(uint32_t lo, uint32_t hi) {
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v += dpp64<0xb1>(v);   // quad_perm [1,0,3,2]
+  v += dpp64<0x4e>(v);   // quad_perm [2,3,0,1]
+  v += dpp64<0x141>(v);  // row_half_mirror
+  v += dpp64<0x140>(v);  // row_mirror
+  uint64_t b = __builtin_bit_cast(uint64_t, v);
+  auto l16 = __builtin_amdgcn_permlane16_swap((uint32_t)b, (uint32_t)b, false, false);
+  auto h16 = __builtin_amdgcn_permlane16_swap((uint32_t)(b >> 32), (uint32_t)(b >> 32), false, false);
+  v = join64(l16[0], h16[0]) + join64(l16[1], h16[1]);
+  b = __builtin_bit_cast(uint64_t, v);
+  auto l32 = __builtin_amdgcn_permlane32_swap((uint32_t)b, (uint32_t)b, false, false);
+  auto h32 = __builtin_amdgcn_permlane32_swap((uint32_t)(b >> 32), (uint32_t)(b >> 32), false, false);
+  return join64(l32[0], h32[0]) + join64(l32[1], h32[1]);
 }
 
 // sum over the workgroup, the same value in every thread
@@ -113,23 +135,31 @@ __device__ __forceinline__ void note_pick(const double (&r)[4], double run, doub
   if (any && lane == 63 - __clzll((long long)any)) atomicMax(last, end);
 }
 
-// e^x for x <= 0 (NaN: 0); table: 2^(j / 64)
-__device__ __forceinline__ double exp_neg(double x, const double *table) {
-  x = fmax(x, -800.);  // far below the smallest double
-  const double n = rint(x * 92.332482616893656768);  // 64 / ln 2
-  const double r = fma(n, -1.0830424696249145e-02, x);  // ln 2 / 64: n has at most 17 bits, an error of n 2^-60
-  const double q = fma(r, fma(r, fma(r, fma(r, 1. / 120., 1. / 24.), 1. / 6.), 0.5), 1.);
-  const int k = (int)n;
-  const double t = table[k & 63];
-  return ldexp(fma(t * r, q, t), k >> 6);
-}
+// The weights of a row whose largest logit is m (not -inf): e^((l - m) / t).
+// e^x = 2^(k / 64) e^r: k comes from adding 1.5 2^52, which leaves it in the low
+// bits, and its multiple of 64 goes straight into the table entry's exponent.
+// Weights under e^-700 and those of NaN are 0; of an infinite m only its like
+// have weight.
+struct Weights {
+  double m, inv_t, scale;  // scale: 64 / (t ln 2)
+  float top, cut;          // m, and m - 700 t
+  const double *table;     // 2^(j / 64)
+  __device__ __forceinline__ Weights(float m_, float t, const double *tab)
+      : m(m_), inv_t(1. / (double)t), scale(92.332482616893656768 / (double)t), top(m_),
+        cut(m_ == INFINITY ? m_ : fmaxf(m_ - 700.f * t, -FLT_MAX)), table(tab) {}
+  __device__ __forceinline__ double operator()(float l) const {
+    const double d = top == INFINITY ? 0. : (double)l - m;
+    const double y = fma(d, scale, 6755399441055744.);
+    const uint32_t k = (uint32_t)__builtin_bit_cast(uint64_t, y);
+    const double r = fma(y - 6755399441055744., -1.0830424696249145e-02, d * inv_t);  // |r| <= ln 2 / 128
+    const double q = fma(r, fma(r, fma(r, 1. / 24., 1. / 6.), 0.5), 1.);
+    const double t = table[k & 63];
+    const uint64_t w = __builtin_bit_cast(uint64_t, fma(t * r, q, t)) + ((uint64_t)((k & ~63u) << 14) << 32);
+    return l >= cut ? __builtin_bit_cast(double, w) : 0.;
+  }
+};
 __device__ __forceinline__ void fill_table(double *table) {
   if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x * (1. / 64.));
-}
-
-// weight of logit x in a row whose largest is m (m itself infinite: its like)
-__device__ __forceinline__ double weight_of(float x, float m, double inv_t, const double *table) {
-  return x == m ? 1. : x < m ? exp_neg(((double)x - (double)m) * inv_t, table) : 0.;
 }
 
 // ---------------------------------------------------------------------------
@@ -177,10 +207,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_part_kernel(SampleLaunch 
     for (int e = 0; e < E; ++e)
       if (at == tid + kPartThreads * e) x[e] = NAN;  // no weight
   }
-  const double inv_t = 1. / (double)p.temperature;
   double s = 0.;
+  if (m > -INFINITY) {
+    const Weights weight(m, p.temperature, table);
 #pragma unroll
-  for (int e = 0; e < E; ++e) s += m > -INFINITY ? weight_of(x[e], m, inv_t, table) : 0.;
+    for (int e = 0; e < E; ++e) s += weight(x[e]);
+  }
   s = block_sum64<kPartThreads>(s, wave_s);
   if (tid == 0) p.part[(size_t)a * gridDim.x + blockIdx.x] = SamplePart{m, (uint32_t)nan_s, s};
 }
@@ -197,7 +229,6 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
   __shared__ double base_s;
   __shared__ int n_s, pick_s, last_s, first_s, final_s, n_part_s;
   const int tid = threadIdx.x, T = p.T, V = p.vocab;
-  const double inv_t = 1. / (double)p.temperature;
   fill_table(table);
   if (tid < T) {
     const int up = p.parent[tid];
@@ -232,10 +263,11 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
       m = fmaxf(m, __shfl_xor(m, o, 64));
       nan |= __shfl_xor(nan, o, 64);
     }
+    const Weights weight(m, p.temperature, table);
     double rest = 0.;
     for (int s = tid & 7; on && s < parts; s += 8) {
       const double r = part[s].rest;
-      if (r > 0.) rest += r * weight_of(part[s].m, m, inv_t, table);
+      if (r > 0.) rest += r * weight(part[s].m);
     }
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) rest += __shfl_xor(rest, o, 64);
@@ -246,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
     }
   }
   __syncthreads();
-  if (tid < T) w_s[tid] = child && m_s[up_s[tid]] > -INFINITY ? weight_of(lc, m_s[up_s[tid]], inv_t, table) : 0.;
+  if (tid < T) w_s[tid] = child && m_s[up_s[tid]] > -INFINITY ? Weights(m_s[up_s[tid]], p.temperature, table)(lc) : 0.;
   __syncthreads();
   // a child's weight in the residual when its turn comes: 0 where an earlier
   // sibling holds its token (that one was rejected).  Eight threads a child look
@@ -291,11 +323,12 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
     // the part that the draw falls into (a draw of 1 or more: the last that has
     // weight), then the token: a part's tokens in runs of four a thread
     const SamplePart *part = p.part + (size_t)a * parts;
+    const Weights weight(m, p.temperature, table);
     const double goal = (double)u_s[0] * rest;
     const int per = (parts + kThreads - 1) / kThreads;
     auto part_sum = [&](int s) {
       const SamplePart x = part[min(s, parts - 1)];
-      return s < parts && x.rest > 0. ? x.rest * weight_of(x.m, m, inv_t, table) : 0.;
+      return s < parts && x.rest > 0. ? x.rest * weight(x.m) : 0.;
     };
     double sum = 0., all;
     for (int s = 0; s < per; ++s) sum += part_sum(tid * per + s);
@@ -332,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
     const uint32_t out = out_s[tid >> 3] >> (4 * (tid & 7));
     double r[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = i0 + e < V && !(out >> e & 1u) ? weight_of(x[e], m, inv_t, table) : 0.;
+    for (int e = 0; e < 4; ++e) r[e] = i0 + e < V && !(out >> e & 1u) ? weight(x[e]) : 0.;
     sum = (r[0] + r[1]) + (r[2] + r[3]);
     note_pick(r, base + block_before64(sum, wave_s, &all), goal, i0, &pick_s, &last_s);
   } else if (m > -INFINITY) {
@@ -364,6 +397,7 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
 // and whose probabilities in LDS; else a pass over the row forms them again.
 constexpr int kRun = 4, kChunk = kThreads * kRun;
 constexpr int kResChunks = 8;
+constexpr int kChunkSums = 32;
 
 template <bool RES>
 __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
@@ -372,21 +406,31 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
   __shared__ double table[64];
   __shared__ int par_s[PPD_T_MAX], id_s[PPD_T_MAX];
   __shared__ double cw_s[PPD_T_MAX], cq_s[PPD_T_MAX];  // a child's weight and probability in the node's row
-  __shared__ int nan_s, pick_s, last_s;
+  __shared__ double sums_s[kChunkSums][kThreads / 64], before_s[kChunkSums];
+  __shared__ int nan_s, pick_s, last_s, first_s, final_s;
   __shared__ __attribute__((aligned(16))) float4 q_s[RES ? kResChunks : 1][kThreads];
   const int tid = threadIdx.x, a = blockIdx.x, V = p.vocab;
   if (a > 0 && !candidate(p.ids[a], V)) return;  // never reached
   const float *row = p.logits + (size_t)a * V;
   const float *draft = p.draft + (size_t)a * V;
   const int n_chunks = (V + kChunk - 1) / kChunk;
-  // four tokens from i on (past the row: `past`)
-  const bool vec = V % 4 == 0 && ((uintptr_t)p.logits | (uintptr_t)p.draft) % 16 == 0;
-  // (a conditional load would be waited for by itself: indices are clamped)
+  // four tokens from i on (past the row: `past`), one 16-byte load wherever the
+  // row starts (4-byte alignment is enough for it).  The last run is loaded as
+  // the row's last four tokens and moved up; a conditional load would be waited
+  // for by itself.
+  typedef float Run __attribute__((ext_vector_type(4), aligned(4)));
   auto get4 = [&](const float *from, int i) {
-    if (vec) return *(const float4 *)(from + min(i, V - 4));
-    return float4{from[min(i, V - 1)], from[min(i + 1, V - 1)], from[min(i + 2, V - 1)], from[min(i + 3, V - 1)]};
+    if (V < 4) return float4{from[min(i, V - 1)], from[min(i + 1, V - 1)], from[min(i + 2, V - 1)], 0.f};
+    const Run v = *(const Run *)(from + min(i, V - 4));
+    return float4{v[0], v[1], v[2], v[3]};
+  };
+  auto up4 = [&](float4 v, int i) {
+    const int d = V < 4 ? 0 : i - min(i, V - 4);
+    return float4{d == 0 ? v.x : d == 1 ? v.y : d == 2 ? v.z : v.w, d == 0 ? v.y : d == 1 ? v.z : v.w,
+                  d == 0 ? v.z : v.w, v.w};
   };
   auto cut4 = [&](float4 v, int i, float past) {
+    v = up4(v, i);
     return float4{i < V ? v.x : past, i + 1 < V ? v.y : past, i + 2 < V ? v.z : past, i + 3 < V ? v.w : past};
   };
   auto load4 = [&](const float *from, int i, float past) { return cut4(get4(from, i), i, past); };
@@ -407,7 +451,7 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
       q_s[k][tid] = float4{prob(q[k].x), prob(q[k].y), prob(q[k].z), prob(q[k].w)};
     }
   }
-  if (tid == 0) nan_s = 0, pick_s = INT_MAX, last_s = -1;
+  if (tid == 0) nan_s = 0, pick_s = first_s = INT_MAX, last_s = final_s = -1;
   fill_table(table);
   if (tid < p.T) {
     const int up = p.parent[tid];
@@ -431,9 +475,9 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
   }
   if (nan) nan_s = 1;
   m = block_max<kThreads>(m, max_s);
-  const double inv_t = 1. / (double)p.temperature;
+  const Weights weight(m, p.temperature, table);
   if (tid > a && tid < p.T && par_s[tid] == a && candidate(id_s[tid], V)) {
-    cw_s[tid] = weight_of(row[id_s[tid]], m, inv_t, table);
+    cw_s[tid] = weight(row[id_s[tid]]);
     cq_s[tid] = prob(draft[id_s[tid]]);
   }
   double w[RES ? kResChunks : 1][kRun];
@@ -441,8 +485,9 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
 #pragma unroll
     for (int k = 0; k < kResChunks; ++k) {
       const float v[kRun] = {x[k].x, x[k].y, x[k].z, x[k].w};
+      if (k < n_chunks)
 #pragma unroll
-      for (int e = 0; e < kRun; ++e) w[k][e] = weight_of(v[e], m, inv_t, table);
+        for (int e = 0; e < kRun; ++e) w[k][e] = weight(v[e]);
     }
   }
   // the residuals of this thread's run of chunk k
@@ -458,7 +503,7 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
       q = float4{prob(q.x), prob(q.y), prob(q.z), prob(q.w)};
       const float l[kRun] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int e = 0; e < kRun; ++e) r[e] = weight_of(l[e], m, inv_t, table);
+      for (int e = 0; e < kRun; ++e) r[e] = weight(l[e]);
     }
     const float qe[kRun] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -474,7 +519,8 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
     double s = 0.;
     if constexpr (RES) {
 #pragma unroll
-      for (int k = 0; k < kResChunks; ++k) s += chunk_sum(k, C);
+      for (int k = 0; k < kResChunks; ++k)
+        if (k < n_chunks) s += chunk_sum(k, C);
     } else {
 #pragma unroll 2
       for (int k = 0; k < n_chunks; ++k) s += chunk_sum(k, C);
@@ -497,24 +543,55 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
     if (taken < 0) {
       if (!(Z > 0.)) C = 0., Z = total(0.);  // nothing is left: the bonus token is drawn from the weights
       // the chunk that the draw falls into, then the token (a draw of 1 or
-      // more: the last token that has weight)
+      // more: the last token that has weight).  The chunks' sums come from one
+      // pass, kChunkSums of them at a time.
       const double goal = (double)p.u[0] * Z;
+      const int lane = tid & 63, wave = tid >> 6;
       double base = 0.;
-      for (int k = 0; k < n_chunks; ++k) {
-        double r[kRun], all;
+      for (int k0 = 0; k0 < n_chunks; k0 += kChunkSums) {
+        const int nk = min(kChunkSums, n_chunks - k0);
+        auto note_sum = [&](int k, double v) {
+          v = wave_sum64(v);
+          if (lane == 0) sums_s[k][wave] = v;
+        };
         if constexpr (RES) {
 #pragma unroll
-          for (int j = 0; j < kResChunks; ++j)
-            if (j == k) residual4(j, C, r);
+          for (int k = 0; k < kResChunks; ++k)
+            if (k < n_chunks) note_sum(k, chunk_sum(k, C));
         } else {
-          residual4(k, C, r);
+#pragma unroll 2
+          for (int k = 0; k < nk; ++k) note_sum(k, chunk_sum(k0 + k, C));
         }
-        const double before = block_before64((r[0] + r[1]) + (r[2] + r[3]), wave_s, &all);
-        note_pick(r, base + before, goal, k * kChunk + kRun * tid, &pick_s, &last_s);
-        base += all;
         __syncthreads();
-        if (pick_s != INT_MAX) break;
+        double sum = 0., all;
+        if (tid < nk)
+#pragma unroll
+          for (int w = 0; w < kThreads / 64; ++w) sum += sums_s[tid][w];
+        const double before = base + block_before64(sum, wave_s, &all);
+        if (sum > 0.) {  // (one thread a chunk)
+          if (before + sum > goal) atomicMin(&first_s, k0 + tid);
+          atomicMax(&final_s, k0 + tid);
+        }
+        if (tid < nk) before_s[tid] = before;
+        __syncthreads();
+        if (first_s != INT_MAX || k0 + kChunkSums >= n_chunks) {
+          const int k = first_s != INT_MAX ? first_s : max(0, final_s);  // final_s < k0: a row of more chunks
+          double r[kRun];
+          if constexpr (RES) {
+#pragma unroll
+            for (int j = 0; j < kResChunks; ++j)
+              if (j == k) residual4(j, C, r);
+          } else {
+            residual4(k, C, r);
+          }
+          const double at = (k >= k0 ? before_s[k - k0] : base) + block_before64((r[0] + r[1]) + (r[2] + r[3]), wave_s, &all);
+          note_pick(r, at, goal, k * kChunk + kRun * tid, &pick_s, &last_s);
+          break;
+        }
+        base += all;
+        __syncthreads();  // the sums' LDS is written next
       }
+      __syncthreads();
       bonus = pick_s != INT_MAX ? pick_s : max(0, last_s);
     }
   }
