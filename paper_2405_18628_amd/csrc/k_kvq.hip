@@ -12,12 +12,16 @@
 //
 // All of them are bound by memory.  (us; 8 layers of 32 heads, 2048 positions)
 #include <algorithm>
+#include <type_traits>
 
 #include "ppd_kvq.h"
 
 #pragma clang fp contract(off)  // codes are defined by separate float32 operations
 
 namespace {
+
+template <int N>
+using Const = std::integral_constant<int, N>;
 
 constexpr int kWaves = 4;  // blocks a workgroup works on together
 // 16 bytes at any 2-byte border
@@ -29,88 +33,142 @@ __device__ __forceinline__ float piece_elem(u32x4 v, int e) {  // e a constant
 __device__ __forceinline__ float low16(uint32_t sz) { return __uint_as_float(sz << 16); }
 __device__ __forceinline__ float high16(uint32_t sz) { return __uint_as_float(sz & 0xffff0000u); }
 
-// running range of a group
-struct Range {
-  float lo = INFINITY, hi = -INFINITY;
-  uint32_t bad = 0;  // it holds a NaN or an infinity
-  __device__ __forceinline__ void add(float v) {
-    lo = fminf(lo, v);
-    hi = fmaxf(hi, v);
-    bad |= (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
+// ---- ranges, on bfloat16 pairs as they are loaded: the bits of a number with
+// those of a negative one flipped order as 16-bit integers do, infinities and
+// NaN at the ends
+typedef short Pair __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pmin(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(Pair, a), __builtin_bit_cast(Pair, b)));
+}
+__device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(Pair, a), __builtin_bit_cast(Pair, b)));
+}
+// to the order and back
+__device__ __forceinline__ uint32_t ordered(uint32_t x) {
+  const Pair sign = __builtin_bit_cast(Pair, x) >> (Pair){15, 15};
+  return x ^ (__builtin_bit_cast(uint32_t, sign) & 0x7fff7fffu);
+}
+struct Range {  // of the pair's two numbers, in the order
+  uint32_t lo = 0x7fff7fffu, hi = 0x80008000u;
+  __device__ __forceinline__ void add(uint32_t pair) {
+    const uint32_t x = ordered(pair);
+    lo = pmin(lo, x);
+    hi = pmax(hi, x);
   }
-  // (scale, zero) of the group
-  __device__ __forceinline__ uint32_t pair() const {
-    const float r = hi - lo;
-    return bad || !(r < INFINITY) ? 0x7fc0u : f32_to_bf16(r / 15.f) | (__float_as_uint(lo) & 0xffff0000u);
+  __device__ __forceinline__ void join(uint32_t l, uint32_t h) {
+    lo = pmin(lo, l);
+    hi = pmax(hi, h);
   }
 };
-// over the lanes of a position's key: l, l ^ 16, l ^ 32, l ^ 48
+// over both halves and the lanes of a position's key: l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ void join_groups(Range &r) {
-  r.lo = -quad_max(-r.lo);
-  r.hi = quad_max(r.hi);
-  r.bad = quad_max((float)r.bad) > 0.f;
+  r.join(r.lo >> 16 | r.lo << 16, r.hi >> 16 | r.hi << 16);
+  auto l16 = __builtin_amdgcn_permlane16_swap(r.lo, r.lo, false, false);
+  auto h16 = __builtin_amdgcn_permlane16_swap(r.hi, r.hi, false, false);
+  r.lo = pmin(l16[0], l16[1]);
+  r.hi = pmax(h16[0], h16[1]);
+  auto l32 = __builtin_amdgcn_permlane32_swap(r.lo, r.lo, false, false);
+  auto h32 = __builtin_amdgcn_permlane32_swap(r.hi, r.hi, false, false);
+  r.lo = pmin(l32[0], l32[1]);
+  r.hi = pmax(h32[0], h32[1]);
 }
 // over the 16 lanes of a row
 template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, false));
-}
-template <int CTRL>
-__device__ __forceinline__ void join_step(Range &r) {
-  r.lo = fminf(r.lo, dpp<CTRL>(r.lo));
-  r.hi = fmaxf(r.hi, dpp<CTRL>(r.hi));
-  r.bad |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)r.bad, CTRL, 0xf, 0xf, false);
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
 __device__ __forceinline__ void join_row(Range &r) {
-  join_step<0xb1>(r);   // quad_perm [1,0,3,2]
-  join_step<0x4e>(r);   // quad_perm [2,3,0,1]
-  join_step<0x141>(r);  // row_half_mirror
-  join_step<0x140>(r);  // row_mirror
+  r.join(dpp<0xb1>(r.lo), dpp<0xb1>(r.hi));    // quad_perm [1,0,3,2]
+  r.join(dpp<0x4e>(r.lo), dpp<0x4e>(r.hi));    // quad_perm [2,3,0,1]
+  r.join(dpp<0x141>(r.lo), dpp<0x141>(r.hi));  // row_half_mirror
+  r.join(dpp<0x140>(r.lo), dpp<0x140>(r.hi));  // row_mirror
 }
 
-// Codes of eight elements (element e with its group's s[e], z[e] and inv[e], about
-// 1 / s[e]) as a word.  rint((x - z) / s) is that of the product with inv unless
-// that lies within 2^-10 of a half (both quotients are within 2^-16 of each
-// other) or is no number; then the division itself decides.
-template <typename F>
-__device__ __forceinline__ uint32_t code_word(F elem, const float (&s)[8], const float (&z)[8], const float (&inv)[8]) {
-  float c[8];
-  bool close = false;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float q = (elem(e) - z[e]) * inv[e];
-    c[e] = rintf(q);
-    close |= !(fabsf(fabsf(q - c[e]) - 0.5f) > 0x1p-10f);
+// A group's (scale, zero) pair and the reciprocal that its codes are taken with
+// (0 for an even group); `odd`: a group without a value, or a scale so small
+// that remainders underflow.
+struct Affine {
+  uint32_t pair;
+  float inv;
+  bool odd;
+  // lo, hi: the range in the order, in the low halves
+  __device__ __forceinline__ Affine(uint32_t lo, uint32_t hi) {
+    const float l = __uint_as_float(ordered(lo) << 16), h = __uint_as_float(ordered(hi) << 16);
+    const bool end = (int16_t)hi >= 0x7f80 || (int16_t)lo <= (int16_t)0x807f;
+    const float r = h - l;
+    // r / 15, correctly rounded: the remainder of the product with RN(1 / 15)
+    // corrects it (checked for every mantissa; subnormal quotients are divided)
+    const float q0 = r * (1.f / 15.f);
+    float q = fmaf(fmaf(-15.f, q0, r), 1.f / 15.f, q0);
+    const bool tiny = r < 0x1p-90f;
+    if (__ballot(tiny)) q = tiny ? r / 15.f : q;
+    const bool none = end || !(r < INFINITY);
+    pair = none ? 0x7fc0u : f32_to_bf16(q) | (__float_as_uint(l) & 0xffff0000u);
+    const float s = low16(pair), y = __builtin_amdgcn_rcpf(s);
+    inv = s > 0.f ? fmaf(fmaf(-s, y, 1.f), y, y) : 0.f;
+    odd = none || tiny;
   }
-  if (close)
+  __device__ __forceinline__ Affine(uint32_t pair_, float inv_) : pair(pair_), inv(inv_), odd(false) {}
+  // rint of the float32 quotient (x - z) / s: a product with the reciprocal and
+  // one correction by its remainder give it to the last bit, so that a quotient
+  // that is exactly a half is one here (with bfloat16 rows these are common)
+  __device__ __forceinline__ float code(float x) const {
+    const float s = low16(pair), d = x - high16(pair), q0 = d * inv;
+    return rintf(fmaf(fmaf(-q0, s, d), inv, q0));
+  }
+  __device__ __forceinline__ float divide(float x) const {
+    const float s = low16(pair), z = high16(pair);
+    return s > 0.f ? fminf(rintf((x - z) / s), 15.f) : 0.f;
+  }
+};
+
+// Codes of eight elements as a word, its two halves put together in float32
+// (16 bits, exact).
+template <typename X, typename A>
+__device__ __forceinline__ uint32_t code_word(X x, A affine, bool odd) {
+  float lo = 0.f, hi = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = s[e] > 0.f ? rintf((elem(e) - z[e]) / s[e]) : 0.f;  // 0: an even group, or one without a value
-  uint32_t w = 0;
+  for (int e = 7; e >= 0; --e) {
+    const float c = affine(e).code(x(e));
+    if (e & 1)
+      hi = fmaf(hi, 16.f, c);
+    else
+      lo = fmaf(lo, 16.f, c);
+  }
+  uint32_t w = (uint32_t)lo | (uint32_t)hi << 16;
+  if (odd) {
+    w = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w |= (uint32_t)fminf(c[e], 15.f) << kvq_shift(e);
+    for (int e = 0; e < 8; ++e) w |= (uint32_t)affine(e).divide(x(e)) << kvq_shift(e);
+  }
   return w;
 }
 
-// ---- bf16 rows -> blocks.  Workgroup (head, run of blocks), a block a wave.
-template <bool PATH>
-__global__ __launch_bounds__(64 * kWaves) void kvq_store_kernel(KvqStore p) {
+// ---- bf16 rows -> blocks.  Workgroup (head, run of W blocks), a block a wave.
+template <int W, bool PATH>
+__global__ __launch_bounds__(64 * W, 2) void kvq_store_kernel(KvqStore p) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, g = lane >> 4;
-  int n = p.n;
-  if constexpr (PATH) {
-    n = max(0, min(*p.n_path, min(p.n, p.room)));
-    if (p.len_dev && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.len_dev = p.pos0 + n;
-  }
-  const size_t head = blockIdx.x;
+  // (most runs behind a path's first are empty: the heads' first ones come first)
+  const size_t head = PATH ? blockIdx.x % p.heads : blockIdx.x / p.runs;
+  const int run0 = PATH ? blockIdx.x / p.heads : blockIdx.x % p.runs;
   const bf16_t *ks = p.k + head * p.scap * 128, *vs = p.v + head * 128 * (size_t)p.scap;
-  for (int blk = p.pos0 / kQB + blockIdx.y * kWaves + wave; blk * kQB < p.pos0 + n; blk += gridDim.y * kWaves) {
-    const int i0 = blk * kQB - p.pos0;                // index of the block's first position in the run
+  for (int blk = p.pos0 / kQB + run0 * W + wave; blk * kQB < p.pos0 + p.n; blk += p.runs * W) {
+    const int i0 = blk * kQB - p.pos0;  // index of the block's first position in the run
+    int n = p.n, own = 0;
+    if constexpr (PATH) {
+      // the path is read beside its length
+      own = max(0, min(p.path[max(0, min(i0 + (lane & 31), p.n - 1))], p.scap - 1));
+      n = max(0, min(*p.n_path, min(p.n, p.room)));
+      if (p.len_dev && blockIdx.x == 0 && threadIdx.x == 0) *p.len_dev = p.pos0 + n;
+    }
     const int a = max(0, -i0), b = min(kQB, n - i0);  // the block's positions [a, b) are written
-    if (a >= b) break;  // an empty path
+    if (a >= b) return;                               // a shorter path: no later block either
     auto source = [&](int j) {                        // source row of the block's position j, kept in [a, b)
-      const int i = i0 + max(a, min(j, b - 1));
-      return PATH ? max(0, min(p.path[i], p.scap - 1)) : p.src0 + i;
+      j = max(a, min(j, b - 1));
+      return PATH ? __shfl(own, j, 64) : p.src0 + i0 + j;
     };
+    const bool all = !PATH && a == 0 && b == kQB;
     unsigned char *out = p.blocks + (head * p.nb + blk) * (size_t)kQBytes;
     u32x4 kx[2][4], vx[2][4];
 #pragma unroll
@@ -120,7 +178,8 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_store_kernel(KvqStore p) {
       for (int w = 0; w < 4; ++w) kx[t][w] = *(const u32x4 *)(row + 32 * w);
     }
     const bf16_t *col = vs + (size_t)r * p.scap;
-    if (!PATH && a == 0 && b == kQB) {
+    const bool some = 8 * g < b && 8 * g + 8 > a;  // the lane has a value to write
+    if (all) {
       const bf16_t *at = col + p.src0 + i0 + 8 * g;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -133,13 +192,20 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_store_kernel(KvqStore p) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
+        for (int w = 0; w < 4; ++w) vx[h][w] = u32x4{0u, 0u, 0u, 0u};
+      if (some) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bf16_t *at = col + (size_t)(64 * h + 16 * w) * p.scap;
-            vx[h][w][e] = at[from[2 * e]] | (uint32_t)at[from[2 * e + 1]] << 16;
-          }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bf16_t *at = col + (size_t)(64 * h + 16 * w) * p.scap;
+              vx[h][w][e] = at[from[2 * e]] | (uint32_t)at[from[2 * e + 1]] << 16;
+            }
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);  // every load in flight
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int j = kvq_key_of(t, r);
@@ -151,51 +217,71 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_store_kernel(KvqStore p) {
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) range.add(piece_elem(kx[t][2 * q + w], e));
+          for (int e = 0; e < 4; ++e) range.add(kx[t][2 * q + w][e]);
         join_groups(range);
-        sz[q] = range.pair();
-        float s[8], z[8], inv[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = low16(sz[q]), z[e] = high16(sz[q]), inv[e] = __builtin_amdgcn_rcpf(s[e]);
+        const Affine f(range.lo, range.hi);
+        sz[q] = f.pair;
 #pragma unroll
         for (int w = 0; w < 2; ++w)
-          words[2 * q + w] = code_word([&](int e) { return piece_elem(kx[t][2 * q + w], e); }, s, z, inv);
+          words[2 * q + w] = code_word([&](int e) { return piece_elem(kx[t][2 * q + w], e); }, [&](int) { return f; }, f.odd);
       }
       if (j >= a && j < b) {
         *(u32x4 *)(out + (t * 64 + lane) * 16) = words;
         if (g == 0) *(u32x2 *)(out + kQP + j * 8) = u32x2{sz[0], sz[1]};
       }
     }
+    // the values' 16 groups of eight positions: all lanes of a row take part in
+    // each range, lane r then settles group r / 8 of position 8 g + r % 8
+    Range range[2][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float s[8], z[8], inv[8];
-      uint32_t mine = 0;  // position 8 g + r % 8's pair
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        Range range;
+      for (int e = 0; e < 4; ++e) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) range.add(piece_elem(vx[h][w], e));
-        join_row(range);
-        const uint32_t sz = range.pair();
-        s[e] = low16(sz), z[e] = high16(sz), inv[e] = __builtin_amdgcn_rcpf(s[e]);
-        if ((r & 7) == e) mine = sz;
+        for (int w = 0; w < 4; ++w) range[h][e].add(vx[h][w][e]);
+        join_row(range[h][e]);
       }
+    // (bits, not selections: those of array elements become memory accesses)
+    const uint32_t m8 = 0u - (r >> 3), m4 = 0u - (r >> 2 & 1), m2 = 0u - (r >> 1 & 1);
+    auto either = [](uint32_t m, uint32_t one, uint32_t zero) { return (one & m) | (zero & ~m); };
+    auto own_group = [&](auto part) {  // of the 8 pairs of groups, the lane's
+      const uint32_t p0 = either(m8, part(1, 0), part(0, 0)), p1 = either(m8, part(1, 1), part(0, 1));
+      const uint32_t p2 = either(m8, part(1, 2), part(0, 2)), p3 = either(m8, part(1, 3), part(0, 3));
+      return either(m2, either(m4, p3, p1), either(m4, p2, p0)) >> (16 * (r & 1));
+    };
+    const Affine mine(own_group([&](int h, int e) { return range[h][e].lo; }),
+                      own_group([&](int h, int e) { return range[h][e].hi; }));
+    const bool odd = __ballot(mine.odd) != 0;
+    {
+      const int j = 8 * g + (r & 7);
+      if (j >= a && j < b) *(uint32_t *)(out + kQP + (kQB + j) * 8 + 4 * (r >> 3)) = mine.pair;
+    }
+    auto share = [&](auto tag) {  // lane k's
+      constexpr int CTRL = 0x150 + decltype(tag)::value;  // row_newbcast:k
+      return Affine(dpp<CTRL>(mine.pair), __uint_as_float(dpp<CTRL>(__float_as_uint(mine.inv))));
+    };
+    auto store_half = [&](auto tag) {
+      constexpr int h = decltype(tag)::value;
+      const Affine f[8] = {share(Const<8 * h>()),     share(Const<8 * h + 1>()), share(Const<8 * h + 2>()),
+                           share(Const<8 * h + 3>()), share(Const<8 * h + 4>()), share(Const<8 * h + 5>()),
+                           share(Const<8 * h + 6>()), share(Const<8 * h + 7>())};
       u32x4 words;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) words[w] = code_word([&](int e) { return piece_elem(vx[h][w], e); }, s, z, inv);
+      for (int w = 0; w < 4; ++w)
+        words[w] = code_word([&](int e) { return piece_elem(vx[h][w], e); }, [&](int e) -> const Affine & { return f[e]; }, odd);
       u32x4 *o = (u32x4 *)(out + kQV + (h * 64 + lane) * 16);
       if (8 * g >= a && 8 * g + 8 <= b) {
         *o = words;
-      } else if (8 * g < b && 8 * g + 8 > a) {
+      } else if (some) {
         uint32_t put = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) put |= 8 * g + e >= a && 8 * g + e < b ? 15u << kvq_shift(e) : 0u;
         const u32x4 old = *o;
         *o = (words & put) | (old & ~put);
       }
-      const int j = 8 * g + (r & 7);
-      if (r < 8 && j >= a && j < b) *(uint32_t *)(out + kQP + (kQB + j) * 8 + 4 * h) = mine;
-    }
+    };
+    store_half(Const<0>());
+    store_half(Const<1>());
   }
 }
 
@@ -207,9 +293,10 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_load_kernel(KvqLoad p) {
   __shared__ u32x2 par_s[kWaves][2 * kQB];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, g = lane >> 4;
-  const size_t head = blockIdx.x;
+  const size_t head = blockIdx.x / p.runs;
+  const int run0 = blockIdx.x % p.runs;
   bf16_t *ks = p.k + head * p.dcap * 128, *vs = p.v + head * 128 * (size_t)p.dcap;
-  for (int blk = p.pos0 / kQB + blockIdx.y * kWaves + wave; blk * kQB < p.pos0 + p.n; blk += gridDim.y * kWaves) {
+  for (int blk = p.pos0 / kQB + run0 * kWaves + wave; blk * kQB < p.pos0 + p.n; blk += p.runs * kWaves) {
     const int i0 = blk * kQB - p.pos0;
     const int a = max(0, -i0), b = min(kQB, p.n - i0);
     const unsigned char *in = p.blocks + (head * p.nb + blk) * (size_t)kQBytes;
@@ -388,11 +475,11 @@ template <int W, bool WAIT>
 __global__ __launch_bounds__(64 * W) void kvq_gather_kernel(KvqEvict p) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, g = lane >> 4;
-  const size_t head = blockIdx.x;
+  const size_t head = blockIdx.x / p.runs;
   const unsigned char *src = p.src + head * (size_t)p.src_nb * kQBytes;
   const int32_t *kept = p.kept + head * (size_t)p.budget;
   const int nblk = (p.n + kQB - 1) / kQB;
-  for (int run = blockIdx.y * W; run < nblk; run += gridDim.y * W) {
+  for (int run = blockIdx.x % p.runs * W; run < nblk; run += p.runs * W) {
     const int blk = run + wave, b = min(kQB, p.n - blk * kQB);  // b <= 0: no block
     unsigned char *out = p.dst + (head * p.dst_nb + blk) * (size_t)kQBytes;
     u32x4 kw[2], vw[2];
@@ -451,33 +538,42 @@ __global__ __launch_bounds__(64 * W) void kvq_gather_kernel(KvqEvict p) {
   }
 }
 
-int runs_of(int pos0, int n, int waves) {
-  return std::min(65535, ((pos0 % kQB + n + kQB - 1) / kQB + waves - 1) / waves);
+// Workgroups of a head, which follow one another in the grid: neighbours then
+// work on neighbouring positions.  (With the heads first, all workgroups under
+// way touch the same positions of their heads; where a dim's row of positions is
+// a multiple of 4 KB they meet in the same memory channels.)
+int runs_of(int heads, int pos0, int n, int waves) {
+  return std::min(INT32_MAX / heads, ((pos0 % kQB + n + kQB - 1) / kQB + waves - 1) / waves);
 }
 
 }  // namespace
 
-hipError_t launch_kvq_store(const KvqStore &p, hipStream_t s) {
-  const dim3 grid(p.heads, runs_of(p.pos0, p.n, kWaves)), block(64 * kWaves);
+hipError_t launch_kvq_store(KvqStore p, hipStream_t s) {
+  // a path is short: a wave a workgroup, so that a head's blocks spread
+  p.runs = runs_of(p.heads, p.pos0, p.n, p.path ? 1 : kWaves);
   if (p.path)
-    hipLaunchKernelGGL(kvq_store_kernel<true>, grid, block, 0, s, p);
+    hipLaunchKernelGGL((kvq_store_kernel<1, true>), dim3(p.heads * p.runs), dim3(64), 0, s, p);
   else
-    hipLaunchKernelGGL(kvq_store_kernel<false>, grid, block, 0, s, p);
+    hipLaunchKernelGGL((kvq_store_kernel<kWaves, false>), dim3(p.heads * p.runs), dim3(64 * kWaves), 0, s, p);
   return hipGetLastError();
 }
 
-hipError_t launch_kvq_load(const KvqLoad &p, hipStream_t s) {
-  hipLaunchKernelGGL(kvq_load_kernel, dim3(p.heads, runs_of(p.pos0, p.n, kWaves)), dim3(64 * kWaves), 0, s, p);
+hipError_t launch_kvq_load(KvqLoad p, hipStream_t s) {
+  p.runs = runs_of(p.heads, p.pos0, p.n, kWaves);
+  hipLaunchKernelGGL(kvq_load_kernel, dim3(p.heads * p.runs), dim3(64 * kWaves), 0, s, p);
   return hipGetLastError();
 }
 
-hipError_t launch_kvq_evict(const KvqEvict &p, hipStream_t s) {
+hipError_t launch_kvq_evict(KvqEvict p, hipStream_t s) {
   hipLaunchKernelGGL(kvq_select_kernel, dim3(p.heads), dim3(kSel), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.src == p.dst)
-    hipLaunchKernelGGL((kvq_gather_kernel<16, true>), dim3(p.heads, 1), dim3(64 * 16), 0, s, p);
-  else
-    hipLaunchKernelGGL((kvq_gather_kernel<kWaves, false>), dim3(p.heads, runs_of(0, p.n, kWaves)), dim3(64 * kWaves), 0, s, p);
+  if (p.src == p.dst) {
+    p.runs = 1;
+    hipLaunchKernelGGL((kvq_gather_kernel<16, true>), dim3(p.heads), dim3(64 * 16), 0, s, p);
+  } else {
+    p.runs = runs_of(p.heads, 0, p.n, kWaves);
+    hipLaunchKernelGGL((kvq_gather_kernel<kWaves, false>), dim3(p.heads * p.runs), dim3(64 * kWaves), 0, s, p);
+  }
   return hipGetLastError();
 }

@@ -39,16 +39,18 @@ struct KvqStore {
   const int32_t *path, *n_path;
   int room;             // path: positions of the cache from pos0 on
   int32_t *len_dev;
+  int runs;             // workgroups a head (the launcher's)
 };
-hipError_t launch_kvq_store(const KvqStore &p, hipStream_t s);
+hipError_t launch_kvq_store(KvqStore p, hipStream_t s);
 
 struct KvqLoad {
   const unsigned char *blocks;
   bf16_t *k, *v;
   int heads, nb, dcap;
   int pos0, n, dst0;
+  int runs;
 };
-hipError_t launch_kvq_load(const KvqLoad &p, hipStream_t s);
+hipError_t launch_kvq_load(KvqLoad p, hipStream_t s);
 
 struct KvqEvict {
   const unsigned char *src;
@@ -58,8 +60,9 @@ struct KvqEvict {
   const float *score;
   float *score_out;
   int32_t *kept;
+  int runs;
 };
-hipError_t launch_kvq_evict(const KvqEvict &p, hipStream_t s);
+hipError_t launch_kvq_evict(KvqEvict p, hipStream_t s);
 
 // ---- attention over 4-bit prefixes and bf16 tree rows
 struct KvqSeqs {
