@@ -149,23 +149,32 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
     rt[i].l_run = 0.f;
   }
   const float c = p.scale_log2;
+  const KvqBits bits;
 
-  if (n_live > 0)
-    for (int blk = b0 + par; blk < b1; blk += PARS) {
-      if (blk < n4) {
-        const unsigned char *src = blocks + (size_t)blk * kQBytes;
-        u32x4 kw[2], vw[2];
+  // a block's codes and parameters; past the wave's blocks the first one again
+  // (the same loads on every path, so that the wait for them is a counted one)
+  u32x4 kw[2], vw[2];
+  u32x2 pr;
+  auto request = [&](int blk) {
+    const unsigned char *src = blocks + (size_t)(blk < b1 && blk < n4 ? blk : 0) * kQBytes;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          kw[t] = *(const u32x4 *)(src + (t * 64 + lane) * 16);
-          vw[t] = *(const u32x4 *)(src + kQV + (t * 64 + lane) * 16);
-        }
-        const u32x2 pr = *(const u32x2 *)(src + kQP + lane * 8);
+    for (int t = 0; t < 2; ++t) {
+      kw[t] = __builtin_nontemporal_load((const u32x4 *)(src + (t * 64 + lane) * 16));
+      vw[t] = __builtin_nontemporal_load((const u32x4 *)(src + kQV + (t * 64 + lane) * 16));
+    }
+    pr = __builtin_nontemporal_load((const u32x2 *)(src + kQP + lane * 8));
+  };
+  int blk = b0 + par;
+  if (n_live > 0) {
+    if (n4 > 0) request(blk);
+    for (; blk < min(b1, n4); blk += PARS) {
+        const u32x4 kc[2] = {kw[0], kw[1]}, vc[2] = {vw[0], vw[1]};
+        const u32x2 pc = pr;
+        request(blk + PARS);
         const bool valid = blk * kQB + (lane & 31) < L;
-        const float2 a0 = kvq_affine(pr[0]), a1 = kvq_affine(pr[1]);
+        const float2 a0 = kvq_affine(pc[0]), a1 = kvq_affine(pc[1]);
         par_s[wave][lane] = valid ? floatx4{a0.x, a0.y, a1.x, a1.y} : floatx4{0.f, 0.f, 0.f, 0.f};
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const int vis = L - blk * kQB - 8 * lg;  // keys of the lane below it are in the prefix
         float sv[NQ][8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -176,7 +185,7 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
             for (int i = 0; i < NQ; ++i) acc[i][g] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
-              const bf16x8 x = as_bf16x8(kvq_expand(kw[t][2 * g + d]));
+              const bf16x8 x = as_bf16x8(kvq_expand(kc[t][2 * g + d], bits));
 #pragma unroll
               for (int part = PLANES ? 1 : 0; part >= 0; --part)
 #pragma unroll
@@ -191,9 +200,16 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
             for (int i = 0; i < NQ; ++i) {
               float x = fmaf(a[0], acc[i][0][e], a[1] * rt[i].qs[0]);
               x = fmaf(a[2], acc[i][1][e], fmaf(a[3], rt[i].qs[1], x));
-              sv[i][4 * t + e] = 4 * t + e < vis ? x : -INFINITY;
+              sv[i][4 * t + e] = x;
             }
           }
+        }
+        if (blk * kQB + kQB > L) {  // the prefix ends in this block
+          const int vis = L - blk * kQB - 8 * lg;
+#pragma unroll
+          for (int i = 0; i < NQ; ++i)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sv[i][u] = u < vis ? sv[i][u] : -INFINITY;
         }
         float pv[NQ][8];
         __builtin_amdgcn_sched_barrier(0);
@@ -217,7 +233,7 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
           for (int i = 0; i < NQ; ++i) split8(ps[i], ph[i], pl[i]);
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            const bf16x8 x = as_bf16x8(kvq_expand(vw[g][w]));
+            const bf16x8 x = as_bf16x8(kvq_expand(vc[g][w], bits));
 #pragma unroll
             for (int i = 0; i < NQ; ++i) rt[i].o[4 * g + w] = mfma16x16x32(x, as_bf16x8(pl[i]), rt[i].o[4 * g + w]);
 #pragma unroll
@@ -225,7 +241,8 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
           }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the parameters' LDS is written next
-      } else {
+    }
+    for (; blk < b1; blk += PARS) {
         // tree rows: keys and values straight from the tail
         const int k0 = (blk - n4) * kQB;
         const int j0 = k0 + 8 * lg, keep_n = max(0, min(8, T - j0));  // keys of the lane that exist
@@ -295,8 +312,8 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
           }
           if (dt & 1) __builtin_amdgcn_sched_barrier(0);
         }
-      }
     }
+  }
 
   // ---- the waves meet in LDS: thread -> row tid / 32 + 16 n, dims 4 (tid % 32) .. + 3
 #pragma unroll
@@ -408,6 +425,7 @@ __global__ __launch_bounds__(256) void kvq_score_kernel(KvqScoreLaunch p) {
   const float *in = p.in ? p.in + (size_t)lh * p.cap : nullptr;
   float *out = p.out + (size_t)lh * p.cap;
   const float c = p.scale_log2;
+  const KvqBits bits;
   for (int r0 = 0; r0 == 0 || r0 < R; r0 += kPassTiles * 16) {
     __syncthreads();
     const int tiles = min(kPassTiles, (R - r0 + 15) / 16);
@@ -471,7 +489,7 @@ __global__ __launch_bounds__(256) void kvq_score_kernel(KvqScoreLaunch p) {
           const u32x4 w = *(const u32x4 *)(src + (t * 64 + lane) * 16);
           const u32x2 pr = *(const u32x2 *)(src + kQP + j * 8);
 #pragma unroll
-          for (int ds = 0; ds < 4; ++ds) b[ds] = kvq_expand(w[ds]);
+          for (int ds = 0; ds < 4; ++ds) b[ds] = kvq_expand(w[ds], bits);
           const float2 a0 = kvq_affine(pr[0]), a1 = kvq_affine(pr[1]);
           a = float4{a0.x, a0.y, a1.x, a1.y};
         } else {
@@ -524,6 +542,7 @@ size_t kvq_attn_part_bytes(int nh, int nkv, int T) {
   return (size_t)kvq_attn_max_splits(nkv) * T * nh * OROW * sizeof(float);
 }
 
+constexpr long kSlots = 256;
 void kvq_attn_plan(KvqAttnLaunch &a) {
   const int B = a.sb.B, G = a.nh / a.nkv, cap = kvq_attn_max_splits(a.nkv);
   a.max_splits = cap;
@@ -540,12 +559,12 @@ void kvq_attn_plan(KvqAttnLaunch &a) {
     units[j] = a.nkv * ((T * G + rw - 1) / rw);
     total += (long)units[j] * nblk[j];
   }
-  const long share = std::max<long>(pars, (total + 255) / 256);
   a.n_slots = 0;
   for (int j = 0; j < B; ++j) {
-    a.splits[j] = (int)std::max<long>(1, std::min<long>(cap, nblk[j] / share));
-    const int per = (nblk[j] + a.splits[j] - 1) / a.splits[j];
-    a.chunk[j] = (per + pars - 1) / pars * pars;
+    // the sequence's share of kSlots workgroups, a block a wave at least
+    const long want = std::max<long>(1, kSlots * (long)nblk[j] / std::max<long>(1, total));
+    a.splits[j] = (int)std::max<long>(1, std::min<long>(std::min<long>(cap, want), nblk[j] / pars));
+    a.chunk[j] = (nblk[j] + a.splits[j] - 1) / a.splits[j];
     a.splits[j] = (nblk[j] + a.chunk[j] - 1) / a.chunk[j];
     a.slot0[j] = a.n_slots;
     a.n_slots += units[j] * a.splits[j];

@@ -16,9 +16,15 @@ __host__ __device__ __forceinline__ int kvq_key_of(int t, int m) { return 8 * (m
 // 8.0, so a pair costs a shift and an and-or.  With it a row's value s c + z is
 // (2 s) x + (z - 16 s) of the operand element x: exact products on the matrix
 // cores, the scale and the zero applied to their float32 sums.
-__device__ __forceinline__ u32x4 kvq_expand(uint32_t w) {
-  return u32x4{((w << 3) & 0x00780078u) | 0x41004100u, ((w >> 1) & 0x00780078u) | 0x41004100u,
-               ((w >> 5) & 0x00780078u) | 0x41004100u, ((w >> 9) & 0x00780078u) | 0x41004100u};
+// (The mask and the magic bits are kept in registers: as literals they take an
+// instruction each.)
+struct KvqBits {
+  uint32_t mask = 0x00780078u, magic = 0x41004100u;
+  __device__ __forceinline__ KvqBits() { asm("" : "+v"(mask), "+v"(magic)); }
+};
+__device__ __forceinline__ u32x4 kvq_expand(uint32_t w, const KvqBits &k) {
+  return u32x4{((w << 3) & k.mask) | k.magic, ((w >> 1) & k.mask) | k.magic, ((w >> 5) & k.mask) | k.magic,
+               ((w >> 9) & k.mask) | k.magic};
 }
 // a (scale, zero) pair as (2 s, z - 16 s)
 __device__ __forceinline__ float2 kvq_affine(uint32_t sz) {
