@@ -25,9 +25,8 @@ constexpr int OROW = PPD_ATTN_OROW;  // partial row: 128 dims, m, l, padding (fl
 constexpr int kGroupRows = 128;      // rows of a workgroup at most
 constexpr float kLn2 = 0.69314718055994531f;
 
-// what a wave keeps of one 16-row tile
+// what a wave keeps of one 16-row tile (its queries apart)
 struct RTile {
-  u32x4 q[4][2];  // B operand, dims 32 ds + 8 (lane / 16) .. + 7, parts hi, lo
   float qs[2];    // sums of q over the two groups' dims
   uint64_t mk0, mk1;
   floatx4 o[8];   // O^T: dims 16 dt + 4 (lane / 16) + e, row lane % 16
@@ -80,7 +79,12 @@ template <int NQ, int QW, int PARS, bool PLANES>
 __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
   static_assert(QW * PARS * 64 == NT && QW * NQ * 16 <= kGroupRows, "eight waves");
   constexpr int RW = QW * NQ * 16;  // rows of the workgroup
+  constexpr int PARTS = PLANES ? 2 : 1;
+  // the waves' rows, after the main loop; before, with several tiles a wave,
+  // their queries (64 registers would not be left for them)
   __shared__ __attribute__((aligned(16))) float rows_s[PARS][RW][OROW];
+  u32x4 *q_s = (u32x4 *)rows_s;  // [tile][ds][part][lane]
+  static_assert((size_t)QW * NQ * 4 * PARTS * 1024 <= sizeof(rows_s), "queries fit");
   __shared__ __attribute__((aligned(16))) floatx4 par_s[8][2 * kQB];  // per wave: affine pairs of 32 keys, 32 values
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -105,52 +109,6 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
   const int row0 = grp * RW;
   const int MT = p.T_pad >> 4;
 
-  RTile rt[NQ];
-  const int n_live = min(NQ, ((min(R - row0, RW) + 15) / 16 - qw + QW - 1) / QW);
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int r = row0 + (qw + QW * i) * 16 + lr;
-    const bool live = r < R;
-    const int rc = min(r, R - 1);
-    const int tok = t0 + rc / G, head = kvh * G + rc % G;
-#pragma unroll
-    for (int ds = 0; ds < 4; ++ds) {
-      if constexpr (PLANES) {
-        const unsigned char *src = (const unsigned char *)p.q + plane_off(MT, tok, head * 128 + ds * 32 + lg * 8);
-        rt[i].q[ds][0] = *(const u32x4 *)src;
-        rt[i].q[ds][1] = *(const u32x4 *)(src + kPlaneLo);
-      } else {
-        rt[i].q[ds][0] = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + ds * 32 + lg * 8);
-        rt[i].q[ds][1] = u32x4{0u, 0u, 0u, 0u};
-      }
-    }
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-      rt[i].qs[g] = quad_sum((sum8(rt[i].q[2 * g][0]) + sum8(rt[i].q[2 * g + 1][0])) +
-                             (PLANES ? sum8(rt[i].q[2 * g][1]) + sum8(rt[i].q[2 * g + 1][1]) : 0.f));
-    if (PLANES && p.q_out && ks == 0 && par == 0 && live) {
-      float *dst = p.q_out + ((size_t)tok * p.nh + head) * 128 + lg * 8;
-#pragma unroll
-      for (int ds = 0; ds < 4; ++ds)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t a = rt[i].q[ds][0][w], b = rt[i].q[ds][1][w];
-          *(float2 *)(dst + ds * 32 + 2 * w) =
-              float2{__uint_as_float(a << 16) + __uint_as_float(b << 16),
-                     __uint_as_float(a & 0xffff0000u) + __uint_as_float(b & 0xffff0000u)};
-        }
-    }
-    rt[i].mk0 = live ? p.mask[2 * (size_t)tok] : 0ull;
-    rt[i].mk1 = live ? p.mask[2 * (size_t)tok + 1] : 0ull;
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) rt[i].o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-    rt[i].pz[0] = rt[i].pz[1] = 0.f;
-    rt[i].m_run = -INFINITY;
-    rt[i].l_run = 0.f;
-  }
-  const float c = p.scale_log2;
-  const KvqBits bits;
-
   // a block's codes and parameters; past the wave's blocks the first one again
   // (the same loads on every path, so that the wait for them is a counted one)
   u32x4 kw[2], vw[2];
@@ -164,9 +122,79 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
     }
     pr = __builtin_nontemporal_load((const u32x2 *)(src + kQP + lane * 8));
   };
+  if (n4 > 0) request(b0 + par);
+  __builtin_amdgcn_sched_barrier(0);
+
+  RTile rt[NQ];
+  u32x4 qr[4][PARTS];  // the queries, with one tile a wave
+  const int n_live = min(NQ, ((min(R - row0, RW) + 15) / 16 - qw + QW - 1) / QW);
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int r = row0 + (qw + QW * i) * 16 + lr;
+    const bool live = r < R;
+    const int rc = min(r, R - 1);
+    const int tok = t0 + rc / G, head = kvh * G + rc % G;
+    u32x4 q[4][PARTS];  // B operand, dims 32 ds + 8 (lane / 16) .. + 7, parts hi, lo
+#pragma unroll
+    for (int ds = 0; ds < 4; ++ds) {
+      if constexpr (PLANES) {
+        const unsigned char *src = (const unsigned char *)p.q + plane_off(MT, tok, head * 128 + ds * 32 + lg * 8);
+        q[ds][0] = *(const u32x4 *)src;
+        q[ds][1] = *(const u32x4 *)(src + kPlaneLo);
+      } else {
+        q[ds][0] = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + ds * 32 + lg * 8);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float sum = 0.f;
+#pragma unroll
+      for (int part = PARTS - 1; part >= 0; --part) sum += sum8(q[2 * g][part]) + sum8(q[2 * g + 1][part]);
+      rt[i].qs[g] = quad_sum(sum);
+    }
+    if constexpr (PLANES) {
+      if (p.q_out && ks == 0 && par == 0 && live) {
+        float *dst = p.q_out + ((size_t)tok * p.nh + head) * 128 + lg * 8;
+#pragma unroll
+        for (int ds = 0; ds < 4; ++ds)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t a = q[ds][0][w], b = q[ds][1][w];
+            *(float2 *)(dst + ds * 32 + 2 * w) =
+                float2{__uint_as_float(a << 16) + __uint_as_float(b << 16),
+                       __uint_as_float(a & 0xffff0000u) + __uint_as_float(b & 0xffff0000u)};
+          }
+      }
+    }
+#pragma unroll
+    for (int ds = 0; ds < 4; ++ds)
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) {
+        if constexpr (NQ == 1)
+          qr[ds][part] = q[ds][part];
+        else if (par == 0)
+          q_s[(((qw + QW * i) * 4 + ds) * PARTS + part) * 64 + lane] = q[ds][part];
+      }
+    rt[i].mk0 = live ? p.mask[2 * (size_t)tok] : 0ull;
+    rt[i].mk1 = live ? p.mask[2 * (size_t)tok + 1] : 0ull;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) rt[i].o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    rt[i].pz[0] = rt[i].pz[1] = 0.f;
+    rt[i].m_run = -INFINITY;
+    rt[i].l_run = 0.f;
+  }
+  if constexpr (NQ > 1) __syncthreads();  // the queries are in LDS
+  auto query = [&](int i, int ds, int part) {
+    if constexpr (NQ == 1)
+      return as_bf16x8(qr[ds][part]);
+    else
+      return as_bf16x8(q_s[(((qw + QW * i) * 4 + ds) * PARTS + part) * 64 + lane]);
+  };
+  const float c = p.scale_log2;
+  const KvqBits bits;
+
   int blk = b0 + par;
   if (n_live > 0) {
-    if (n4 > 0) request(blk);
     for (; blk < min(b1, n4); blk += PARS) {
         const u32x4 kc[2] = {kw[0], kw[1]}, vc[2] = {vw[0], vw[1]};
         const u32x2 pc = pr;
@@ -187,10 +215,10 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
             for (int d = 0; d < 2; ++d) {
               const bf16x8 x = as_bf16x8(kvq_expand(kc[t][2 * g + d], bits));
 #pragma unroll
-              for (int part = PLANES ? 1 : 0; part >= 0; --part)
+              for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
                 for (int i = 0; i < NQ; ++i)
-                  acc[i][g] = mfma16x16x32(x, as_bf16x8(rt[i].q[2 * g + d][part]), acc[i][g]);
+                  acc[i][g] = mfma16x16x32(x, query(i, 2 * g + d, part), acc[i][g]);
             }
           }
 #pragma unroll
@@ -257,9 +285,9 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
           for (int i = 0; i < NQ; ++i) {
             floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int part = PLANES ? 1 : 0; part >= 0; --part)
+            for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
-              for (int ds = 0; ds < 4; ++ds) acc = mfma16x16x32(as_bf16x8(kf[ds]), as_bf16x8(rt[i].q[ds][part]), acc);
+              for (int ds = 0; ds < 4; ++ds) acc = mfma16x16x32(as_bf16x8(kf[ds]), query(i, ds, part), acc);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sv[i][4 * t + e] = acc[e];
           }
@@ -315,6 +343,7 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
     }
   }
 
+  if constexpr (NQ > 1) __syncthreads();  // the queries' LDS is free
   // ---- the waves meet in LDS: thread -> row tid / 32 + 16 n, dims 4 (tid % 32) .. + 3
 #pragma unroll
   for (int i = 0; i < NQ; ++i) {
@@ -372,21 +401,33 @@ __global__ __launch_bounds__(NT) void kvq_merge_kernel(KvqAttnLaunch p) {
   for (int j = 1; j < p.sb.B; ++j) sq = tok >= p.sb.t0[j] ? j : sq;
   const int KS = p.splits[sq];
   if (KS == 1) return;  // already final
+  constexpr int N = 8;  // rows in flight: one round trip for all of them
   float M = -INFINITY, l = 0.f;
   floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < KS; ++s) {
-    const float *row = p.part + ((size_t)s * n_rows + at) * OROW;
-    const float2 ml = *(const float2 *)(row + 128);
-    const floatx4 x = *(const floatx4 *)(row + d4);
-    if (ml.x > M) {
-      const float f = exp2f(M - ml.x);
-      o *= f;
-      l *= f;
-      M = ml.x;
+  for (int s0 = 0; s0 < KS; s0 += N) {
+    float2 ml[N];
+    floatx4 x[N];
+#pragma unroll
+    for (int v = 0; v < N; ++v) {
+      const float *row = p.part + ((size_t)min(s0 + v, KS - 1) * n_rows + at) * OROW;
+      ml[v] = *(const float2 *)(row + 128);
+      x[v] = *(const floatx4 *)(row + d4);
     }
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-    l += f * ml.y;
-    o += f * x;
+    __builtin_amdgcn_sched_barrier(0);
+    float m = M;
+#pragma unroll
+    for (int v = 0; v < N; ++v) m = fmaxf(m, ml[v].x);  // (the last row repeats)
+    const float keep = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - m);
+    o *= keep;
+    l *= keep;
+    M = m;
+#pragma unroll
+    for (int v = 0; v < N; ++v) {
+      const float f = s0 + v >= KS || ml[v].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[v].x - M);
+      // (a split that sees NaN alone has no maximum: 0 times its sum keeps it)
+      l += s0 + v < KS ? f * ml[v].y : 0.f;
+      if (s0 + v < KS) o += f * x[v];
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if constexpr (PLANES)
@@ -532,8 +573,8 @@ __global__ __launch_bounds__(256) void kvq_score_kernel(KvqScoreLaunch p) {
 
 // 16-row tiles a wave holds and waves side by side, by the most tiles a kv head has
 static void kvq_shape(int tiles, int *nq, int *qw) {
-  *nq = 1;
-  *qw = tiles <= 1 ? 1 : tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
+  *nq = tiles <= 1 ? 1 : 2;
+  *qw = tiles <= 2 ? 1 : tiles <= 4 ? 2 : 4;
 }
 
 int kvq_attn_max_splits(int nkv) { return std::max(1, std::min(64, 512 / nkv)); }
@@ -574,9 +615,9 @@ void kvq_attn_plan(KvqAttnLaunch &a) {
 template <bool PLANES>
 static hipError_t launch_attn(const KvqAttnLaunch &a, hipStream_t s) {
   auto kernel = a.tiles <= 1   ? kvq_attention_kernel<1, 1, 8, PLANES>
-                : a.tiles <= 2 ? kvq_attention_kernel<1, 2, 4, PLANES>
-                : a.tiles <= 4 ? kvq_attention_kernel<1, 4, 2, PLANES>
-                               : kvq_attention_kernel<1, 8, 1, PLANES>;
+                : a.tiles <= 2 ? kvq_attention_kernel<2, 1, 8, PLANES>
+                : a.tiles <= 4 ? kvq_attention_kernel<2, 2, 4, PLANES>
+                               : kvq_attention_kernel<2, 4, 2, PLANES>;
   const bool merge = *std::max_element(a.splits, a.splits + a.sb.B) > 1;
   const hipEvent_t ev0 = (hipEvent_t)a.ev_start, ev1 = (hipEvent_t)a.ev_stop;
   if (ev0)
