@@ -87,6 +87,9 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
   static_assert((size_t)QW * NQ * 4 * PARTS * 1024 <= sizeof(rows_s), "queries fit");
   __shared__ __attribute__((aligned(16))) floatx4 par_s[8][2 * kQB];  // per wave: affine pairs of 32 keys, 32 values
 
+  __shared__ float fac_s[RW][PARS];  // what a row's waves are added with
+  __shared__ int at_s[RW];           // its place, token x heads + head
+
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qw = wave % QW, par = wave / QW;
@@ -128,23 +131,32 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
   RTile rt[NQ];
   u32x4 qr[4][PARTS];  // the queries, with one tile a wave
   const int n_live = min(NQ, ((min(R - row0, RW) + 15) / 16 - qw + QW - 1) / QW);
+  // queries and masks, all requested before the first is used
+  u32x4 qa[NQ][4][PARTS];  // B operand, dims 32 ds + 8 (lane / 16) .. + 7, parts hi, lo
+  int tok_of[NQ], head_of[NQ];
 #pragma unroll
   for (int i = 0; i < NQ; ++i) {
-    const int r = row0 + (qw + QW * i) * 16 + lr;
-    const bool live = r < R;
-    const int rc = min(r, R - 1);
-    const int tok = t0 + rc / G, head = kvh * G + rc % G;
-    u32x4 q[4][PARTS];  // B operand, dims 32 ds + 8 (lane / 16) .. + 7, parts hi, lo
+    const int r = row0 + (qw + QW * i) * 16 + lr, rc = min(r, R - 1);
+    const int tok = tok_of[i] = t0 + rc / G, head = head_of[i] = kvh * G + rc % G;
 #pragma unroll
     for (int ds = 0; ds < 4; ++ds) {
       if constexpr (PLANES) {
         const unsigned char *src = (const unsigned char *)p.q + plane_off(MT, tok, head * 128 + ds * 32 + lg * 8);
-        q[ds][0] = *(const u32x4 *)src;
-        q[ds][1] = *(const u32x4 *)(src + kPlaneLo);
+        qa[i][ds][0] = *(const u32x4 *)src;
+        qa[i][ds][1] = *(const u32x4 *)(src + kPlaneLo);
       } else {
-        q[ds][0] = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + ds * 32 + lg * 8);
+        qa[i][ds][0] = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + ds * 32 + lg * 8);
       }
     }
+    rt[i].mk0 = p.mask[2 * (size_t)tok];
+    rt[i].mk1 = p.mask[2 * (size_t)tok + 1];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const bool live = row0 + (qw + QW * i) * 16 + lr < R;
+    const int tok = tok_of[i], head = head_of[i];
+    const u32x4 (&q)[4][PARTS] = qa[i];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       float sum = 0.f;
@@ -175,8 +187,8 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
         else if (par == 0)
           q_s[(((qw + QW * i) * 4 + ds) * PARTS + part) * 64 + lane] = q[ds][part];
       }
-    rt[i].mk0 = live ? p.mask[2 * (size_t)tok] : 0ull;
-    rt[i].mk1 = live ? p.mask[2 * (size_t)tok + 1] : 0ull;
+    rt[i].mk0 = live ? rt[i].mk0 : 0ull;
+    rt[i].mk1 = live ? rt[i].mk1 : 0ull;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) rt[i].o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
     rt[i].pz[0] = rt[i].pz[1] = 0.f;
@@ -271,57 +283,66 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the parameters' LDS is written next
     }
     for (; blk < b1; blk += PARS) {
-        // tree rows: keys and values straight from the tail
+        // tree rows: keys and values straight from the tail, all requested at once
         const int k0 = (blk - n4) * kQB;
         const int j0 = k0 + 8 * lg, keep_n = max(0, min(8, T - j0));  // keys of the lane that exist
-        float sv[NQ][8];
+        u32x4 kf[2][4], vf[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const bf16_t *kr = tk + (size_t)min(k0 + kvq_key_of(t, lr), tcap - 1) * 128 + lg * 8;
-          u32x4 kf[4];
+          const bf16_t *row = tk + (size_t)min(k0 + kvq_key_of(t, lr), tcap - 1) * 128 + lg * 8;
 #pragma unroll
-          for (int ds = 0; ds < 4; ++ds) kf[ds] = *(const u32x4 *)(kr + ds * 32);
+          for (int ds = 0; ds < 4; ++ds) kf[t][ds] = *(const u32x4 *)(row + ds * 32);
+        }
 #pragma unroll
-          for (int i = 0; i < NQ; ++i) {
+        for (int dt = 0; dt < 8; ++dt) vf[dt] = *(const u32x4 *)(tv + (size_t)(16 * dt + lr) * tcap + min(j0, tcap - 8));
+        __builtin_amdgcn_sched_barrier(0);
+        float sv[NQ][8];
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
             floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
-              for (int ds = 0; ds < 4; ++ds) acc = mfma16x16x32(as_bf16x8(kf[ds]), query(i, ds, part), acc);
+              for (int ds = 0; ds < 4; ++ds) acc = mfma16x16x32(as_bf16x8(kf[t][ds]), query(i, ds, part), acc);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sv[i][4 * t + e] = acc[e];
           }
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        __builtin_amdgcn_sched_barrier(0);
         u32x4 ph[NQ], pl[NQ];
         uint32_t seen[NQ];
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
           const uint64_t win = j0 >= 128 ? 0ull : j0 >= 64 ? rt[i].mk1 >> (j0 - 64) : rt[i].mk0 >> j0;
-          const uint32_t vis = seen[i] = (uint32_t)win & ((1u << keep_n) - 1u);
+          seen[i] = (uint32_t)win & ((1u << keep_n) - 1u);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) sv[i][u] = (vis >> u) & 1u ? sv[i][u] : -INFINITY;
+          for (int u = 0; u < 8; ++u) sv[i][u] = (seen[i] >> u) & 1u ? sv[i][u] : -INFINITY;
           float pv[8];
           softmax_step(rt[i], sv[i], c, pv);
           split8(pv, ph[i], pl[i]);
         }
         __builtin_amdgcn_sched_barrier(0);
+        uint32_t end = 0;  // bit 15 of a half: an exponent of all ones
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-          u32x4 vf = *(const u32x4 *)(tv + (size_t)(16 * dt + lr) * tcap + min(j0, tcap - 8));
+        for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
-            vf[w] &= (2 * w < keep_n ? 0xffffu : 0u) | (2 * w + 1 < keep_n ? 0xffff0000u : 0u);
+          for (int w = 0; w < 4; ++w) {
+            vf[dt][w] &= (2 * w < keep_n ? 0xffffu : 0u) | (2 * w + 1 < keep_n ? 0xffff0000u : 0u);
+            end |= (vf[dt][w] & 0x7fff7fffu) + 0x00800080u;
+          }
+        if (__ballot(end & 0x80008000u)) {
           // infinities and NaN must not reach the rows that do not see them (0
           // times them is NaN): they are taken out, and the rows that see one
           // get NaN
-          u32x4 odd;
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
-            odd[w] = ((vf[w] & 0x7f80u) == 0x7f80u ? 0x3f80u : 0u) | ((vf[w] & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0u);
-          if (__ballot(odd[0] | odd[1] | odd[2] | odd[3])) {
+          for (int dt = 0; dt < 8; ++dt) {
+            u32x4 odd;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) vf[w] &= (odd[w] & 0xffffu ? 0u : 0xffffu) | (odd[w] >> 16 ? 0u : 0xffff0000u);
+            for (int w = 0; w < 4; ++w) {
+              odd[w] = ((((vf[dt][w] & 0x7fff7fffu) + 0x00800080u) >> 15) & 0x00010001u) * 0x3f80u;  // 1.0 where one is
+              vf[dt][w] &= ~(odd[w] / 0x3f80u * 0xffffu);
+            }
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
               u32x4 on;
@@ -333,12 +354,13 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
               for (int e = 0; e < 4; ++e) rt[i].o[dt][e] = n[e] > 0.f ? NAN : rt[i].o[dt][e];
             }
           }
+        }
 #pragma unroll
-          for (int i = 0; i < NQ; ++i) {
-            rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(pl[i]), rt[i].o[dt]);
-            rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf), as_bf16x8(ph[i]), rt[i].o[dt]);
-          }
-          if (dt & 1) __builtin_amdgcn_sched_barrier(0);
+        for (int dt = 0; dt < 8; ++dt) {
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf[dt]), as_bf16x8(pl[i]), rt[i].o[dt]);
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf[dt]), as_bf16x8(ph[i]), rt[i].o[dt]);
         }
     }
   }
@@ -356,36 +378,48 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
     }
   }
   __syncthreads();
-  const int d4 = (tid & 31) * 4;
-  for (int rl = tid >> 5; rl < min(R - row0, RW); rl += NT / 32) {
-    const int r = row0 + rl, tok = t0 + r / G, head = kvh * G + r % G;
+  // a row's factors of the waves' sums, its place, maximum and sum: a thread a row
+  const int n_rows = min(R - row0, RW);
+  const size_t part0 = (size_t)ks * p.sb.t0[p.sb.B] * p.nh;
+  if (tid < n_rows) {
+    const int r = row0 + tid, at = (t0 + r / G) * p.nh + kvh * G + r % G;
     float2 ml[PARS];
-    float M = -INFINITY;
+    float M = -INFINITY, l = 0.f;
 #pragma unroll
     for (int w = 0; w < PARS; ++w) {
-      ml[w] = *(const float2 *)(rows_s[w][rl] + 128);
+      ml[w] = *(const float2 *)(rows_s[w][tid] + 128);
       M = fmaxf(M, ml[w].x);
     }
-    float l = 0.f;
-    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+    float f[PARS];
 #pragma unroll
     for (int w = 0; w < PARS; ++w) {
-      const float f = ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - M);
-      l += f * ml[w].y;
-      o += f * *(const floatx4 *)(rows_s[w][rl] + d4);
+      f[w] = ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - M);
+      l += f[w] * ml[w].y;
     }
-    const size_t at = (size_t)tok * p.nh + head;
-    if (KS == 1) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      if constexpr (PLANES)
-        store_plane4((unsigned char *)p.out, MT, tok, head * 128 + d4, {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
-      else
-        *(u32x2 *)((bf16_t *)p.out + at * 128 + d4) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
-      if (p.lse && d4 == 0) p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+    const float inv = KS > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) fac_s[tid][w] = f[w] * inv;
+    at_s[tid] = at;
+    if (KS > 1)
+      *(float2 *)(p.part + (part0 + at) * OROW + 128) = float2{M, l};
+    else if (p.lse)
+      p.lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+  }
+  __syncthreads();
+  const int d4 = (tid & 31) * 4;
+#pragma unroll 2
+  for (int rl = tid >> 5; rl < n_rows; rl += NT / 32) {
+    const int at = at_s[rl];
+    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) o += fac_s[rl][w] * *(const floatx4 *)(rows_s[w][rl] + d4);
+    if (KS > 1) {
+      *(floatx4 *)(p.part + (part0 + at) * OROW + d4) = o;
+    } else if constexpr (PLANES) {
+      const int tok = at / p.nh;
+      store_plane4((unsigned char *)p.out, MT, tok, (at - tok * p.nh) * 128 + d4, {o[0], o[1], o[2], o[3]});
     } else {
-      float *row = p.part + ((size_t)ks * p.sb.t0[p.sb.B] * p.nh + at) * OROW;
-      *(floatx4 *)(row + d4) = o;
-      if (d4 == 0) *(float2 *)(row + 128) = float2{M, l};
+      *(u32x2 *)((bf16_t *)p.out + (size_t)at * 128 + d4) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
     }
   }
 }
