@@ -475,131 +475,152 @@ __global__ __launch_bounds__(NT) void kvq_merge_kernel(KvqAttnLaunch p) {
 // Accumulated weights.  Here the rows are the A operand and the keys the B
 // operand, S = Q K^T: a lane then holds one key and four rows, and the sum over
 // rows is over its registers and four lane groups.  Rows: path node x head, r =
-// i G + a, in passes of kPassTiles tiles, whose queries lie in LDS as three
-// bf16 parts (a float32 to its last bits, so that a weight is exact to
-// float32's own rounding of its exponent).  Workgroup: (layer and kv head, run
-// of blocks), four waves, a block a wave.
-
-constexpr int kPassTiles = 2;
+// i G + a, in passes of TILES tiles, whose queries stay in registers as bf16
+// parts: three of a float32 (its last bits too, so that a weight is exact to
+// float32's own rounding of its exponent), one of a bfloat16.  A wave takes every
+// step-th block of a (layer, kv head), the next one requested ahead.
 struct ScoreRow {
   float qs0, qs1, lse2;  // sums of q over the groups, ln sum exp in log2
   int node;              // place on the path; rows that do not exist: -1
 };
+constexpr int kScoreWaves = 4;
 
-__global__ __launch_bounds__(256) void kvq_score_kernel(KvqScoreLaunch p) {
-  __shared__ u32x4 q_s[kPassTiles][4][3][64];
-  __shared__ ScoreRow row_s[kPassTiles * 16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int lr = lane & 15, lg = lane >> 4;
-  const int lh = blockIdx.x, layer = lh / p.nkv, kvh = lh % p.nkv;
-  const int n = max(0, min(*p.n_path, min(p.path_len, p.cap - p.L)));
-  const int G = p.nh / p.nkv, R = n * G;
-  const int n4 = (p.L + kQB - 1) / kQB, nblk = n4 + (n + kQB - 1) / kQB;
+template <int TILES, int PARTS>
+__global__ __launch_bounds__(64 * kScoreWaves, 2) void kvq_score_kernel(KvqScoreLaunch p) {
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int lh = blockIdx.x / p.runs, layer = lh / p.nkv, kvh = lh % p.nkv;
+  const int first = (blockIdx.x % p.runs) * kScoreWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int step = p.runs * kScoreWaves;
   const unsigned char *blocks = p.blocks + (size_t)lh * p.nb * kQBytes;
-  const bf16_t *tk = p.tk + (size_t)lh * p.tcap * 128;
   const float *in = p.in ? p.in + (size_t)lh * p.cap : nullptr;
   float *out = p.out + (size_t)lh * p.cap;
+  const int n4 = (p.L + kQB - 1) / kQB;
   const float c = p.scale_log2;
   const KvqBits bits;
-  for (int r0 = 0; r0 == 0 || r0 < R; r0 += kPassTiles * 16) {
-    __syncthreads();
-    const int tiles = min(kPassTiles, (R - r0 + 15) / 16);
-    // row tid / 8 (of 32), dims 16 (tid % 8) .. + 15
-    {
-      const int r = r0 + tid / 8, rl = tid / 8;
+  // a block's keys: codes, this lane's keys' parameters, their sums so far
+  u32x4 kw[2];
+  u32x2 pr[2];
+  float base[2];
+  auto request = [&](int blk, bool more) {
+    blk = blk < n4 ? blk : 0;  // past the last one: the first again
+    const unsigned char *src = blocks + (size_t)blk * kQBytes;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int j = kvq_key_of(t, lr);
+      kw[t] = *(const u32x4 *)(src + (t * 64 + lane) * 16);
+      pr[t] = *(const u32x2 *)(src + kQP + j * 8);
+      const float *from = more ? out : in;
+      base[t] = from ? from[min(blk * kQB + j, p.L - 1)] : 0.f;
+    }
+  };
+  if (n4 > 0) request(first, false);
+  const int n = max(0, min(*p.n_path, min(p.path_len, p.cap - p.L)));
+  const int G = p.nh / p.nkv, R = n * G, nblk = n4 + (n + kQB - 1) / kQB;
+
+  for (int r0 = 0; r0 == 0 || r0 < R; r0 += TILES * 16) {
+    const bool more = r0 > 0;  // a further pass adds to the sums of the last
+    if (more && n4 > 0) request(first, true);
+    // ---- the pass's rows: lane lr loads row r0 + 16 m + lr; the products' rows
+    // are 4 lg + e
+    u32x4 q[TILES][4][PARTS];
+    ScoreRow row[TILES][4];
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) {
+      const int r = r0 + 16 * m + lr;
       const bool live = r < R;
-      const int i = live ? r / G : 0, head = kvh * G + (live ? r % G : 0);
+      const int i = live ? r / G : 0, head = kvh * G + (live ? r - i * G : 0);
       const int node = n > 0 ? max(0, min(p.path[i], p.T - 1)) : 0;
       const size_t at = ((size_t)layer * p.rows + node) * p.nh + head;
-      float sum = 0.f;
+      const float lse = p.lse[at];
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int d = 16 * (tid % 8) + 8 * b;
+      for (int ds = 0; ds < 4; ++ds) {
         float v[8];
-        if (!live) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        } else if (p.q_bf16) {
-          const u32x4 w = *(const u32x4 *)((const bf16_t *)p.q + at * 128 + d);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = bf16_to_f32((w[e >> 1] >> (16 * (e & 1))) & 0xffffu);
+        if constexpr (PARTS == 1) {
+          const u32x4 w = *(const u32x4 *)((const bf16_t *)p.q + at * 128 + ds * 32 + lg * 8);
+          q[m][ds][0] = w;
+          sum[ds >> 1] += live ? sum8(w) : 0.f;
         } else {
-          const floatx4 x = *(const floatx4 *)((const float *)p.q + at * 128 + d);
-          const floatx4 y = *(const floatx4 *)((const float *)p.q + at * 128 + d + 4);
+          const floatx4 x = *(const floatx4 *)((const float *)p.q + at * 128 + ds * 32 + lg * 8);
+          const floatx4 y = *(const floatx4 *)((const float *)p.q + at * 128 + ds * 32 + lg * 8 + 4);
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = x[e], v[4 + e] = y[e];
-        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += v[e];
+          for (int e = 0; e < 8; ++e) sum[ds >> 1] += live ? v[e] : 0.f;
 #pragma unroll
-        for (int part = 0; part < 3; ++part) {
-          u32x4 w;
+          for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-            v[2 * e] -= __uint_as_float(w[e] << 16);
-            v[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
-          }
-          q_s[rl >> 4][d >> 5][part][(rl & 15) + 16 * ((d >> 3) & 3)] = w;
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t w = q[m][ds][part][e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+              v[2 * e] -= __uint_as_float(w << 16);
+              v[2 * e + 1] -= __uint_as_float(w & 0xffff0000u);
+            }
         }
       }
-      // the four threads of a group
-      sum += __shfl_xor(sum, 1, 64);
-      sum += __shfl_xor(sum, 2, 64);
-      const float other = __shfl_xor(sum, 4, 64);
-      if (tid % 8 == 0)
-        row_s[rl] = ScoreRow{sum, other, live ? p.lse[at] * 1.4426950408889634f : INFINITY, live ? i : -1};
+      sum[0] = quad_sum(sum[0]);
+      sum[1] = quad_sum(sum[1]);
+      const float l2 = lse * 1.4426950408889634f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        row[m][e] = ScoreRow{__shfl(sum[0], 4 * lg + e, 64), __shfl(sum[1], 4 * lg + e, 64), __shfl(l2, 4 * lg + e, 64),
+                             __shfl(live ? i : -1, 4 * lg + e, 64)};
     }
-    __syncthreads();
-    for (int blk = blockIdx.y * 4 + wave; blk < nblk; blk += gridDim.y * 4) {
-      const bool tree = blk >= n4;
-      const int k0 = tree ? (blk - n4) * kQB : blk * kQB;
+    // weights of this lane's key: a its affine pairs, only rows from `from` on
+    auto weigh = [&](const u32x4 (&b)[4], float4 a, int from) {
+      float w = 0.f;
+#pragma unroll
+      for (int m = 0; m < TILES; ++m) {
+        if (m > 0 && r0 + 16 * m >= R) break;
+        floatx4 acc[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          acc[g] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+            for (int d = 0; d < 2; ++d)
+              acc[g] = mfma16x16x32(as_bf16x8(q[m][2 * g + d][part]), as_bf16x8(b[2 * g + d]), acc[g]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const ScoreRow &x = row[m][e];
+          const float s = fmaf(a.x, acc[0][e], a.y * x.qs0) + fmaf(a.z, acc[1][e], a.w * x.qs1);
+          w += x.node >= from ? __builtin_amdgcn_exp2f(fmaf(s, c, -x.lse2)) : 0.f;
+        }
+      }
+      return quad_sum(w);
+    };
+    // ---- the prefix
+    int blk = first;
+    for (; blk < n4; blk += step) {
+      const u32x4 kc[2] = {kw[0], kw[1]};
+      const u32x2 pc[2] = {pr[0], pr[1]};
+      const float bc[2] = {base[0], base[1]};
+      request(blk + step, more);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const int j = kvq_key_of(t, lr);  // this lane's key of the block
         u32x4 b[4];
-        float4 a = float4{1.f, 0.f, 1.f, 0.f};
-        if (!tree) {
-          const unsigned char *src = blocks + (size_t)blk * kQBytes;
-          const u32x4 w = *(const u32x4 *)(src + (t * 64 + lane) * 16);
-          const u32x2 pr = *(const u32x2 *)(src + kQP + j * 8);
 #pragma unroll
-          for (int ds = 0; ds < 4; ++ds) b[ds] = kvq_expand(w[ds], bits);
-          const float2 a0 = kvq_affine(pr[0]), a1 = kvq_affine(pr[1]);
-          a = float4{a0.x, a0.y, a1.x, a1.y};
-        } else {
-          const int node = max(0, min(p.path[min(k0 + j, n - 1)], min(p.T, p.tcap) - 1));
-#pragma unroll
-          for (int ds = 0; ds < 4; ++ds) b[ds] = *(const u32x4 *)(tk + (size_t)node * 128 + ds * 32 + lg * 8);
-        }
-        float w = 0.f;
-        for (int m = 0; m < tiles; ++m) {
-          floatx4 acc[2];
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            acc[g] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int part = 2; part >= 0; --part)
-#pragma unroll
-              for (int d = 0; d < 2; ++d)
-                acc[g] = mfma16x16x32(as_bf16x8(q_s[m][2 * g + d][part][lane]), as_bf16x8(b[2 * g + d]), acc[g]);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const ScoreRow row = row_s[m * 16 + 4 * lg + e];
-            const float s = fmaf(a.x, acc[0][e], a.y * row.qs0) + fmaf(a.z, acc[1][e], a.w * row.qs1);
-            const bool seen = row.node >= 0 && (!tree || row.node >= k0 + j);
-            w += seen ? __builtin_amdgcn_exp2f(fmaf(s, c, -row.lse2)) : 0.f;
-          }
-        }
-        w = quad_sum(w);
-        const int pos = tree ? p.L + k0 + j : k0 + j;
-        if (lg == 0 && (tree ? k0 + j < n : pos < p.L)) {
-          const float base = r0 > 0 ? out[pos] : tree || !in ? 0.f : in[pos];
-          out[pos] = base + w;
-        }
+        for (int ds = 0; ds < 4; ++ds) b[ds] = kvq_expand(kc[t][ds], bits);
+        const float2 a0 = kvq_affine(pc[t][0]), a1 = kvq_affine(pc[t][1]);
+        const float w = weigh(b, float4{a0.x, a0.y, a1.x, a1.y}, 0);
+        const int pos = blk * kQB + kvq_key_of(t, lr);
+        if (lg == 0 && pos < p.L) out[pos] = bc[t] + w;
       }
     }
+    // ---- the accepted nodes' own keys, from the tail
+    const bf16_t *tk = p.tk + (size_t)lh * p.tcap * 128;
+    for (; blk < nblk; blk += step)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int k = (blk - n4) * kQB + kvq_key_of(t, lr);
+        const int node = max(0, min(p.path[min(k, n - 1)], min(p.T, p.tcap) - 1));
+        u32x4 b[4];
+#pragma unroll
+        for (int ds = 0; ds < 4; ++ds) b[ds] = *(const u32x4 *)(tk + (size_t)node * 128 + ds * 32 + lg * 8);
+        const float w = weigh(b, float4{1.f, 0.f, 1.f, 0.f}, k);
+        if (lg == 0 && k < n) out[p.L + k] = (more ? out[p.L + k] : 0.f) + w;
+      }
   }
 }
 
@@ -674,9 +695,16 @@ hipError_t launch_kvq_attn(const KvqAttnLaunch &a, hipStream_t s) {
   return a.planes ? launch_attn<true>(a, s) : launch_attn<false>(a, s);
 }
 
-hipError_t launch_kvq_score(const KvqScoreLaunch &p, hipStream_t s) {
+hipError_t launch_kvq_score(KvqScoreLaunch p, hipStream_t s) {
+  // Enough workgroups to fill the chip twice, eight blocks a wave or more where
+  // there are.  How many rows there are is only known on the device: an accepted
+  // path is a few nodes, so a tile holds those of one or two heads, two tiles
+  // those of four.
   const int heads = p.layers * p.nkv, nblk = (p.L + p.path_len + 2 * kQB - 2) / kQB;
-  const int want = std::max(1, 1024 / heads);
-  hipLaunchKernelGGL(kvq_score_kernel, dim3(heads, std::max(1, std::min(want, (nblk + 3) / 4))), dim3(256), 0, s, p);
+  p.runs = std::max(1, std::min((1024 + heads - 1) / heads, nblk / (8 * kScoreWaves)));
+  const bool two = p.nh / p.nkv > 2;
+  auto kernel = p.q_bf16 ? (two ? kvq_score_kernel<2, 1> : kvq_score_kernel<1, 1>)
+                         : (two ? kvq_score_kernel<2, 3> : kvq_score_kernel<1, 3>);
+  hipLaunchKernelGGL(kernel, dim3(heads * p.runs), dim3(64 * kScoreWaves), 0, s, p);
   return hipGetLastError();
 }

@@ -118,8 +118,9 @@ struct KvqScoreLaunch {
   const float *in;
   float *out;
   float scale_log2;
+  int runs;  // workgroups a (layer, kv head) (the launcher's)
 };
-hipError_t launch_kvq_score(const KvqScoreLaunch &p, hipStream_t s);
+hipError_t launch_kvq_score(KvqScoreLaunch p, hipStream_t s);
 
 // The step of ppd_api.cpp on 4-bit caches
 struct KvqStep {
