@@ -431,8 +431,8 @@ ppd_status ppd_kvq_attention(int32_t n_heads, int32_t B, const ppd_kvq *kvs, int
  * ppd_verify_step and ppd_verify_batch on 4-bit caches.  pos[s] is the
  * position of sequence s's root (its node i sits at pos[s] + depth[i]): L[s]
  * as long as nothing was evicted, else the number of tokens so far.  The tree's
- * rows go to kvs[s].tail, whose capacity has to hold T[s]; L[s] <=
- * kvs[s].capacity.  ws: ppd_kvq_workspace_bytes(model, all tree tokens).
+ * rows go to kvs[s].tail, which no other sequence shares and whose capacity
+ * has to hold T[s]; L[s] <= kvs[s].capacity.  ws: ppd_kvq_workspace_bytes(model, all tree tokens).
  *   q_out    device float32 [n_layers][all tree tokens][n_heads][128]: the
  *            queries after RoPE, or NULL
  *   lse_out  device float32 [n_layers][all tree tokens][n_heads], or NULL

@@ -206,6 +206,16 @@ def _dev(t, dtype=None, name="tensor"):
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
 
 
+def _here(**tensors):
+    """Refuse tensors of another device than the current one, on whose stream
+    a call is enqueued."""
+    import torch
+    now = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != now:
+            raise ValueError(f"{name} is on device {t.get_device()}, the current device is {now}")
+
+
 # ---------------------------------------------------------------------------
 
 
@@ -325,9 +335,11 @@ class KVQCache:
 
     def _on_device(self):
         _dev(self.blocks, None, "blocks")
+        _here(blocks=self.blocks)
         if self.tail is not None:
             _dev(self.tail.k, None, "tail.k")
             _dev(self.tail.v, None, "tail.v")
+            _here(tail=self.tail.k)
 
 
 # ---------------------------------------------------------------------------
@@ -491,6 +503,7 @@ def _rows_of(kv: KVQCache, other: KVCache, name: str):
     KVQCache._check_rows(other, (kv.n_layers, kv.n_kv_heads), name)
     _dev(other.k, None, name)
     _dev(other.v, None, name)
+    _here(**{name: other.k})
 
 
 def ppd_kvq_quantize(kv: KVQCache, dst_pos: int, src: KVCache, src_pos: int, n: int, stream=None):
@@ -542,6 +555,7 @@ def ppd_kvq_attention(kvs: Sequence[KVQCache], layer: int, L: Sequence[int], T: 
     _dev(mask, None, "mask")
     _dev(ws, None, "ws")
     B, descs, Ls, Ts = _kvq_batch(kvs, L, T)
+    _here(q=q, out=out, mask=mask, ws=ws, lse=lse)
     n = int(Ts.sum())
     if q.dim() != 3 or tuple(q.shape) != (n, q.shape[1], 128) or out.shape != q.shape:
         raise ValueError(f"q and out must be [{n}][heads][128]")
@@ -558,9 +572,10 @@ def ppd_kvq_workspace_bytes(model: Model, t_max: int) -> int:
     return _bytes(lib().ppd_kvq_workspace_bytes(C.byref(model.desc), int(t_max)))
 
 
-def _trace(model, n, q_out, lse_out):
+def _trace(model, n, q_out, lse_out, **tensors):
     import torch
     sh = model.shape
+    _here(q_out=q_out, lse_out=lse_out, **tensors)
     _dev(q_out, torch.float32, "q_out")
     _dev(lse_out, torch.float32, "lse_out")
     if q_out is not None and tuple(q_out.shape) != (sh.n_layers, n, sh.n_heads, 128):
@@ -578,7 +593,7 @@ def ppd_verify_batch_kvq(model: Model, kvs: Sequence[KVQCache], L: Sequence[int]
     _dev(ws, None, "ws")
     _dev(logits, torch.float32, "logits")
     B, descs, Ls, ps, Ts = _kvq_batch(kvs, L, pos, T)
-    _trace(model, int(Ts.sum()), q_out, lse_out)
+    _trace(model, int(Ts.sum()), q_out, lse_out, ids=ids, ws=ws, pred=pred, logits=logits)
     _check(lib().ppd_verify_batch_kvq(C.byref(model.desc), B, C.cast(descs, C.c_void_p), _np_ptr(Ls), _np_ptr(ps),
                                       _np_ptr(Ts), _ptr(ids), _ptr(depth), _ptr(mask), _ptr(ws),
                                       ws.numel() * ws.element_size(), _ptr(logits) or None, _ptr(pred),
@@ -594,7 +609,7 @@ def ppd_verify_step_kvq(model: Model, kv: KVQCache, L: int, pos: int, T: int, id
     _dev(ws, None, "ws")
     _dev(logits, torch.float32, "logits")
     kv._on_device()
-    _trace(model, int(T), q_out, lse_out)
+    _trace(model, int(T), q_out, lse_out, ids=ids, ws=ws, pred=pred, logits=logits)
     _check(lib().ppd_verify_step_kvq(C.byref(model.desc), C.byref(kv.desc), int(L), int(pos), int(T), _ptr(ids),
                                      _ptr(depth), _ptr(mask), _ptr(ws), ws.numel() * ws.element_size(),
                                      _ptr(logits) or None, _ptr(pred), _ptr(q_out) or None, _ptr(lse_out) or None,
@@ -613,6 +628,8 @@ def ppd_kvq_score(kv: KVQCache, L: int, q, lse, path, n_path, score_in, score_ou
         raise ValueError("q must be [layers][T][heads][128], lse [layers][T][heads]")
     if q.dtype not in (torch.float32, torch.bfloat16) or lse.dtype != torch.float32:
         raise ValueError("q must be float32 or bfloat16, lse float32")
+    if q.is_cuda:
+        _here(q=q, lse=lse, path=path, n_path=n_path, score_in=score_in, score_out=score_out)
     nh, T = int(q.shape[2]), int(q.shape[1])
     rows = T if kv.n_layers == 1 else q.stride(0) // (nh * 128)
     for t, name, row in ((q, "q", nh * 128), (lse, "lse", nh)):
@@ -642,6 +659,7 @@ def ppd_kvq_evict(src: KVQCache, dst: KVQCache, L: int, budget: int, n_sink: int
         _dev(t, torch.float32, name)
         if tuple(t.shape) != (kv.n_layers, kv.n_kv_heads, kv.capacity):
             raise ValueError(f"{name} must be [{kv.n_layers}][{kv.n_kv_heads}][{kv.capacity}]")
+    _here(score=score, score_out=score_out, kept=kept)
     if tuple(kept.shape) != (src.n_layers, src.n_kv_heads, budget):
         raise ValueError(f"kept must be [{src.n_layers}][{src.n_kv_heads}][{budget}]")
     _check(lib().ppd_kvq_evict(C.byref(src.desc), C.byref(dst.desc), int(L), int(budget), int(n_sink), int(n_recent),
@@ -664,6 +682,12 @@ def ppd_accept_sample(T: int, parent, ids, vocab: int, logits, temperature: floa
     _dev(draft, torch.float32, "draft")
     _dev(u, torch.float32, "u")
     _dev(ws, None, "ws")
+    _here(parent=parent, ids=ids, logits=logits, draft=draft, u=u, path=path, n_path=n_path, next_tok=next_tok, ws=ws)
+    n = int(T)
+    for t, name, least in ((parent, "parent", n), (ids, "ids", n), (u, "u", n), (path, "path", n), (logits, "logits", n * vocab),
+                           (draft, "draft", n * vocab), (n_path, "n_path", 1), (next_tok, "next_tok", 1)):
+        if t is not None and t.numel() < least:
+            raise ValueError(f"{name} holds {t.numel()} elements, not {least}")
     _check(lib().ppd_accept_sample(int(T), _ptr(parent), _ptr(ids), int(vocab), _ptr(logits), float(temperature),
                                    _ptr(draft) or None, _ptr(u), _ptr(path), _ptr(n_path), _ptr(next_tok), _ptr(ws),
                                    ws.numel() * ws.element_size(), _stream(stream)))

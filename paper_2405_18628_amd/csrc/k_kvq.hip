@@ -543,7 +543,8 @@ __global__ __launch_bounds__(64 * W) void kvq_gather_kernel(KvqEvict p) {
 // way touch the same positions of their heads; where a dim's row of positions is
 // a multiple of 4 KB they meet in the same memory channels.)
 int runs_of(int heads, int pos0, int n, int waves) {
-  return std::min(INT32_MAX / heads, ((pos0 % kQB + n + kQB - 1) / kQB + waves - 1) / waves);
+  constexpr int kMostWorkgroups = 1 << 22;  // a launch's threads are counted in 32 bits (heads <= 2^20)
+  return std::min(kMostWorkgroups / heads, ((pos0 % kQB + n + kQB - 1) / kQB + waves - 1) / waves);
 }
 
 }  // namespace

@@ -25,7 +25,6 @@
 // max(w - a - b, 0): one row of weights, one of probabilities and a number, but
 // a sum over the row for each rejection, the next depending on it.  A workgroup
 // settles a node alone: weights in registers, probabilities in LDS.
-#include <cfloat>
 
 #include "ppd_sample.h"
 
@@ -141,21 +140,22 @@ __device__ __forceinline__ void note_pick(const double (&r)[4], double run, doub
 // Weights under e^-700 and those of NaN are 0; of an infinite m only its like
 // have weight.
 struct Weights {
-  double m, inv_t, scale;  // scale: 64 / (t ln 2)
-  float top, cut;          // m, and m - 700 t
-  const double *table;     // 2^(j / 64)
+  double m, inv_t, scale, cut;  // scale: 64 / (t ln 2), cut: -700 t
+  bool endless;                 // m is infinite
+  const double *table;          // 2^(j / 64)
   __device__ __forceinline__ Weights(float m_, float t, const double *tab)
-      : m(m_), inv_t(1. / (double)t), scale(92.332482616893656768 / (double)t), top(m_),
-        cut(m_ == INFINITY ? m_ : fmaxf(m_ - 700.f * t, -FLT_MAX)), table(tab) {}
+      : m(m_), inv_t(1. / (double)t), scale(92.332482616893656768 / (double)t), cut(-700. * (double)t),
+        endless(m_ == INFINITY), table(tab) {}
   __device__ __forceinline__ double operator()(float l) const {
-    const double d = top == INFINITY ? 0. : (double)l - m;
+    // (float64: the difference of two floats has no rounding that could pass the cut)
+    const double d = endless ? (l == INFINITY ? 0. : -INFINITY) : (double)l - m;
     const double y = fma(d, scale, 6755399441055744.);
     const uint32_t k = (uint32_t)__builtin_bit_cast(uint64_t, y);
     const double r = fma(y - 6755399441055744., -1.0830424696249145e-02, d * inv_t);  // |r| <= ln 2 / 128
     const double q = fma(r, fma(r, fma(r, 1. / 24., 1. / 6.), 0.5), 1.);
     const double t = table[k & 63];
     const uint64_t w = __builtin_bit_cast(uint64_t, fma(t * r, q, t)) + ((uint64_t)((k & ~63u) << 14) << 32);
-    return l >= cut ? __builtin_bit_cast(double, w) : 0.;
+    return d >= cut ? __builtin_bit_cast(double, w) : 0.;
   }
 };
 __device__ __forceinline__ void fill_table(double *table) {

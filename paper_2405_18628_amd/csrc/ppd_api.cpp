@@ -798,6 +798,9 @@ ppd_status ppd_verify_batch_kvq(const ppd_model *model, int32_t B, const ppd_kvq
       return fail(PPD_EINVAL, "sequence %d: a cache of %d layers and %d heads, not the model's", j, kvs[j].n_layers,
                   kvs[j].n_kv_heads);
     if (pos[j] < 0) return fail(PPD_EINVAL, "pos[%d] must be >= 0", j);
+    for (int i = 0; i < j; ++i)
+      if (kvs[i].tail.k == kvs[j].tail.k || kvs[i].tail.v == kvs[j].tail.v)
+        return fail(PPD_EINVAL, "sequences %d and %d share a tail", i, j);
     tails[j] = kvs[j].tail;
   }
   if (!ids || !depth || !mask || !pred) return fail(PPD_EINVAL, "NULL tree or output pointer");

@@ -15,9 +15,17 @@ namespace {
     if (e_ != hipSuccess) return ppd_fail(PPD_EDEVICE, "%s: %s", #call, hipGetErrorString(e_)); \
   } while (0)
 
+constexpr int kMaxHeads = 1 << 20, kMaxQueryHeads = 1 << 16;
+
+// row and head indices are 32-bit in the kernels
+bool heads_ok(int n_heads, int n_kv_heads) {
+  return n_kv_heads >= 1 && n_heads >= 1 && n_heads <= kMaxQueryHeads && n_heads % n_kv_heads == 0;
+}
+
 ppd_status check_sizes(int n_layers, int n_kv_heads, int capacity) {
   if (n_layers < 1 || n_kv_heads < 1) return ppd_fail(PPD_EINVAL, "a cache needs layers and heads");
-  if ((int64_t)n_layers * n_kv_heads > (1 << 24)) return ppd_fail(PPD_EINVAL, "too many layers and heads");
+  if ((int64_t)n_layers * n_kv_heads > kMaxHeads)  // a launch's threads are counted in 32 bits
+    return ppd_fail(PPD_EUNSUPPORTED, "%lld layers x heads > %d", (long long)n_layers * n_kv_heads, kMaxHeads);
   if (capacity < kQB || capacity % kQB)
     return ppd_fail(PPD_EUNSUPPORTED, "4-bit caches need a capacity that is a multiple of %d, got %d", kQB, capacity);
   if (capacity > PPD_CAPACITY_MAX)
@@ -173,8 +181,8 @@ ppd_status ppd_kvq_commit(const ppd_kvq *kv, int32_t L, const int32_t *path, int
 }
 
 size_t ppd_kvq_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t t_max) {
-  if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || t_max < 1 || t_max > PPD_T_MAX) {
-    ppd_fail(PPD_EINVAL, "n_kv_heads must divide n_heads, t_max be in [1, %d]", PPD_T_MAX);
+  if (!heads_ok(n_heads, n_kv_heads) || t_max < 1 || t_max > PPD_T_MAX) {
+    ppd_fail(PPD_EINVAL, "n_kv_heads must divide n_heads <= %d, t_max be in [1, %d]", kMaxQueryHeads, PPD_T_MAX);
     return 0;
   }
   return 256 + kvq_attn_part_bytes(n_heads, n_kv_heads, t_max);
@@ -187,7 +195,7 @@ ppd_status ppd_kvq_attention(int32_t n_heads, int32_t B, const ppd_kvq *kvs, int
   const ppd_status st = kvq_check_seqs(B, kvs, L, T, &total);
   if (st != PPD_OK) return st;
   const int nkv = kvs[0].n_kv_heads;
-  if (n_heads < 1 || n_heads % nkv) return ppd_fail(PPD_EINVAL, "n_kv_heads must divide n_heads");
+  if (!heads_ok(n_heads, nkv)) return ppd_fail(PPD_EINVAL, "n_kv_heads must divide n_heads <= %d", kMaxQueryHeads);
   for (int j = 0; j < B; ++j) {
     if (kvs[j].n_kv_heads != nkv) return ppd_fail(PPD_EINVAL, "sequence %d has %d kv heads, not %d", j, kvs[j].n_kv_heads, nkv);
     if (layer < 0 || layer >= kvs[j].n_layers)
@@ -221,7 +229,8 @@ ppd_status ppd_kvq_score(const ppd_kvq *kv, int32_t L, int32_t n_heads, int32_t 
   if (st != PPD_OK) return st;
   if ((st = check_kv(&kv->tail, "tail")) != PPD_OK) return st;
   if (L < 0 || L > kv->capacity) return ppd_fail(PPD_ECAPACITY, "L=%d must be in [0, capacity=%d]", L, kv->capacity);
-  if (n_heads < 1 || n_heads % kv->n_kv_heads) return ppd_fail(PPD_EINVAL, "n_kv_heads must divide n_heads");
+  if (!heads_ok(n_heads, kv->n_kv_heads))
+    return ppd_fail(PPD_EINVAL, "n_kv_heads must divide n_heads <= %d", kMaxQueryHeads);
   if (T < 1 || T > PPD_T_MAX || rows < T) return ppd_fail(PPD_EINVAL, "T must be in [1, %d], rows at least T", PPD_T_MAX);
   if (T > kv->tail.capacity)
     return ppd_fail(PPD_ECAPACITY, "%d tree rows exceed the tail's capacity %d", T, kv->tail.capacity);

@@ -102,6 +102,22 @@ def test_rows_with_infinities_and_nan(with_draft):
             _check(parent, ids, V, logits, 1.0, draft, rng.random(T).astype(np.float32))
 
 
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("scale,temperature", [(3e9, 4.0), (1e30, 1.0), (1e-3, 1e-30), (700.0, 1.0), (2e3, 2.8), (1.0, 1e30),
+                                               (3e38, 1e36), (50.0, 0.07)])
+def test_far_logits_and_temperatures(scale, temperature, with_draft):
+    """Logits whose neighbours lie further apart than any weight reaches, and
+    weights down to the smallest number."""
+    rng = np.random.default_rng(7)
+    T, V = 9, 5000
+    parent, ids = _tree(rng, T, "tree"), rng.integers(0, V, T).astype(np.int32)
+    draft = np.full((T, V), 1 / V, np.float32) if with_draft else None
+    for trial in range(3):
+        logits = (rng.uniform(-1, 1, (T, V)) * scale).astype(np.float32)
+        u = rng.random(T).astype(np.float32)
+        _check(parent, ids, V, logits, temperature, draft, u)
+
+
 def test_borders_of_the_draws():
     """Draws of 0 take the first token that has weight, draws of 1 (out of
     range) the last; a draw of 0 accepts every child that has weight."""

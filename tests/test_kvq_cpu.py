@@ -31,11 +31,11 @@ def test_sizes():
     assert ppd.ppd_kvq_bytes(2, 4, 256) == 2 * 4 * 8 * 4608
     assert ppd.ppd_kvq_bytes(32, 32, 1 << 24) == 32 * 32 * (1 << 19) * 4608
     L = ppd.lib()
-    for bad in ((0, 4, 256), (2, 0, 256), (2, 4, 0), (2, 4, 255), (2, 4, (1 << 24) + 32), (1 << 13, 1 << 13, 32)):
+    for bad in ((0, 4, 256), (2, 0, 256), (2, 4, 0), (2, 4, 255), (2, 4, (1 << 24) + 32), (1 << 13, 1 << 13, 32), (1 << 20, 2, 32)):
         assert L.ppd_kvq_bytes(*bad) == 0 and ppd.ppd_last_error()
     small, big = (ppd.ppd_kvq_attention_workspace_bytes(32, 8, t) for t in (1, 128))
     assert 0 < small < big
-    for bad in ((0, 1, 1), (4, 3, 1), (4, 4, 0), (4, 4, 129), (4, 0, 4)):
+    for bad in ((0, 1, 1), (4, 3, 1), (4, 4, 0), (4, 4, 129), (4, 0, 4), (1 << 17, 1, 4)):
         assert L.ppd_kvq_attention_workspace_bytes(*bad) == 0 and ppd.ppd_last_error()
     assert ppd.ppd_accept_sample_workspace_bytes(64, 32000) > 0
     for bad in ((0, 10), (129, 10), (4, 0)):
@@ -145,6 +145,36 @@ def test_verify_refuses():
     assert call(ws=None) == ppd.PPD_EWORKSPACE and call(n=need - 1) == ppd.PPD_EWORKSPACE
 
 
+def test_batch_refuses_a_shared_tail():
+    """Two sequences' trees in one staging cache would overwrite each other."""
+    L = ppd.lib()
+    m, keep = _fake_model()
+    far = dict(k=F + (1 << 20), v=F + (2 << 20), capacity=128)
+    need = L.ppd_kvq_workspace_bytes(C.byref(m), 32)
+
+    def call(second, n=need):
+        arr = (ppd.ppd_kvq * 2)(_kvq(), _kvq(tail=second))
+        v = _i32(16, 16)
+        return L.ppd_verify_batch_kvq(C.byref(m), 2, C.cast(arr, C.c_void_p), v.ctypes.data, v.ctypes.data, v.ctypes.data, F,
+                                      F, F, F, n, None, F, None, None, None)
+    assert call(OK_TAIL) == ppd.PPD_EINVAL and call(dict(far, v=F)) == ppd.PPD_EINVAL
+    assert call(far, need - 1) == ppd.PPD_EWORKSPACE
+
+
+def test_another_device_refuses(monkeypatch):
+    """A tensor of another device than the current one is named."""
+    class On:
+        def __init__(self, d):
+            self.d = d
+
+        def get_device(self):
+            return self.d
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    ppd._here(a=On(1), b=None)
+    with pytest.raises(ValueError, match="q is on device 0"):
+        ppd._here(a=On(1), q=On(0))
+
+
 def test_score_refuses():
     L = ppd.lib()
 
@@ -156,7 +186,7 @@ def test_score_refuses():
     for kw, code in BAD_ROWS:
         assert call(_kvq(tail=kw)) == code, kw
     assert call(Lc=-1) == ppd.PPD_ECAPACITY and call(Lc=257) == ppd.PPD_ECAPACITY
-    assert call(nh=6) == ppd.PPD_EINVAL and call(nh=0) == ppd.PPD_EINVAL
+    assert call(nh=6) == ppd.PPD_EINVAL and call(nh=0) == ppd.PPD_EINVAL and call(nh=1 << 17) == ppd.PPD_EINVAL
     assert call(T=0) == ppd.PPD_EINVAL and call(T=129, rows=200) == ppd.PPD_EINVAL and call(rows=3) == ppd.PPD_EINVAL
     assert call(_kvq(tail=dict(k=F, v=F, capacity=8)), T=9, rows=9) == ppd.PPD_ECAPACITY
     assert call(dt=7) == ppd.PPD_EINVAL and call(q=F + 4) == ppd.PPD_EINVAL
