@@ -175,7 +175,7 @@ __global__ __launch_bounds__(64 * W, 2) void kvq_store_kernel(KvqStore p) {
     for (int t = 0; t < 2; ++t) {
       const bf16_t *row = ks + (size_t)source(kvq_key_of(t, r)) * 128 + 8 * g;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) kx[t][w] = *(const u32x4 *)(row + 32 * w);
+      for (int w = 0; w < 4; ++w) kx[t][w] = __builtin_nontemporal_load((const u32x4 *)(row + 32 * w));
     }
     const bf16_t *col = vs + (size_t)r * p.scap;
     const bool some = 8 * g < b && 8 * g + 8 > a;  // the lane has a value to write
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_load_kernel(KvqLoad p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           o[e] = pack_bf16x2(held(s, z, (kw[t][w] >> kvq_shift(2 * e)) & 15u), held(s, z, (kw[t][w] >> kvq_shift(2 * e + 1)) & 15u));
-        *(u32x4 *)(row + 32 * w) = o;
+        __builtin_nontemporal_store(o, (u32x4 *)(row + 32 * w));
       }
     }
     bf16_t *at = vs + (size_t)r * p.dcap + p.dst0 + i0 + 8 * g;

@@ -120,10 +120,10 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
     const unsigned char *src = blocks + (size_t)(blk < b1 && blk < n4 ? blk : 0) * kQBytes;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      kw[t] = __builtin_nontemporal_load((const u32x4 *)(src + (t * 64 + lane) * 16));
-      vw[t] = __builtin_nontemporal_load((const u32x4 *)(src + kQV + (t * 64 + lane) * 16));
+      kw[t] = *(const u32x4 *)(src + (t * 64 + lane) * 16);
+      vw[t] = *(const u32x4 *)(src + kQV + (t * 64 + lane) * 16);
     }
-    pr = __builtin_nontemporal_load((const u32x2 *)(src + kQP + lane * 8));
+    pr = *(const u32x2 *)(src + kQP + lane * 8);
   };
   if (n4 > 0) request(b0 + par);
   __builtin_amdgcn_sched_barrier(0);
@@ -208,160 +208,160 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
   int blk = b0 + par;
   if (n_live > 0) {
     for (; blk < min(b1, n4); blk += PARS) {
-        const u32x4 kc[2] = {kw[0], kw[1]}, vc[2] = {vw[0], vw[1]};
-        const u32x2 pc = pr;
-        request(blk + PARS);
-        const bool valid = blk * kQB + (lane & 31) < L;
-        const float2 a0 = kvq_affine(pc[0]), a1 = kvq_affine(pc[1]);
-        par_s[wave][lane] = valid ? floatx4{a0.x, a0.y, a1.x, a1.y} : floatx4{0.f, 0.f, 0.f, 0.f};
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        float sv[NQ][8];
+      const u32x4 kc[2] = {kw[0], kw[1]}, vc[2] = {vw[0], vw[1]};
+      const u32x2 pc = pr;
+      request(blk + PARS);
+      const bool valid = blk * kQB + (lane & 31) < L;
+      const float2 a0 = kvq_affine(pc[0]), a1 = kvq_affine(pc[1]);
+      par_s[wave][lane] = valid ? floatx4{a0.x, a0.y, a1.x, a1.y} : floatx4{0.f, 0.f, 0.f, 0.f};
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      float sv[NQ][8];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          floatx4 acc[NQ][2];
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) acc[i][g] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int d = 0; d < 2; ++d) {
-              const bf16x8 x = as_bf16x8(kvq_expand(kc[t][2 * g + d], bits));
-#pragma unroll
-              for (int part = PARTS - 1; part >= 0; --part)
-#pragma unroll
-                for (int i = 0; i < NQ; ++i)
-                  acc[i][g] = mfma16x16x32(x, query(i, 2 * g + d, part), acc[i][g]);
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const floatx4 a = par_s[wave][8 * lg + 4 * t + e];
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-              float x = fmaf(a[0], acc[i][0][e], a[1] * rt[i].qs[0]);
-              x = fmaf(a[2], acc[i][1][e], fmaf(a[3], rt[i].qs[1], x));
-              sv[i][4 * t + e] = x;
-            }
-          }
-        }
-        if (blk * kQB + kQB > L) {  // the prefix ends in this block
-          const int vis = L - blk * kQB - 8 * lg;
-#pragma unroll
-          for (int i = 0; i < NQ; ++i)
-#pragma unroll
-            for (int u = 0; u < 8; ++u) sv[i][u] = u < vis ? sv[i][u] : -INFINITY;
-        }
-        float pv[NQ][8];
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) softmax_step(rt[i], sv[i], c, pv[i]);
-        __builtin_amdgcn_sched_barrier(0);
+      for (int t = 0; t < 2; ++t) {
+        floatx4 acc[NQ][2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          u32x4 ph[NQ], pl[NQ];
-          float ps[NQ][8];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float2 a = *((const float2 *)&par_s[wave][kQB + 8 * lg + u] + g);
+          for (int i = 0; i < NQ; ++i) acc[i][g] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-              ps[i][u] = pv[i][u] * a.x;
-              rt[i].pz[g] = fmaf(pv[i][u], a.y, rt[i].pz[g]);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < NQ; ++i) split8(ps[i], ph[i], pl[i]);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const bf16x8 x = as_bf16x8(kvq_expand(vc[g][w], bits));
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) rt[i].o[4 * g + w] = mfma16x16x32(x, as_bf16x8(pl[i]), rt[i].o[4 * g + w]);
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) rt[i].o[4 * g + w] = mfma16x16x32(x, as_bf16x8(ph[i]), rt[i].o[4 * g + w]);
-          }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the parameters' LDS is written next
-    }
-    for (; blk < b1; blk += PARS) {
-        // tree rows: keys and values straight from the tail, all requested at once
-        const int k0 = (blk - n4) * kQB;
-        const int j0 = k0 + 8 * lg, keep_n = max(0, min(8, T - j0));  // keys of the lane that exist
-        u32x4 kf[2][4], vf[8];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const bf16_t *row = tk + (size_t)min(k0 + kvq_key_of(t, lr), tcap - 1) * 128 + lg * 8;
-#pragma unroll
-          for (int ds = 0; ds < 4; ++ds) kf[t][ds] = *(const u32x4 *)(row + ds * 32);
-        }
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) vf[dt] = *(const u32x4 *)(tv + (size_t)(16 * dt + lr) * tcap + min(j0, tcap - 8));
-        __builtin_amdgcn_sched_barrier(0);
-        float sv[NQ][8];
-#pragma unroll
-        for (int i = 0; i < NQ; ++i)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
+          for (int d = 0; d < 2; ++d) {
+            const bf16x8 x = as_bf16x8(kvq_expand(kc[t][2 * g + d], bits));
 #pragma unroll
             for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
-              for (int ds = 0; ds < 4; ++ds) acc = mfma16x16x32(as_bf16x8(kf[t][ds]), query(i, ds, part), acc);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sv[i][4 * t + e] = acc[e];
+              for (int i = 0; i < NQ; ++i)
+                acc[i][g] = mfma16x16x32(x, query(i, 2 * g + d, part), acc[i][g]);
           }
-        __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const floatx4 a = par_s[wave][8 * lg + 4 * t + e];
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) {
+            float x = fmaf(a[0], acc[i][0][e], a[1] * rt[i].qs[0]);
+            x = fmaf(a[2], acc[i][1][e], fmaf(a[3], rt[i].qs[1], x));
+            sv[i][4 * t + e] = x;
+          }
+        }
+      }
+      if (blk * kQB + kQB > L) {  // the prefix ends in this block
+        const int vis = L - blk * kQB - 8 * lg;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+          for (int u = 0; u < 8; ++u) sv[i][u] = u < vis ? sv[i][u] : -INFINITY;
+      }
+      float pv[NQ][8];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) softmax_step(rt[i], sv[i], c, pv[i]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
         u32x4 ph[NQ], pl[NQ];
-        uint32_t seen[NQ];
+        float ps[NQ][8];
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-          const uint64_t win = j0 >= 128 ? 0ull : j0 >= 64 ? rt[i].mk1 >> (j0 - 64) : rt[i].mk0 >> j0;
-          seen[i] = (uint32_t)win & ((1u << keep_n) - 1u);
+        for (int u = 0; u < 8; ++u) {
+          const float2 a = *((const float2 *)&par_s[wave][kQB + 8 * lg + u] + g);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) sv[i][u] = (seen[i] >> u) & 1u ? sv[i][u] : -INFINITY;
-          float pv[8];
-          softmax_step(rt[i], sv[i], c, pv);
-          split8(pv, ph[i], pl[i]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        uint32_t end = 0;  // bit 15 of a half: an exponent of all ones
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            vf[dt][w] &= (2 * w < keep_n ? 0xffffu : 0u) | (2 * w + 1 < keep_n ? 0xffff0000u : 0u);
-            end |= (vf[dt][w] & 0x7fff7fffu) + 0x00800080u;
-          }
-        if (__ballot(end & 0x80008000u)) {
-          // infinities and NaN must not reach the rows that do not see them (0
-          // times them is NaN): they are taken out, and the rows that see one
-          // get NaN
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt) {
-            u32x4 odd;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              odd[w] = ((((vf[dt][w] & 0x7fff7fffu) + 0x00800080u) >> 15) & 0x00010001u) * 0x3f80u;  // 1.0 where one is
-              vf[dt][w] &= ~(odd[w] / 0x3f80u * 0xffffu);
-            }
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-              u32x4 on;
-#pragma unroll
-              for (int w = 0; w < 4; ++w)
-                on[w] = (seen[i] >> (2 * w) & 1u ? 0x3f80u : 0u) | (seen[i] >> (2 * w + 1) & 1u ? 0x3f800000u : 0u);
-              const floatx4 n = mfma16x16x32(as_bf16x8(odd), as_bf16x8(on), floatx4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-              for (int e = 0; e < 4; ++e) rt[i].o[dt][e] = n[e] > 0.f ? NAN : rt[i].o[dt][e];
-            }
+          for (int i = 0; i < NQ; ++i) {
+            ps[i][u] = pv[i][u] * a.x;
+            rt[i].pz[g] = fmaf(pv[i][u], a.y, rt[i].pz[g]);
           }
         }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) split8(ps[i], ph[i], pl[i]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const bf16x8 x = as_bf16x8(kvq_expand(vc[g][w], bits));
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) rt[i].o[4 * g + w] = mfma16x16x32(x, as_bf16x8(pl[i]), rt[i].o[4 * g + w]);
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) rt[i].o[4 * g + w] = mfma16x16x32(x, as_bf16x8(ph[i]), rt[i].o[4 * g + w]);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the parameters' LDS is written next
+    }
+    for (; blk < b1; blk += PARS) {
+      // tree rows: keys and values straight from the tail, all requested at once
+      const int k0 = (blk - n4) * kQB;
+      const int j0 = k0 + 8 * lg, keep_n = max(0, min(8, T - j0));  // keys of the lane that exist
+      u32x4 kf[2][4], vf[8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16_t *row = tk + (size_t)min(k0 + kvq_key_of(t, lr), tcap - 1) * 128 + lg * 8;
+#pragma unroll
+        for (int ds = 0; ds < 4; ++ds) kf[t][ds] = *(const u32x4 *)(row + ds * 32);
+      }
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) vf[dt] = *(const u32x4 *)(tv + (size_t)(16 * dt + lr) * tcap + min(j0, tcap - 8));
+      __builtin_amdgcn_sched_barrier(0);
+      float sv[NQ][8];
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+            for (int ds = 0; ds < 4; ++ds) acc = mfma16x16x32(as_bf16x8(kf[t][ds]), query(i, ds, part), acc);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sv[i][4 * t + e] = acc[e];
+        }
+      __builtin_amdgcn_sched_barrier(0);
+      u32x4 ph[NQ], pl[NQ];
+      uint32_t seen[NQ];
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const uint64_t win = j0 >= 128 ? 0ull : j0 >= 64 ? rt[i].mk1 >> (j0 - 64) : rt[i].mk0 >> j0;
+        seen[i] = (uint32_t)win & ((1u << keep_n) - 1u);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sv[i][u] = (seen[i] >> u) & 1u ? sv[i][u] : -INFINITY;
+        float pv[8];
+        softmax_step(rt[i], sv[i], c, pv);
+        split8(pv, ph[i], pl[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      uint32_t end = 0;  // bit 15 of a half: an exponent of all ones
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          vf[dt][w] &= (2 * w < keep_n ? 0xffffu : 0u) | (2 * w + 1 < keep_n ? 0xffff0000u : 0u);
+          end |= (vf[dt][w] & 0x7fff7fffu) + 0x00800080u;
+        }
+      if (__ballot(end & 0x80008000u)) {
+        // infinities and NaN must not reach the rows that do not see them (0
+        // times them is NaN): they are taken out, and the rows that see one
+        // get NaN
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
+          u32x4 odd;
 #pragma unroll
-          for (int i = 0; i < NQ; ++i) rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf[dt]), as_bf16x8(pl[i]), rt[i].o[dt]);
+          for (int w = 0; w < 4; ++w) {
+            odd[w] = ((((vf[dt][w] & 0x7fff7fffu) + 0x00800080u) >> 15) & 0x00010001u) * 0x3f80u;  // 1.0 where one is
+            vf[dt][w] &= ~(odd[w] / 0x3f80u * 0xffffu);
+          }
 #pragma unroll
-          for (int i = 0; i < NQ; ++i) rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf[dt]), as_bf16x8(ph[i]), rt[i].o[dt]);
+          for (int i = 0; i < NQ; ++i) {
+            u32x4 on;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              on[w] = (seen[i] >> (2 * w) & 1u ? 0x3f80u : 0u) | (seen[i] >> (2 * w + 1) & 1u ? 0x3f800000u : 0u);
+            const floatx4 n = mfma16x16x32(as_bf16x8(odd), as_bf16x8(on), floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rt[i].o[dt][e] = n[e] > 0.f ? NAN : rt[i].o[dt][e];
+          }
         }
+      }
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf[dt]), as_bf16x8(pl[i]), rt[i].o[dt]);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf[dt]), as_bf16x8(ph[i]), rt[i].o[dt]);
+      }
     }
   }
 
