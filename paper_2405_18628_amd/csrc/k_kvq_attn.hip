@@ -216,34 +216,35 @@ __global__ __launch_bounds__(NT, 1) void kvq_attention_kernel(KvqAttnLaunch p) {
       par_s[wave][lane] = valid ? floatx4{a0.x, a0.y, a1.x, a1.y} : floatx4{0.f, 0.f, 0.f, 0.f};
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       float sv[NQ][8];
+      floatx4 acc[NQ][2][2];  // [tile][group][key tile]: a query fragment is read once for both key tiles
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        floatx4 acc[NQ][2];
+      for (int g = 0; g < 2; ++g) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
+        for (int i = 0; i < NQ; ++i) acc[i][g][0] = acc[i][g][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < NQ; ++i) acc[i][g] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int d = 0; d < 2; ++d) {
+          const bf16x8 x0 = as_bf16x8(kvq_expand(kc[0][2 * g + d], bits)), x1 = as_bf16x8(kvq_expand(kc[1][2 * g + d], bits));
 #pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            const bf16x8 x = as_bf16x8(kvq_expand(kc[t][2 * g + d], bits));
+          for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
-            for (int part = PARTS - 1; part >= 0; --part)
-#pragma unroll
-              for (int i = 0; i < NQ; ++i)
-                acc[i][g] = mfma16x16x32(x, query(i, 2 * g + d, part), acc[i][g]);
-          }
+            for (int i = 0; i < NQ; ++i) {
+              const bf16x8 q = query(i, 2 * g + d, part);
+              acc[i][g][0] = mfma16x16x32(x0, q, acc[i][g][0]);
+              acc[i][g][1] = mfma16x16x32(x1, q, acc[i][g][1]);
+            }
         }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const floatx4 a = par_s[wave][8 * lg + 4 * t + e];
 #pragma unroll
           for (int i = 0; i < NQ; ++i) {
-            float x = fmaf(a[0], acc[i][0][e], a[1] * rt[i].qs[0]);
-            x = fmaf(a[2], acc[i][1][e], fmaf(a[3], rt[i].qs[1], x));
-            sv[i][4 * t + e] = x;
+            const float x = fmaf(a[0], acc[i][0][t][e], a[1] * rt[i].qs[0]);
+            sv[i][4 * t + e] = fmaf(a[2], acc[i][1][t][e], fmaf(a[3], rt[i].qs[1], x));
           }
         }
-      }
       if (blk * kQB + kQB > L) {  // the prefix ends in this block
         const int vis = L - blk * kQB - 8 * lg;
 #pragma unroll
