@@ -216,6 +216,19 @@ def _here(**tensors):
             raise ValueError(f"{name} is on device {t.get_device()}, the current device is {now}")
 
 
+def _tensors(dev, *checks):
+    """Every (tensor or None, dtype or None, name) is contiguous, of its type and
+    on device `dev`, which is the current one; _dev and _here name a fault.  One
+    pass of a few lookups a tensor, as _i32_ok: the short calls are bound by it."""
+    if dev >= 0 and _torch is None:
+        _stream(None)  # sets _torch
+    ok = dev >= 0 and _torch._C._cuda_getDevice() == dev
+    for t, dtype, name in checks:
+        if t is not None and not (ok and t.get_device() == dev and t.is_contiguous() and (dtype is None or t.dtype is dtype)):
+            _dev(t, dtype, name)
+            _here(**{name: t})
+
+
 # ---------------------------------------------------------------------------
 
 
@@ -305,6 +318,7 @@ class KVQCache:
         if tail is not None:
             self._check_rows(tail, blocks.shape[:2], "tail")
         self.blocks, self.tail = blocks, tail
+        self.device = blocks.get_device()
         self.n_layers, self.n_kv_heads = int(blocks.shape[0]), int(blocks.shape[1])
         self.capacity = int(blocks.shape[2]) * PPD_KVQ_BLOCK
         self.desc = ppd_kvq(_ptr(blocks), self.n_layers, self.n_kv_heads, self.capacity,
@@ -324,22 +338,25 @@ class KVQCache:
 
     @staticmethod
     def _check_rows(kv: KVCache, heads, name):
-        """kv is a bf16 cache of [layers][kv_heads] = heads, head_dim 128."""
+        """kv is a bf16 cache of [layers][kv_heads] = heads, head_dim 128 (looked at
+        once: a KVCache describes its tensors as they were given)."""
         import torch
-        want = (heads[0], heads[1])
+        want = (int(heads[0]), int(heads[1]))
+        if getattr(kv, "_rows", None) == want:
+            return
         if (tuple(kv.k.shape) != (*want, kv.capacity, 128) or tuple(kv.v.shape) != (*want, 128, kv.capacity) or
                 kv.k.dtype != torch.bfloat16 or kv.v.dtype != torch.bfloat16):
             raise ValueError(f"{name} must be a bf16 cache of {want[0]} layers, {want[1]} heads and 128 dims")
         if not (kv.k.is_contiguous() and kv.v.is_contiguous()):
             raise ValueError(f"{name} must be contiguous")
+        if kv.k.get_device() != kv.v.get_device():
+            raise ValueError(f"{name} lies on two devices")
+        kv._rows = want
 
-    def _on_device(self):
-        _dev(self.blocks, None, "blocks")
-        _here(blocks=self.blocks)
-        if self.tail is not None:
-            _dev(self.tail.k, None, "tail.k")
-            _dev(self.tail.v, None, "tail.v")
-            _here(tail=self.tail.k)
+    def _on_device(self, *checks):
+        """The cache, and the call's other tensors, are on the current device."""
+        tail = self.tail
+        _tensors(self.device, (self.blocks, None, "blocks"), (tail.k if tail is not None else None, None, "tail"), *checks)
 
 
 # ---------------------------------------------------------------------------
@@ -499,11 +516,8 @@ def ppd_kvq_bytes(n_layers: int, n_kv_heads: int, capacity: int) -> int:
 
 
 def _rows_of(kv: KVQCache, other: KVCache, name: str):
-    kv._on_device()
     KVQCache._check_rows(other, (kv.n_layers, kv.n_kv_heads), name)
-    _dev(other.k, None, name)
-    _dev(other.v, None, name)
-    _here(**{name: other.k})
+    kv._on_device((other.k, None, name))
 
 
 def ppd_kvq_quantize(kv: KVQCache, dst_pos: int, src: KVCache, src_pos: int, n: int, stream=None):
@@ -522,9 +536,9 @@ def ppd_kvq_dequantize(kv: KVQCache, src_pos: int, dst: KVCache, dst_pos: int, n
 
 def ppd_kvq_commit(kv: KVQCache, L: int, path, n_path, stream=None, path_len: Optional[int] = None):
     """Rows path[0], .., path[*n_path - 1] of kv.tail to positions L, L + 1, .. of kv."""
-    _i32(path=path, n_path=n_path)
-    kv._on_device()
-    n = int(path.numel()) if path_len is None else int(path_len)
+    import torch
+    kv._on_device((path, torch.int32, "path"), (n_path, torch.int32, "n_path"))
+    n = path.numel() if path_len is None else int(path_len)
     _check(lib().ppd_kvq_commit(C.byref(kv.desc), int(L), _ptr(path), n, _ptr(n_path), _stream(stream)))
 
 
@@ -532,69 +546,73 @@ def ppd_kvq_attention_workspace_bytes(n_heads: int, n_kv_heads: int, t_max: int)
     return _bytes(lib().ppd_kvq_attention_workspace_bytes(int(n_heads), int(n_kv_heads), int(t_max)))
 
 
-def _kvq_batch(kvs, *counts):
-    """The sequences' descriptions and host int32 arrays of one entry each."""
+def _dtypes():
+    t = _torch
+    if t is None:
+        import torch as t
+    return t.bfloat16, t.float32
+
+
+def _kvq_batch(kvs, counts, checks=()):
+    """The sequences' descriptions and host int32 arrays of one entry each; the
+    caches and the call's tensors (`checks`) are on the current device."""
     B = len(kvs)
     arrays = [_host_i32(a) for a in counts]
     for a in arrays:
         if a.shape != (B,):
             raise ValueError("kvs and the sequences' counts differ in length")
-    for kv in kvs:
-        kv._on_device()
-    return (B, (ppd_kvq * max(B, 1))(*[kv.desc for kv in kvs]), *arrays)
+    for i, kv in enumerate(kvs):
+        kv._on_device(*(() if i else checks))
+    descs = C.byref(kvs[0].desc) if B == 1 else (ppd_kvq * max(B, 1))(*[kv.desc for kv in kvs])
+    return (B, descs, *arrays)
 
 
 def ppd_kvq_attention(kvs: Sequence[KVQCache], layer: int, L: Sequence[int], T: Sequence[int], q, mask, out, ws,
                       lse=None, stream=None):
     """Tree attention of one layer: q, out bf16 [tokens][heads][128], lse float32
     [tokens][heads] (optional), mask int64 / uint64 [tokens][2]."""
-    import torch
-    _dev(q, torch.bfloat16, "q")
-    _dev(out, torch.bfloat16, "out")
-    _dev(lse, torch.float32, "lse")
-    _dev(mask, None, "mask")
-    _dev(ws, None, "ws")
-    B, descs, Ls, Ts = _kvq_batch(kvs, L, T)
-    _here(q=q, out=out, mask=mask, ws=ws, lse=lse)
-    n = int(Ts.sum())
-    if q.dim() != 3 or tuple(q.shape) != (n, q.shape[1], 128) or out.shape != q.shape:
+    bf16, f32 = _dtypes()
+    B, descs, Ls, Ts = _kvq_batch(kvs, (L, T), ((q, bf16, "q"), (out, bf16, "out"), (lse, f32, "lse"), (mask, None, "mask"),
+                                                (ws, None, "ws")))
+    n = int(Ts[0]) if B == 1 else int(Ts.sum())
+    shape = q.shape
+    if len(shape) != 3 or shape[0] != n or shape[2] != 128 or out.shape != shape:
         raise ValueError(f"q and out must be [{n}][heads][128]")
-    if lse is not None and tuple(lse.shape) != (n, q.shape[1]):
-        raise ValueError(f"lse must be [{n}][{q.shape[1]}]")
+    nh = shape[1]
+    if lse is not None and lse.shape != (n, nh):
+        raise ValueError(f"lse must be [{n}][{nh}]")
     if mask.numel() * mask.element_size() < 16 * n:
         raise ValueError(f"mask must be [{n}][2] words of 64 bits")
-    _check(lib().ppd_kvq_attention(int(q.shape[1]), B, C.cast(descs, C.c_void_p), int(layer), _np_ptr(Ls), _np_ptr(Ts),
-                                   _ptr(q), _ptr(mask), _ptr(out), _ptr(lse) or None, _ptr(ws),
-                                   ws.numel() * ws.element_size(), _stream(stream)))
+    _check(lib().ppd_kvq_attention(nh, B, descs, int(layer), _np_ptr(Ls), _np_ptr(Ts), _ptr(q), _ptr(mask), _ptr(out),
+                                   _ptr(lse) or None, _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def ppd_kvq_workspace_bytes(model: Model, t_max: int) -> int:
     return _bytes(lib().ppd_kvq_workspace_bytes(C.byref(model.desc), int(t_max)))
 
 
-def _trace(model, n, q_out, lse_out, **tensors):
-    import torch
+def _trace(model, n, q_out, lse_out):
     sh = model.shape
-    _here(q_out=q_out, lse_out=lse_out, **tensors)
-    _dev(q_out, torch.float32, "q_out")
-    _dev(lse_out, torch.float32, "lse_out")
     if q_out is not None and tuple(q_out.shape) != (sh.n_layers, n, sh.n_heads, 128):
         raise ValueError(f"q_out must be [{sh.n_layers}][{n}][{sh.n_heads}][128]")
     if lse_out is not None and tuple(lse_out.shape) != (sh.n_layers, n, sh.n_heads):
         raise ValueError(f"lse_out must be [{sh.n_layers}][{n}][{sh.n_heads}]")
 
 
+def _step_tensors(dev, ids, depth, mask, ws, logits, pred, q_out, lse_out):
+    import torch
+    i32, f32 = torch.int32, torch.float32
+    _tensors(dev, (ids, i32, "ids"), (depth, i32, "depth"), (pred, i32, "pred"), (mask, None, "mask"), (ws, None, "ws"),
+             (logits, f32, "logits"), (q_out, f32, "q_out"), (lse_out, f32, "lse_out"))
+
+
 def ppd_verify_batch_kvq(model: Model, kvs: Sequence[KVQCache], L: Sequence[int], pos: Sequence[int], T: Sequence[int],
                          ids, depth, mask, ws, logits, pred, q_out=None, lse_out=None, stream=None):
     """ppd_verify_batch on 4-bit caches; pos: the roots' positions."""
-    import torch
-    _i32(ids=ids, depth=depth, pred=pred)
-    _dev(mask, None, "mask")
-    _dev(ws, None, "ws")
-    _dev(logits, torch.float32, "logits")
-    B, descs, Ls, ps, Ts = _kvq_batch(kvs, L, pos, T)
-    _trace(model, int(Ts.sum()), q_out, lse_out, ids=ids, ws=ws, pred=pred, logits=logits)
-    _check(lib().ppd_verify_batch_kvq(C.byref(model.desc), B, C.cast(descs, C.c_void_p), _np_ptr(Ls), _np_ptr(ps),
+    B, descs, Ls, ps, Ts = _kvq_batch(kvs, (L, pos, T))
+    _step_tensors(kvs[0].device if B else -1, ids, depth, mask, ws, logits, pred, q_out, lse_out)
+    _trace(model, int(Ts.sum()), q_out, lse_out)
+    _check(lib().ppd_verify_batch_kvq(C.byref(model.desc), B, descs, _np_ptr(Ls), _np_ptr(ps),
                                       _np_ptr(Ts), _ptr(ids), _ptr(depth), _ptr(mask), _ptr(ws),
                                       ws.numel() * ws.element_size(), _ptr(logits) or None, _ptr(pred),
                                       _ptr(q_out) or None, _ptr(lse_out) or None, _stream(stream)))
@@ -603,13 +621,9 @@ def ppd_verify_batch_kvq(model: Model, kvs: Sequence[KVQCache], L: Sequence[int]
 def ppd_verify_step_kvq(model: Model, kv: KVQCache, L: int, pos: int, T: int, ids, depth, mask, ws, logits, pred,
                         q_out=None, lse_out=None, stream=None):
     """ppd_verify_step on a 4-bit cache; pos: the root's position."""
-    import torch
-    _i32(ids=ids, depth=depth, pred=pred)
-    _dev(mask, None, "mask")
-    _dev(ws, None, "ws")
-    _dev(logits, torch.float32, "logits")
     kv._on_device()
-    _trace(model, int(T), q_out, lse_out, ids=ids, ws=ws, pred=pred, logits=logits)
+    _step_tensors(kv.device, ids, depth, mask, ws, logits, pred, q_out, lse_out)
+    _trace(model, int(T), q_out, lse_out)
     _check(lib().ppd_verify_step_kvq(C.byref(model.desc), C.byref(kv.desc), int(L), int(pos), int(T), _ptr(ids),
                                      _ptr(depth), _ptr(mask), _ptr(ws), ws.numel() * ws.element_size(),
                                      _ptr(logits) or None, _ptr(pred), _ptr(q_out) or None, _ptr(lse_out) or None,
@@ -622,29 +636,26 @@ def ppd_kvq_score(kv: KVQCache, L: int, q, lse, path, n_path, score_in, score_ou
     q float32 or bf16 [layers][T][heads][128], lse float32 [layers][T][heads]:
     a tree's rows, which may be a slice [:, t0:t0 + T] of a batch's."""
     import torch
-    _i32(path=path, n_path=n_path)
-    kv._on_device()
-    if q.dim() != 4 or q.shape[0] != kv.n_layers or q.shape[3] != 128 or tuple(lse.shape) != tuple(q.shape[:3]):
+    i32, f32 = torch.int32, torch.float32
+    kv._on_device((path, i32, "path"), (n_path, i32, "n_path"), (score_in, f32, "score_in"), (score_out, f32, "score_out"))
+    layers, T, nh, d = q.shape if q.dim() == 4 else (0, 0, 0, 0)
+    if layers != kv.n_layers or d != 128 or lse.shape != q.shape[:3]:
         raise ValueError("q must be [layers][T][heads][128], lse [layers][T][heads]")
-    if q.dtype not in (torch.float32, torch.bfloat16) or lse.dtype != torch.float32:
+    if q.dtype not in (f32, torch.bfloat16) or lse.dtype is not f32:
         raise ValueError("q must be float32 or bfloat16, lse float32")
-    if q.is_cuda:
-        _here(q=q, lse=lse, path=path, n_path=n_path, score_in=score_in, score_out=score_out)
-    nh, T = int(q.shape[2]), int(q.shape[1])
-    rows = T if kv.n_layers == 1 else q.stride(0) // (nh * 128)
+    rows = T if layers == 1 else q.stride(0) // (nh * 128)
     for t, name, row in ((q, "q", nh * 128), (lse, "lse", nh)):
-        if not t.is_cuda:
-            raise ValueError(f"{name} must be a device tensor")
-        if not t[0].is_contiguous() or (kv.n_layers > 1 and t.stride(0) != rows * row):
+        if t.get_device() != kv.device:
+            raise ValueError(f"{name} must be a device tensor, on the cache's device")
+        if not t[0].is_contiguous() or (layers > 1 and t.stride(0) != rows * row):
             raise ValueError(f"{name} must be contiguous, or a slice of the rows of a contiguous tensor")
-    for t, name in ((score_in, "score_in"), (score_out, "score_out")):
-        _dev(t, torch.float32, name)
-        if t is not None and tuple(t.shape) != (kv.n_layers, kv.n_kv_heads, kv.capacity):
-            raise ValueError(f"{name} must be [{kv.n_layers}][{kv.n_kv_heads}][{kv.capacity}]")
-    n = int(path.numel()) if path_len is None else int(path_len)
-    _check(lib().ppd_kvq_score(C.byref(kv.desc), int(L), nh, T, _ptr(q), PPD_F32 if q.dtype == torch.float32 else PPD_BF16,
-                               _ptr(lse), int(rows), _ptr(path), n, _ptr(n_path), _ptr(score_in) or None,
-                               _ptr(score_out), _stream(stream)))
+    want = (layers, kv.n_kv_heads, kv.capacity)
+    if score_out.shape != want or (score_in is not None and score_in.shape != want):
+        raise ValueError(f"score_in and score_out must be [{want[0]}][{want[1]}][{want[2]}]")
+    n = path.numel() if path_len is None else int(path_len)
+    _check(lib().ppd_kvq_score(C.byref(kv.desc), int(L), nh, T, _ptr(q), PPD_F32 if q.dtype is f32 else PPD_BF16,
+                               _ptr(lse), rows, _ptr(path), n, _ptr(n_path), _ptr(score_in) or None, _ptr(score_out),
+                               _stream(stream)))
 
 
 def ppd_kvq_evict(src: KVQCache, dst: KVQCache, L: int, budget: int, n_sink: int, n_recent: int, score, score_out, kept,
@@ -652,15 +663,14 @@ def ppd_kvq_evict(src: KVQCache, dst: KVQCache, L: int, budget: int, n_sink: int
     """The kept positions of src moved up into dst (which may be src); returns
     how many stay, min(L, budget)."""
     import torch
-    src._on_device()
-    dst._on_device()
-    _i32(kept=kept)
+    f32 = torch.float32
+    src._on_device((score, f32, "score"), (score_out, f32, "score_out"), (kept, torch.int32, "kept"))
+    if dst is not src:
+        dst._on_device()
     for t, name, kv in ((score, "score", src), (score_out, "score_out", dst)):
-        _dev(t, torch.float32, name)
-        if tuple(t.shape) != (kv.n_layers, kv.n_kv_heads, kv.capacity):
+        if t.shape != (kv.n_layers, kv.n_kv_heads, kv.capacity):
             raise ValueError(f"{name} must be [{kv.n_layers}][{kv.n_kv_heads}][{kv.capacity}]")
-    _here(score=score, score_out=score_out, kept=kept)
-    if tuple(kept.shape) != (src.n_layers, src.n_kv_heads, budget):
+    if kept.shape != (src.n_layers, src.n_kv_heads, budget):
         raise ValueError(f"kept must be [{src.n_layers}][{src.n_kv_heads}][{budget}]")
     _check(lib().ppd_kvq_evict(C.byref(src.desc), C.byref(dst.desc), int(L), int(budget), int(n_sink), int(n_recent),
                                _ptr(score), _ptr(score_out), _ptr(kept), _stream(stream)))
@@ -677,15 +687,12 @@ def ppd_accept_sample(T: int, parent, ids, vocab: int, logits, temperature: floa
     target's probabilities with the draws u [T]; draft float32 [T][vocab] or
     None (children chosen without chance)."""
     import torch
-    _i32(parent=parent, ids=ids, path=path, n_path=n_path, next_tok=next_tok)
-    _dev(logits, torch.float32, "logits")
-    _dev(draft, torch.float32, "draft")
-    _dev(u, torch.float32, "u")
-    _dev(ws, None, "ws")
-    _here(parent=parent, ids=ids, logits=logits, draft=draft, u=u, path=path, n_path=n_path, next_tok=next_tok, ws=ws)
+    i32, f32 = torch.int32, torch.float32
+    _tensors(logits.get_device(), (logits, f32, "logits"), (parent, i32, "parent"), (ids, i32, "ids"), (u, f32, "u"),
+             (path, i32, "path"), (n_path, i32, "n_path"), (next_tok, i32, "next_tok"), (draft, f32, "draft"), (ws, None, "ws"))
     n = int(T)
-    for t, name, least in ((parent, "parent", n), (ids, "ids", n), (u, "u", n), (path, "path", n), (logits, "logits", n * vocab),
-                           (draft, "draft", n * vocab), (n_path, "n_path", 1), (next_tok, "next_tok", 1)):
+    for t, name, least in ((parent, "parent", n), (ids, "ids", n), (u, "u", n), (path, "path", n),
+                           (logits, "logits", n * vocab), (draft, "draft", n * vocab)):
         if t is not None and t.numel() < least:
             raise ValueError(f"{name} holds {t.numel()} elements, not {least}")
     _check(lib().ppd_accept_sample(int(T), _ptr(parent), _ptr(ids), int(vocab), _ptr(logits), float(temperature),

@@ -255,6 +255,9 @@ def test_python_refusals():
         ppd.KVQCache.empty(2, 4, 100, device="cpu")
     with pytest.raises(ValueError, match="device"):
         ppd.ppd_kvq_quantize(kv, 0, rows, 0, 4)
+    z = torch.zeros(4)
+    with pytest.raises(ValueError, match="device"):
+        ppd.ppd_accept_sample(1, z.int(), z.int(), 4, z, 1.0, None, z, z.int(), z.int(), z.int(), z)
     with pytest.raises(ValueError, match="device"):
         ppd.ppd_kvq_commit(kv, 0, torch.zeros(4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
 
