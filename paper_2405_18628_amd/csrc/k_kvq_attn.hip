@@ -14,6 +14,27 @@
 // over the 64-dim groups g, so a held value is never rounded.  A block's
 // parameters go through a wave's own LDS, from which every lane reads those of
 // its 8 keys.
+//
+// Work decomposition.  A workgroup takes a sequence, a kv head, up to 128 rows
+// and one of KS key splits; its eight waves are QW side by side over tiles, NQ
+// tiles each, and PARS over blocks, with no barrier in the loop: codes go
+// straight into the registers of the wave that multiplies them, the next block
+// requested while one is multiplied.  (NQ, QW, PARS) by the tiles of a kv head:
+// (1, 1, 8) for one, (2, 1, 8) for two, (2, 2, 4) up to four, (2, 4, 2) beyond:
+// two tiles share a block's expansion and parameters.  (64 nodes, 32768
+// positions: one tile a wave 112 us, two 99.)  Queries of two tiles a wave lie in
+// LDS, their registers hold the sums.  Splits: as many as fill the compute
+// units; a second launch adds them in order.
+//
+// Bounds.  A block takes 345 vector instructions for one tile (112 of them the
+// expansion), about 280 a tile for two, 24 or 32 matrix instructions: with small
+// trees that and the stream are near each other, with large ones the vector unit
+// is the bound.  us a launch, kernel alone (+ the launch that adds splits): 32
+// heads, 16 nodes, 32768 positions 33 (4.6 TB/s) + 4; 64 nodes, 2048 positions 17
+// + 4, of which 9 stay at 32 positions (tree rows, meeting of the waves, launch);
+// 16 heads, one node, 200 positions 6.  Not kept: four waves a SIMD (128
+// registers, nothing requested ahead; 16 nodes 46 us against 45 then), two blocks
+// ahead (40.0 against 38.6), loads past the caches (38.8 against 35.5).
 #include <algorithm>
 
 #include "ppd_kvq.h"
@@ -480,6 +501,11 @@ __global__ __launch_bounds__(NT) void kvq_merge_kernel(KvqAttnLaunch p) {
 // parts: three of a float32 (its last bits too, so that a weight is exact to
 // float32's own rounding of its exponent), one of a bfloat16.  A wave takes every
 // step-th block of a (layer, kv head), the next one requested ahead.
+//
+// Three nodes, 32 layers of 32 heads, 2048 positions 45 us (3.7 TB/s of a copy's
+// 4.8); five nodes, 32 heads on 8 kv heads, 8191 positions 56 (3.0 TB/s; two
+// tiles a key).  With queries in LDS instead, 24 KB read for every block and
+// tile, 62 and 89.
 struct ScoreRow {
   float qs0, qs1, lse2;  // sums of q over the groups, ln sum exp in log2
   int node;              // place on the path; rows that do not exist: -1
@@ -633,13 +659,18 @@ static void kvq_shape(int tiles, int *nq, int *qw) {
   *qw = tiles <= 2 ? 1 : tiles <= 4 ? 2 : 4;
 }
 
-int kvq_attn_max_splits(int nkv) { return std::max(1, std::min(64, 512 / nkv)); }
+// a workgroup a compute unit: the kernels' registers and LDS leave room for one
+constexpr long kSlots = 256;
+
+// (64: of one or two kv heads 128 splits were slower, what they save lost in
+// adding them: 2 kv heads, 65536 positions 27.3 us against 31.4, one head, 128 rows,
+// 8192 positions 21.8 against 24.7)
+int kvq_attn_max_splits(int nkv) { return (int)std::max<long>(1, std::min<long>(64, kSlots / nkv)); }
 
 size_t kvq_attn_part_bytes(int nh, int nkv, int T) {
   return (size_t)kvq_attn_max_splits(nkv) * T * nh * OROW * sizeof(float);
 }
 
-constexpr long kSlots = 256;
 void kvq_attn_plan(KvqAttnLaunch &a) {
   const int B = a.sb.B, G = a.nh / a.nkv, cap = kvq_attn_max_splits(a.nkv);
   a.max_splits = cap;

@@ -25,6 +25,14 @@
 // max(w - a - b, 0): one row of weights, one of probabilities and a number, but
 // a sum over the row for each rejection, the next depending on it.  A workgroup
 // settles a node alone: weights in registers, probabilities in LDS.
+//
+// Bounds: latency.  64 nodes, V = 32000, no drafts 4.7 + 9.7 us (parts and walk:
+// each a chain of two or three memory round trips and a few barriers); 25 nodes
+// with drafts, V = 32001, 29.5 + 5.0: 256 KB a compute unit and float64 sums and
+// exponentials of a row (with the library's exp 36 + 5).  One node, both launches:
+// V = 4000 15.5, 32000 22.8, 50257, whose rows do not fit the registers, 39.  A
+// cluster of workgroups a node would need waits between them for each
+// rejection.
 
 #include "ppd_sample.h"
 
