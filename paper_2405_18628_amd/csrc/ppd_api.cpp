@@ -846,8 +846,8 @@ ppd_status ppd_accept(int32_t T, const int32_t *parent, const int32_t *ids, cons
 }
 
 size_t ppd_accept_sample_workspace_bytes(int32_t T, int32_t vocab) {
-  if (T < 1 || T > PPD_T_MAX || vocab < 1) {
-    fail(PPD_EINVAL, "T must be in [1, %d], vocab positive", PPD_T_MAX);
+  if (T < 1 || T > PPD_T_MAX || vocab < 1 || vocab > (1 << 30)) {  // token indices past a row's end are 32-bit
+    fail(PPD_EINVAL, "T must be in [1, %d], vocab in [1, %d]", PPD_T_MAX, 1 << 30);
     return 0;
   }
   return sample_workspace_bytes(T, vocab);

@@ -335,7 +335,7 @@ def test_attention_offsets_past_32_bits():
 @pytest.mark.parametrize("layers,nh,nkv,L,T,path,n", [
     (2, 4, 4, 33, 8, [0, 2, 5], 3), (1, 6, 2, 0, 4, [0, 1], 2), (3, 8, 1, 100, 20, list(range(20)), 20),
     (2, 2, 2, 64, 8, [0, 1], 0), (1, 14, 2, 300, 128, list(range(0, 128, 2)), 64), (1, 2, 1, 31, 128, list(range(128)), 128),
-    (1, 2, 2, 95, 8, [0, 3, 4], 3), (2, 4, 2, 257, 3, [0], 9)])
+    (1, 2, 2, 95, 8, [0, 3, 4], 3), (2, 4, 2, 257, 3, [0], 9), (1, 12, 3, 4200, 16, [0, 2, 9, 15], 4)])
 def test_score(layers, nh, nkv, L, T, path, n, dtype):
     cap = (L + 1 + 31) // 32 * 32
     say(f"[score] nh={nh} nkv={nkv} L={L} cap={cap} T={T} n={n} {dtype}")
@@ -450,6 +450,32 @@ def test_evict(kind, L, budget, sink, recent, in_place):
             # positions behind the kept ones are as they were
             for got, rows in zip(R.load(after[l, h], dst.capacity), R.load(held[l, h], dst.capacity)):
                 assert np.array_equal(got[n:], rows[n:], equal_nan=True)
+
+
+@pytest.mark.parametrize("kind,in_place", [("few", True), ("plain", False), ("odd", True)])
+def test_evict_from_a_long_cache(kind, in_place):
+    """Scores read in several chunks, more heads than compute units."""
+    layers, heads, L, budget, cap = 100, 3, 9001, 5003, 9024
+    g = _gen(5)
+    one, _ = _cache(1, heads, L, cap, 1, 8, 1)
+    kv = ppd.KVQCache(one.blocks.expand(layers, -1, -1, -1).contiguous())
+    score = _scores(kind, (layers, heads, cap), g)
+    sc, before = score.cpu().numpy(), R.heads_of(one.blocks)[0]
+    dst = kv if in_place else ppd.KVQCache(torch.zeros((layers, heads, 157, 4608), dtype=torch.uint8, device="cuda"))
+    out = score if in_place else torch.zeros((layers, heads, dst.capacity), device="cuda")
+    kept = torch.zeros((layers, heads, budget), dtype=torch.int32, device="cuda")
+    say(f"[evict] long {kind} in_place={in_place}")
+    ppd.ppd_kvq_evict(kv, dst, L, budget, 3, 500, score, out, kept)
+    torch.cuda.synchronize()
+    got_kept, got_out = kept.cpu().numpy(), out.cpu().numpy()
+    for l in range(0, layers, 9):
+        after = R.heads_of(dst.blocks[l:l + 1])[0]
+        for h in range(heads):
+            at = R.keep(sc[l, h], L, budget, 3, 500)
+            assert got_kept[l, h].tolist() == at
+            assert np.array_equal(got_out[l, h, :budget], sc[l, h, at], equal_nan=True)
+            for x, y in zip(R.load(after[h], budget), R.load(before[h], L)):
+                assert np.array_equal(x, y[at])
 
 
 def test_evict_captured_after_score():

@@ -83,6 +83,20 @@ def test_accept_sample(T, V, style, with_draft):
 
 
 @pytest.mark.parametrize("with_draft", [False, True])
+def test_a_vocabulary_of_millions(with_draft):
+    """More parts of a row than the walk has threads, more chunks than one pass sums."""
+    rng = np.random.default_rng(8)
+    T, V = 3, 4300001
+    parent, ids = [-1, 0, 1], np.array([0, 4299999, 17], np.int32)
+    logits = rng.standard_normal((T, V)).astype(np.float32)
+    logits[0, 4299999] = logits[1, 17] = np.log(V) + 2.0
+    draft = np.full((T, V), 1 / V, np.float32) if with_draft else None
+    for u0 in (0.001, 0.5, 0.9999):
+        for u1 in (0.0, 0.99):
+            _check(parent, ids, V, logits, 1.0, draft, np.array([u0, u1, u1], np.float32))
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
 def test_rows_with_infinities_and_nan(with_draft):
     rng = np.random.default_rng(3)
     T, V = 6, 50

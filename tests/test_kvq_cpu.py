@@ -38,7 +38,7 @@ def test_sizes():
     for bad in ((0, 1, 1), (4, 3, 1), (4, 4, 0), (4, 4, 129), (4, 0, 4), (1 << 17, 1, 4)):
         assert L.ppd_kvq_attention_workspace_bytes(*bad) == 0 and ppd.ppd_last_error()
     assert ppd.ppd_accept_sample_workspace_bytes(64, 32000) > 0
-    for bad in ((0, 10), (129, 10), (4, 0)):
+    for bad in ((0, 10), (129, 10), (4, 0), (4, (1 << 30) + 1)):
         assert L.ppd_accept_sample_workspace_bytes(*bad) == 0 and ppd.ppd_last_error()
 
 
