@@ -673,7 +673,6 @@ size_t kvq_attn_part_bytes(int nh, int nkv, int T) {
 
 void kvq_attn_plan(KvqAttnLaunch &a) {
   const int B = a.sb.B, G = a.nh / a.nkv, cap = kvq_attn_max_splits(a.nkv);
-  a.max_splits = cap;
   a.tiles = 1;
   for (int j = 0; j < B; ++j) a.tiles = std::max(a.tiles, ((a.sb.t0[j + 1] - a.sb.t0[j]) * G + 15) / 16);
   int nq, qw;

@@ -89,7 +89,7 @@ struct KvqAttnLaunch {
   float *lse;           // [T][nh] or null
   float *q_out;         // planes: float32 rows [T][nh][128], or null
   float *part;          // [splits][T][nh][PPD_ATTN_OROW]
-  int nh, nkv, max_splits;
+  int nh, nkv;
   int tiles;            // most 16-row tiles of a kv head's rows (tree rows x heads that share it)
   KvqSeqs sb;
   // sequence s: slots slot0[s] + ((kv head x row groups + row group) x splits[s] + split), a split
