@@ -502,18 +502,19 @@ __global__ __launch_bounds__(NT) void kvq_merge_kernel(KvqAttnLaunch p) {
 // float32's own rounding of its exponent), one of a bfloat16.  A wave takes every
 // step-th block of a (layer, kv head), the next one requested ahead.
 //
-// Three nodes, 32 layers of 32 heads, 2048 positions 45 us (3.7 TB/s of a copy's
-// 4.8); five nodes, 32 heads on 8 kv heads, 8191 positions 56 (3.0 TB/s; two
-// tiles a key).  With queries in LDS instead, 24 KB read for every block and
-// tile, 62 and 89.
+// Three nodes, 32 layers of 32 heads, 2048 positions 42 us (3.9 TB/s of a copy's
+// 4.8); five nodes, 32 heads on 8 kv heads, 8191 positions 49 (3.4 TB/s; two
+// tiles a key).  Bounds on registers: a tile of queries fits four waves a SIMD
+// (45 us with two; what spills lies before the loop over blocks), two tiles
+// three with bfloat16 queries (56 with two), two with float32's three parts.
+// With queries in LDS instead, 24 KB read for every block and tile, 62 and 89.
 struct ScoreRow {
   float qs0, qs1, lse2;  // sums of q over the groups, ln sum exp in log2
-  int node;              // place on the path; rows that do not exist: -1
 };
 constexpr int kScoreWaves = 4;
 
 template <int TILES, int PARTS>
-__global__ __launch_bounds__(64 * kScoreWaves, 2) void kvq_score_kernel(KvqScoreLaunch p) {
+__global__ __launch_bounds__(64 * kScoreWaves, TILES > 1 ? PARTS > 1 ? 2 : 3 : 4) void kvq_score_kernel(KvqScoreLaunch p) {
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int lh = blockIdx.x / p.runs, layer = lh / p.nkv, kvh = lh % p.nkv;
   const int first = (blockIdx.x % p.runs) * kScoreWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -589,15 +590,15 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void kvq_score_kernel(KvqScore
       const float l2 = lse * 1.4426950408889634f;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        row[m][e] = ScoreRow{__shfl(sum[0], 4 * lg + e, 64), __shfl(sum[1], 4 * lg + e, 64), __shfl(l2, 4 * lg + e, 64),
-                             __shfl(live ? i : -1, 4 * lg + e, 64)};
+        row[m][e] = ScoreRow{__shfl(sum[0], 4 * lg + e, 64), __shfl(sum[1], 4 * lg + e, 64), __shfl(l2, 4 * lg + e, 64)};
     }
-    // weights of this lane's key: a its affine pairs, only rows from `from` on
+    // weights of this lane's key: a its affine pairs, only rows r0 + from .. R - 1
+    const int rows = R - r0;
     auto weigh = [&](const u32x4 (&b)[4], float4 a, int from) {
       float w = 0.f;
 #pragma unroll
       for (int m = 0; m < TILES; ++m) {
-        if (m > 0 && r0 + 16 * m >= R) break;
+        if (m > 0 && 16 * m >= rows) break;
         floatx4 acc[2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -612,7 +613,8 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void kvq_score_kernel(KvqScore
         for (int e = 0; e < 4; ++e) {
           const ScoreRow &x = row[m][e];
           const float s = fmaf(a.x, acc[0][e], a.y * x.qs0) + fmaf(a.z, acc[1][e], a.w * x.qs1);
-          w += x.node >= from ? __builtin_amdgcn_exp2f(fmaf(s, c, -x.lse2)) : 0.f;
+          const int r = 16 * m + 4 * lg + e;
+          w += r >= from && r < rows ? __builtin_amdgcn_exp2f(fmaf(s, c, -x.lse2)) : 0.f;
         }
       }
       return quad_sum(w);
@@ -645,7 +647,7 @@ __global__ __launch_bounds__(64 * kScoreWaves, 2) void kvq_score_kernel(KvqScore
         u32x4 b[4];
 #pragma unroll
         for (int ds = 0; ds < 4; ++ds) b[ds] = *(const u32x4 *)(tk + (size_t)node * 128 + ds * 32 + lg * 8);
-        const float w = weigh(b, float4{1.f, 0.f, 1.f, 0.f}, k);
+        const float w = weigh(b, float4{1.f, 0.f, 1.f, 0.f}, k * G - r0);  // the nodes from its own on
         if (lg == 0 && k < n) out[p.L + k] = (more ? out[p.L + k] : 0.f) + w;
       }
   }
@@ -727,13 +729,14 @@ hipError_t launch_kvq_attn(const KvqAttnLaunch &a, hipStream_t s) {
 }
 
 hipError_t launch_kvq_score(KvqScoreLaunch p, hipStream_t s) {
-  // Enough workgroups to fill the chip twice, eight blocks a wave or more where
+  // As many workgroups as are resident at once, eight blocks a wave or more where
   // there are.  How many rows there are is only known on the device: an accepted
   // path is a few nodes, so a tile holds those of one or two heads, two tiles
   // those of four.
   const int heads = p.layers * p.nkv, nblk = (p.L + p.path_len + 2 * kQB - 2) / kQB;
-  p.runs = std::max(1, std::min((1024 + heads - 1) / heads, nblk / (8 * kScoreWaves)));
   const bool two = p.nh / p.nkv > 2;
+  const int resident = 256 * (!two ? 4 : p.q_bf16 ? 3 : 2);
+  p.runs = std::max(1, std::min(resident / heads, nblk / (8 * kScoreWaves)));
   auto kernel = p.q_bf16 ? (two ? kvq_score_kernel<2, 1> : kvq_score_kernel<1, 1>)
                          : (two ? kvq_score_kernel<2, 3> : kvq_score_kernel<1, 3>);
   hipLaunchKernelGGL(kernel, dim3(heads * p.runs), dim3(64 * kScoreWaves), 0, s, p);
