@@ -515,8 +515,8 @@ ppd_status ppd_kvq_evict(const ppd_kvq *src, const ppd_kvq *dst, int32_t L, int3
  *   draft         device float32 [T][vocab], or NULL; entries that are negative
  *                 or NaN count as 0
  *   u             device float32[T], uniform in [0, 1): u[c] decides node c,
- *                 u[0] the bonus token (1 or more: the last token that has
- *                 weight; a NaN accepts nothing)
+ *                 u[0] the bonus token (1 or more, or NaN: the last token that
+ *                 has weight); a child's NaN does not accept it
  *   path, n_path, next_tok   as ppd_accept gives them; path[n_path .. T) = -1
  *   ws            device workspace, 16-byte aligned, of
  *                 ppd_accept_sample_workspace_bytes(T, vocab)

@@ -122,6 +122,11 @@ __device__ __forceinline__ double block_before64(double v, double *wave_s, doubl
   return before + (x - v);
 }
 
+// What the running sum has to pass.  A draw of 1 or more takes the last token
+// that has weight: nothing passes its goal (the whole and the running sum are
+// rounded apart, so the whole may be passed before the last token).
+__device__ __forceinline__ double goal_of(float u, double whole) { return u < 1.f ? (double)u * whole : INFINITY; }
+
 // The first token of a thread's four whose running sum passes the goal goes to
 // *pick (the least), the last that has weight to *last (the greatest); runs rise
 // with the thread, so a wave's first and last lane stand for it (an LDS atomic
@@ -332,7 +337,7 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
     // weight), then the token: a part's tokens in runs of four a thread
     const SamplePart *part = p.part + (size_t)a * parts;
     const Weights weight(m, p.temperature, table);
-    const double goal = (double)u_s[0] * rest;
+    const double goal = goal_of(u_s[0], rest);
     const int per = (parts + kThreads - 1) / kThreads;
     auto part_sum = [&](int s) {
       const SamplePart x = part[min(s, parts - 1)];
@@ -379,10 +384,10 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
   } else if (m > -INFINITY) {
     // all weight lies on the children's tokens, of which none was accepted: the
     // bonus token is drawn from them
-    double goal = 0., run = 0.;
+    double whole = 0., run = 0.;
     for (int j = a + 1; j < T; ++j)
-      if (up_s[j] == a) goal += w_s[j];
-    goal *= (double)u_s[0];
+      if (up_s[j] == a) whole += w_s[j];
+    const double goal = goal_of(u_s[0], whole);
     if (child && up_s[tid] == a && w_s[tid] > 0.) {
       for (int j = a + 1; j < T; ++j)
         if (up_s[j] == a && id_s[j] <= id_s[tid]) run += w_s[j];
@@ -553,7 +558,7 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
       // the chunk that the draw falls into, then the token (a draw of 1 or
       // more: the last token that has weight).  The chunks' sums come from one
       // pass, kChunkSums of them at a time.
-      const double goal = (double)p.u[0] * Z;
+      const double goal = goal_of(p.u[0], Z);
       const int lane = tid & 63, wave = tid >> 6;
       double base = 0.;
       for (int k0 = 0; k0 < n_chunks; k0 += kChunkSums) {
@@ -583,7 +588,7 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
         if (tid < nk) before_s[tid] = before;
         __syncthreads();
         if (first_s != INT_MAX || k0 + kChunkSums >= n_chunks) {
-          const int k = first_s != INT_MAX ? first_s : max(0, final_s);  // final_s < k0: a row of more chunks
+          const int k = first_s != INT_MAX ? first_s : max(0, final_s);
           double r[kRun];
           if constexpr (RES) {
 #pragma unroll
@@ -592,6 +597,7 @@ __global__ __launch_bounds__(kThreads) void sample_node_kernel(SampleLaunch p) {
           } else {
             residual4(k, C, r);
           }
+          // (no first_s: a draw of 1 or more, whose goal nothing passes; then k may lie before k0)
           const double at = (k >= k0 ? before_s[k - k0] : base) + block_before64((r[0] + r[1]) + (r[2] + r[3]), wave_s, &all);
           note_pick(r, at, goal, k * kChunk + kRun * tid, &pick_s, &last_s);
           break;
