@@ -509,7 +509,7 @@ ppd_status ppd_kvq_evict(const ppd_kvq *src, const ppd_kvq *dst, int32_t L, int3
  * 1 and a rejected token leaves r.  Where no child is accepted the walk ends
  * with the bonus token, the smallest i with r_0 + .. + r_i > u[0] (r_0 + r_1 +
  * ..); from w where nothing is left of r.  Weights and sums are float64: of V
- * tokens one's border is always near.
+ * tokens one's border is always near; a weight under e^-700 counts as 0.
  *   parent, ids   device int32[T], this step's tree
  *   logits        device float32 [T][vocab]; temperature > 0
  *   draft         device float32 [T][vocab], or NULL; entries that are negative

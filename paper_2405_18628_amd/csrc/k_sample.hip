@@ -100,6 +100,17 @@ __device__ __forceinline__ float block_max(float v, float *wave_s) {
   for (int w = 0; w < N / 64; ++w) v = fmaxf(v, wave_s[w]);
   return v;
 }
+// of two numbers at once
+template <int N>
+__device__ __forceinline__ void block_max(float &a, float &b, float2 *wave_s) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor(a, o, 64)), b = fmaxf(b, __shfl_xor(b, o, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) wave_s[threadIdx.x >> 6] = float2{a, b};
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < N / 64; ++w) a = fmaxf(a, wave_s[w].x), b = fmaxf(b, wave_s[w].y);
+}
 // sum over the threads before this one; the whole in *all
 __device__ __forceinline__ double block_before64(double v, double *wave_s, double *all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -178,12 +189,12 @@ __device__ __forceinline__ void fill_table(double *table) {
 // ---------------------------------------------------------------------------
 // without draft probabilities
 
-// Workgroup (node, part): the part's largest logit and the sum of its weights
-// against it, the children's tokens left out.
+// Workgroup (node, part): the part's largest logit and, the children's tokens
+// left out, the largest one and the sum of weights against it.
 __global__ __launch_bounds__(kPartThreads) void sample_part_kernel(SampleLaunch p) {
   constexpr int E = kPart / kPartThreads;
   __shared__ double wave_s[kPartThreads / 64];
-  __shared__ float max_s[kPartThreads / 64];
+  __shared__ float2 max_s[kPartThreads / 64];
   __shared__ double table[64];
   __shared__ int tok_s[PPD_T_MAX];
   __shared__ int n_s, nan_s;
@@ -212,7 +223,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_part_kernel(SampleLaunch 
     m = fmaxf(m, x[e]);
   }
   if (nan) nan_s = 1;
-  m = block_max<kPartThreads>(m, max_s);
+  __syncthreads();
   const int n = n_s;
   for (int c = 0; c < n; ++c) {
     const int at = tok_s[c] - i0;
@@ -220,14 +231,20 @@ __global__ __launch_bounds__(kPartThreads) void sample_part_kernel(SampleLaunch 
     for (int e = 0; e < E; ++e)
       if (at == tid + kPartThreads * e) x[e] = NAN;  // no weight
   }
+  // the sum is taken against the largest logit of what it sums, so that a part
+  // has weight in the row exactly where its largest token has
+  float top = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
+  block_max<kPartThreads>(m, top, max_s);
   double s = 0.;
-  if (m > -INFINITY) {
-    const Weights weight(m, p.temperature, table);
+  if (top > -INFINITY) {
+    const Weights weight(top, p.temperature, table);
 #pragma unroll
     for (int e = 0; e < E; ++e) s += weight(x[e]);
   }
   s = block_sum64<kPartThreads>(s, wave_s);
-  if (tid == 0) p.part[(size_t)a * gridDim.x + blockIdx.x] = SamplePart{m, (uint32_t)nan_s, s};
+  if (tid == 0) p.part[(size_t)a * gridDim.x + blockIdx.x] = SamplePart{s, top, m, (uint32_t)nan_s, 0u};
 }
 
 // One workgroup: all nodes decided, the walk, the bonus token.
@@ -280,7 +297,7 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
     double rest = 0.;
     for (int s = tid & 7; on && s < parts; s += 8) {
       const double r = part[s].rest;
-      if (r > 0.) rest += r * weight(part[s].m);
+      if (r > 0.) rest += r * weight(part[s].top);
     }
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) rest += __shfl_xor(rest, o, 64);
@@ -341,7 +358,7 @@ __global__ __launch_bounds__(kThreads) void sample_walk_kernel(SampleLaunch p, i
     const int per = (parts + kThreads - 1) / kThreads;
     auto part_sum = [&](int s) {
       const SamplePart x = part[min(s, parts - 1)];
-      return s < parts && x.rest > 0. ? x.rest * weight(x.m) : 0.;
+      return s < parts && x.rest > 0. ? x.rest * weight(x.top) : 0.;
     };
     double sum = 0., all;
     for (int s = 0; s < per; ++s) sum += part_sum(tid * per + s);

@@ -4,9 +4,11 @@
 #include "ppd_internal.h"
 
 struct SamplePart {
+  double rest;   // sum of exp((l - top) / temperature) without the node's drafted tokens: 0 or at least 1
+  float top;     // the largest logit of those
   float m;       // the largest logit of the part (NaN left out)
   uint32_t nan;  // it holds a NaN
-  double rest;   // sum of exp((l - m) / temperature) without the node's drafted tokens
+  uint32_t pad;
 };
 
 struct SampleNode {

@@ -1,5 +1,6 @@
 """Sampled acceptance where a draw reaches the end of the weights: u[0] of 1 or
-more is the last token that has weight, whatever the rounding of the sums."""
+more is the last token that has weight, whatever the rounding of the sums, and
+a token without weight is never the bonus."""
 import numpy as np
 import pytest
 
@@ -45,3 +46,38 @@ def test_a_draw_of_one_is_the_last_token_with_weight(V, end, with_draft):
         u = np.array([np.nextafter(np.float32(1), np.float32(0)), 0.99], np.float32)
         want = R.accept_sample([-1, 0], [0, 3], V, logits, 1.0, draft, u)
         assert _call([-1, 0], [0, 3], V, logits, 1.0, draft, u)[:2] == want[:2]
+
+
+def _far(V, *at):
+    x = np.full((3, V), -np.inf, np.float32)
+    for token, logit in at:
+        x[:, token] = logit
+    return x
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("V", [4300, 9000, 140000])
+def test_weights_below_the_smallest_count_as_none(V, with_draft):
+    """A weight under e^-700 of the largest is 0.  The faint token shares its
+    part of the row with a rejected child of weight e^-600, against which it
+    alone would have some."""
+    logits = _far(V, (5, 0.0), (4100, -600.0), (V - 50, -701.0))
+    draft = None
+    if with_draft:
+        draft = np.zeros((3, V), np.float32)
+        draft[:, 4100] = 0.5
+    for u0 in (0.0, 0.5, 1.0, 7.0, float("nan")):
+        got = _call([-1, 0], [0, 4100], V, logits[:2], 1.0, draft if draft is None else draft[:2],
+                    np.array([u0, 0.9], np.float32))
+        assert got == ([0], 5, 0), u0
+
+
+@pytest.mark.parametrize("V", [4300, 9000])
+def test_only_weights_below_the_smallest_are_left(V):
+    """Every token that has weight is a child's, and no child is accepted: the
+    bonus token is drawn from the row."""
+    logits = _far(V, (7, 0.0), (4100, -600.0), (V - 50, -701.0))
+    nan = float("nan")
+    for u0, bonus in ((0.0, 7), (0.99, 7), (1.0, 4100)):
+        got = _call([-1, 0, 0], [0, 7, 4100], V, logits, 1.0, None, np.array([u0, nan, nan], np.float32))
+        assert got == ([0], bonus, 0), u0
