@@ -414,6 +414,11 @@ ppd_status ppd_kvq_commit(const ppd_kvq *kv, int32_t L, const int32_t *path, int
  * value product with about 16 significant bits.  A row that sees nothing (L =
  * 0 and an empty mask) gets zeros, and minus infinity in lse; one that sees a
  * NaN or an infinity gets NaN where these enter, and no other row does.
+ * Limits: cached and tree rows of up to 2^90 in magnitude, and products of a
+ * query's and a key's elements of up to 2^116, keep every sum finite (also in
+ * ppd_kvq_score).  The sums hold a code's offset and up to 2^8 times a
+ * probability, so finite rows past that can give infinities or NaN to the rows
+ * that see them; storing them and reading them back is not affected.
  *   q     device bfloat16 [T[0] + .. ][n_heads][128], 16-byte aligned
  *   out   device bfloat16, the same shape and alignment (not q itself)
  *   lse   device float32 [T[0] + ..][n_heads]: ln sum exp of the row's scores,

@@ -26,7 +26,11 @@ __device__ __forceinline__ u32x4 kvq_expand(uint32_t w, const KvqBits &k) {
   return u32x4{((w << 3) & k.mask) | k.magic, ((w >> 1) & k.mask) | k.magic, ((w >> 5) & k.mask) | k.magic,
                ((w >> 9) & k.mask) | k.magic};
 }
-// a (scale, zero) pair as (2 s, z - 16 s)
+// a (scale, zero) pair as (2 s, z - 16 s).  With rows of magnitude M both times
+// x or 1 stay below 4.2 M and 3.2 M (s < 2.01 M / 15), so with 2^24 keys and
+// probabilities of up to 2^8 a sum stays below 2^35 M, a score's below 2^10 M |q|:
+// M = 2^90 and M |q| = 2^116 are the documented limits (float32 ends at 2^128;
+// z - 16 s itself from M = 2^126 on).
 __device__ __forceinline__ float2 kvq_affine(uint32_t sz) {
   const float s = __uint_as_float(sz << 16), z = __uint_as_float(sz & 0xffff0000u);
   return float2{2.f * s, fmaf(-16.f, s, z)};
