@@ -1,5 +1,6 @@
-"""More of the 4-bit cache on the GPU: magnitudes up to the documented limit.
-The bounds are those of test_gpu_kvq."""
+"""More of the 4-bit cache on the GPU: magnitudes up to the documented limit,
+and captured attention with eager attention between its replays.  The bounds
+are those of test_gpu_kvq."""
 import numpy as np
 import pytest
 import torch
@@ -52,3 +53,33 @@ def test_attention_and_weights_at_far_magnitudes(T, L, power):
         assert (np.abs(lse[:, a].cpu().numpy() - rl) <= ds + 2.0 ** -22 * (1 + np.abs(rl))).all()
     # the root's weights add up to the heads of a kv head
     assert float((score[..., :L + 1].double().sum(-1) / (nh // nkv) - 1).abs().max()) < 5e-5
+
+
+def test_attention_captured_between_eager_calls():
+    """Two graphs with a workspace each; between the replays eager calls of
+    other shapes, on a workspace of their own: all give what they gave alone."""
+    cases = []
+    for seed, (T, L) in enumerate(((7, 900), (40, 3000), (100, 5000), (3, 20))):
+        kv, _ = _cache(1, 4, L, (L + 31) // 32 * 32, T, (T + 7) // 8 * 8, seed)
+        m = torch.from_numpy(_tree_mask(T, np.random.default_rng(seed), "tree").view(np.int64)).cuda()
+        q = _bf16((T, 8, 128), _gen(seed))
+        out = torch.empty_like(q)
+        ws = torch.empty(ppd.ppd_kvq_attention_workspace_bytes(8, 4, T), dtype=torch.uint8, device="cuda")
+        ppd.ppd_workspace_init(ws)
+        run = lambda kv=kv, m=m, q=q, out=out, ws=ws, T=T, L=L: ppd.ppd_kvq_attention([kv], 0, [L], [T], q, m, out, ws)
+        run()
+        torch.cuda.synchronize()
+        cases.append([run, out, out.clone()])
+    for c in cases[:2]:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c[0]()
+        c.append(graph)
+    for _ in range(4):
+        for graph_case, eager_case in zip(cases[:2], cases[2:]):
+            graph_case[1].zero_()
+            eager_case[1].zero_()
+            graph_case[3].replay()
+            eager_case[0]()
+            torch.cuda.synchronize()
+            assert torch.equal(graph_case[1], graph_case[2]) and torch.equal(eager_case[1], eager_case[2])
