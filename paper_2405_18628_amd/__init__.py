@@ -534,11 +534,21 @@ def ppd_kvq_dequantize(kv: KVQCache, src_pos: int, dst: KVCache, dst_pos: int, n
                                     _stream(stream)))
 
 
+def _path_len(path, path_len) -> int:
+    """Entries of the path that the kernels may read, at most the tensor's."""
+    n = path.numel()
+    if path_len is None:
+        return n
+    if path_len > n:
+        raise ValueError(f"path holds {n} entries, not {path_len}")
+    return int(path_len)
+
+
 def ppd_kvq_commit(kv: KVQCache, L: int, path, n_path, stream=None, path_len: Optional[int] = None):
     """Rows path[0], .., path[*n_path - 1] of kv.tail to positions L, L + 1, .. of kv."""
     import torch
+    n = _path_len(path, path_len)
     kv._on_device((path, torch.int32, "path"), (n_path, torch.int32, "n_path"))
-    n = path.numel() if path_len is None else int(path_len)
     _check(lib().ppd_kvq_commit(C.byref(kv.desc), int(L), _ptr(path), n, _ptr(n_path), _stream(stream)))
 
 
@@ -637,6 +647,7 @@ def ppd_kvq_score(kv: KVQCache, L: int, q, lse, path, n_path, score_in, score_ou
     a tree's rows, which may be a slice [:, t0:t0 + T] of a batch's."""
     import torch
     i32, f32 = torch.int32, torch.float32
+    n = _path_len(path, path_len)
     kv._on_device((path, i32, "path"), (n_path, i32, "n_path"), (score_in, f32, "score_in"), (score_out, f32, "score_out"))
     layers, T, nh, d = q.shape if q.dim() == 4 else (0, 0, 0, 0)
     if layers != kv.n_layers or d != 128 or lse.shape != q.shape[:3]:
@@ -652,7 +663,6 @@ def ppd_kvq_score(kv: KVQCache, L: int, q, lse, path, n_path, score_in, score_ou
     want = (layers, kv.n_kv_heads, kv.capacity)
     if score_out.shape != want or (score_in is not None and score_in.shape != want):
         raise ValueError(f"score_in and score_out must be [{want[0]}][{want[1]}][{want[2]}]")
-    n = path.numel() if path_len is None else int(path_len)
     _check(lib().ppd_kvq_score(C.byref(kv.desc), int(L), nh, T, _ptr(q), PPD_F32 if q.dtype is f32 else PPD_BF16,
                                _ptr(lse), rows, _ptr(path), n, _ptr(n_path), _ptr(score_in) or None, _ptr(score_out),
                                _stream(stream)))

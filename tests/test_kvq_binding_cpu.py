@@ -57,3 +57,18 @@ def test_calls_refuse_another_device(monkeypatch):
     with pytest.raises(ValueError, match="u is on device 0"):
         ppd.ppd_accept_sample(4, On(1), On(1), 1, On(1, torch.float32), 1.0, None, On(0, torch.float32), On(1), On(1), On(1),
                               On(1))
+
+
+def test_a_count_past_the_path_is_refused():
+    """path_len entries are read on the device: more than the tensor holds would
+    be read past its end."""
+    kv, path, n = _cache(), torch.zeros(4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    q, lse = torch.zeros((2, 4, 8, 128)), torch.zeros((2, 4, 8))
+    score = torch.zeros((2, 4, 256))
+    with pytest.raises(ValueError, match="path holds 4 entries, not 5"):
+        ppd.ppd_kvq_commit(kv, 0, path, n, path_len=5)
+    with pytest.raises(ValueError, match="path holds 4 entries, not 128"):
+        ppd.ppd_kvq_score(kv, 0, q, lse, path, n, None, score, path_len=128)
+    for ok in (None, 1, 4):  # on to the next check
+        with pytest.raises(ValueError, match="device"):
+            ppd.ppd_kvq_commit(kv, 0, path, n, path_len=ok)
