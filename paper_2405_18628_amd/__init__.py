@@ -351,6 +351,9 @@ class KVQCache:
             raise ValueError(f"{name} must be contiguous")
         if kv.k.get_device() != kv.v.get_device():
             raise ValueError(f"{name} lies on two devices")
+        n = kv.len_dev
+        if n is not None and (n.dtype != torch.int32 or n.numel() < 1 or n.get_device() != kv.k.get_device()):
+            raise ValueError(f"{name}: len_dev must be an int32 on its device")
         kv._rows = want
 
     def _on_device(self, *checks):

@@ -72,3 +72,15 @@ def test_a_count_past_the_path_is_refused():
     for ok in (None, 1, 4):  # on to the next check
         with pytest.raises(ValueError, match="device"):
             ppd.ppd_kvq_commit(kv, 0, path, n, path_len=ok)
+
+
+def test_a_count_of_another_kind_or_device_is_refused():
+    """len_dev is written as an int32 by the commit's kernel."""
+    assert _cache(torch.zeros(1, dtype=torch.int32)).tail.len_dev is not None
+    for bad in (torch.zeros(1, dtype=torch.int64), torch.zeros(0, dtype=torch.int32), torch.zeros(1)):
+        with pytest.raises(ValueError, match="tail: len_dev"):
+            _cache(bad)
+    with pytest.raises(ValueError, match="tail: len_dev"):
+        far = _cache().tail
+        far.len_dev, far._rows = On(0), None
+        ppd.KVQCache(torch.zeros((2, 4, 8, 4608), dtype=torch.uint8), far)
