@@ -365,7 +365,8 @@ ppd_status ppd_next_tree(int32_t T, const int32_t *parent, const int32_t *ids, i
  *   Element e of a word is its bits 4 (e / 2) + 16 (e % 2) .. + 3.
  * Positions [0, L) of every head hold the cached prefix; what the positions
  * behind hold is never used, and a call leaves every position that it does
- * not write as it was.
+ * not write as it was.  Eight neighbours (8 i .. 8 i + 7) share words: two calls
+ * that write among them must not overlap in time.
  */
 #define PPD_KVQ_BLOCK 32
 #define PPD_KVQ_BLOCK_BYTES 4608
@@ -494,7 +495,13 @@ ppd_status ppd_kvq_score(const ppd_kvq *kv, int32_t L, int32_t n_heads, int32_t 
  *   kept       device int32 [n_layers][n_kv_heads][budget]: the kept positions,
  *              rising, in its first n entries
  * 1 <= budget <= dst capacity, n_sink, n_recent >= 0, n_sink + n_recent <=
- * budget, L <= src capacity.
+ * budget, L <= src capacity.  L <= budget keeps every position, and writes dst,
+ * score_out and kept all the same.
+ * A head's selection, and its move where src is dst, are one workgroup's work:
+ * with fewer heads (layers x kv heads) than the 256 compute units most of the
+ * device is idle, and a second cache is the faster form (2 heads, 524288
+ * positions cut to half: 0.67 ms, in place 2.7; 32 heads, 32768 positions 83 and
+ * 183 us; 256 heads, 4096 positions 49 and 48).
  */
 ppd_status ppd_kvq_evict(const ppd_kvq *src, const ppd_kvq *dst, int32_t L, int32_t budget, int32_t n_sink,
                          int32_t n_recent, const float *score, float *score_out, int32_t *kept, void *stream);

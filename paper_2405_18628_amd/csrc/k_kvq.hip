@@ -11,10 +11,10 @@
 // writer.
 //
 // All of them are bound by memory (a large copy runs at 4.8 TB/s here).  8 layers
-// of 32 heads: 2048 positions to 4 bits 74 us (4.6 TB/s; 1730 vector
+// of 32 heads: 2048 positions to 4 bits 73 us (4.7 TB/s; 1730 vector
 // instructions a block, 50 us of them, behind the loads), back 66 us (5.2 TB/s);
-// of 4096 positions 2048 kept 13.8 + 43 us (5.2 TB/s counting the lines of rows
-// that go, in place 12.4 + 35).  A path's rows: 1024 heads, five rows, 12.7 us, a
+// of 4096 positions 2048 kept 13.8 + 44 us (5.2 TB/s counting the lines of rows
+// that go, in place 12.5 + 35).  A path's rows: 1024 heads, five rows, 12.8 us, a
 // chain of three round trips (path, rows, the words that neighbours share) and 3
 // us of codes.  Bf16 key rows bypass the caches (with them to 4 bits 92 us, back
 // 77); codes do not, they are read again soon.
@@ -367,7 +367,8 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_load_kernel(KvqLoad p) {
 // searched for the last one that is kept, eleven bits at a time by counting (a
 // thread's scan of 256 counts in four passes took half of 26 us); then the
 // positions are written in order.  One workgroup a head, 4096 positions 13.8 us:
-// three passes of an L2 round trip and four barriers, and one to write.
+// three passes of an L2 round trip and four barriers, and one to write.  (Few
+// heads leave compute units idle: with the move 2 heads, 524288 positions 670 us.)
 constexpr int kSel = 1024, kBins = 2048, kSelRun = 4;
 
 __device__ __forceinline__ uint32_t order_word(float v) {
@@ -480,6 +481,8 @@ __global__ __launch_bounds__(kSel) void kvq_select_kernel(KvqEvict p) {
 // WAIT (src is dst, one workgroup a head): a workgroup's blocks are read whole
 // before any is written, and the runs follow in order, so that no row is
 // overwritten before it was read (a kept position never lies before its place).
+// That is one compute unit's stream: 2 heads, 524288 positions 2.7 ms in place,
+// 0.67 into another cache; from 256 heads on the two are alike.
 template <int W, bool WAIT>
 __global__ __launch_bounds__(64 * W) void kvq_gather_kernel(KvqEvict p) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -21,16 +21,18 @@
 // straight into the registers of the wave that multiplies them, the next block
 // requested while one is multiplied.  (NQ, QW, PARS) by the tiles of a kv head:
 // (1, 1, 8) for one, (2, 1, 8) for two, (2, 2, 4) up to four, (2, 4, 2) beyond:
-// two tiles share a block's expansion and parameters.  (64 nodes, 32768
-// positions: one tile a wave 112 us, two 99.)  Queries of two tiles a wave lie in
+// two tiles share a block's expansion and parameters.  (The rule looks at tiles
+// alone.  32 heads, 64 nodes, one tile a wave and two, both launches: 32768
+// positions 110 and 89 us, 8192 36.2 and 33.8, but 4096 23.3 and 24.2, 2048 16.7
+// and 19.6.)  Queries of two tiles a wave lie in
 // LDS, their registers hold the sums.  Splits: as many as fill the compute
 // units; a second launch adds them in order.
 //
 // Bounds.  A block takes 345 vector instructions for one tile (112 of them the
 // expansion), about 280 a tile for two, 24 or 32 matrix instructions: with small
 // trees that and the stream are near each other, with large ones the vector unit
-// is the bound.  us a launch, kernel alone (+ the launch that adds splits): 32
-// heads, 16 nodes, 32768 positions 33 (4.6 TB/s) + 4; 64 nodes, 2048 positions 17
+// is the bound.  us a launch under the profiler (+ the launch that adds splits): 32
+// heads, 16 nodes, 32768 positions 33 (4.5 TB/s) + 5; 64 nodes, 2048 positions 17
 // + 4, of which 9 stay at 32 positions (tree rows, meeting of the waves, launch);
 // 16 heads, one node, 200 positions 6.  Not kept: four waves a SIMD (128
 // registers, nothing requested ahead; 16 nodes 46 us against 45 then), two blocks
@@ -62,7 +64,11 @@ __device__ __forceinline__ float sum8(u32x4 v) {
   return s;
 }
 
-// probabilities as two bf16 parts
+// Probabilities as two bf16 parts: the matrix cores take bf16, one part would
+// leave 2^-9 of a probability, the size of the output's own rounding; two leave
+// 2^-17, and a third would be half as many products with the values again.  (The
+// outputs differ by 2e-4 to 3e-4 of their norm from those with float32
+// probabilities, single bf16 steps; from 64 bits both differ by 0.0016 to 0.0017.)
 __device__ __forceinline__ void split8(const float (&v)[8], u32x4 &hi, u32x4 &lo) {
   float r[8];
 #pragma unroll
@@ -502,12 +508,13 @@ __global__ __launch_bounds__(NT) void kvq_merge_kernel(KvqAttnLaunch p) {
 // float32's own rounding of its exponent), one of a bfloat16.  A wave takes every
 // step-th block of a (layer, kv head), the next one requested ahead.
 //
-// Three nodes, 32 layers of 32 heads, 2048 positions 42 us (3.9 TB/s of a copy's
-// 4.8); five nodes, 32 heads on 8 kv heads, 8191 positions 49 (3.4 TB/s; two
+// Three nodes, 32 layers of 32 heads, 2048 positions 43 us (3.9 TB/s of a copy's
+// 4.8); five nodes, 32 heads on 8 kv heads, 8191 positions 50 (3.4 TB/s; two
 // tiles a key).  Bounds on registers: a tile of queries fits four waves a SIMD
-// (45 us with two; what spills lies before the loop over blocks), two tiles
-// three with bfloat16 queries (56 with two), two with float32's three parts.
-// With queries in LDS instead, 24 KB read for every block and tile, 62 and 89.
+// (45 us with two; float32's spills 14 registers, outside the loops over blocks),
+// two tiles three with bfloat16 queries (56 with two), two with float32's three
+// parts.  With queries in LDS instead, 24 KB read for every block and tile, 62
+// and 89.
 struct ScoreRow {
   float qs0, qs1, lse2;  // sums of q over the groups, ln sum exp in log2
 };

@@ -24,15 +24,16 @@
 // is max(w - C q, 0), C = Z_1 + .. + Z_j, since max(max(w - a, 0) - b, 0) =
 // max(w - a - b, 0): one row of weights, one of probabilities and a number, but
 // a sum over the row for each rejection, the next depending on it.  A workgroup
-// settles a node alone: weights in registers, probabilities in LDS.
+// settles a node alone: probabilities in LDS, weights in registers (128 a thread:
+// two of eight chunks' weights lie in scratch and come back in each sum).
 //
-// Bounds: latency.  64 nodes, V = 32000, no drafts 4.7 + 9.7 us (parts and walk:
+// Bounds: latency.  64 nodes, V = 32000, no drafts 4.9 + 9.8 us (parts and walk:
 // each a chain of two or three memory round trips and a few barriers); 25 nodes
-// with drafts, V = 32001, 29.5 + 5.0: 256 KB a compute unit and float64 sums and
-// exponentials of a row (with the library's exp 36 + 5).  One node, both launches:
-// V = 4000 15.5, 32000 22.8, 50257, whose rows do not fit the registers, 39.  A
-// cluster of workgroups a node would need waits between them for each
-// rejection.
+// with drafts, V = 32001, 29.4 + 5.1: 256 KB a compute unit and float64 sums and
+// exponentials of a row (with the library's exp 36 + 5), while as many compute
+// units work as there are nodes.  One node, both launches: V = 4000 15.8, 32000
+// 23.6, 50257, whose rows do not fit the registers, 40.6.  Several workgroups a
+// node (a wait among them for each rejection) have not been measured.
 
 #include "ppd_sample.h"
 
