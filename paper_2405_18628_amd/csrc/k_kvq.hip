@@ -482,7 +482,7 @@ __global__ __launch_bounds__(kSel) void kvq_select_kernel(KvqEvict p) {
 // before any is written, and the runs follow in order, so that no row is
 // overwritten before it was read (a kept position never lies before its place).
 // That is one compute unit's stream: 2 heads, 524288 positions 2.7 ms in place,
-// 0.67 into another cache; from 256 heads on the two are alike.
+// 0.67 into another cache; with 256 heads the two are alike.
 template <int W, bool WAIT>
 __global__ __launch_bounds__(64 * W) void kvq_gather_kernel(KvqEvict p) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
