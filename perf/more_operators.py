@@ -484,7 +484,7 @@ def _run_store(s):
 
 
 def _bits(mask, T):
-    """[T][T]: whether row i sees node j."""
+    """[rows][T]: whether a row sees node j of its tree."""
     j = torch.arange(T, device=mask.device)
     return (mask[:, j // 64] >> (j % 64) & 1).bool()
 
@@ -504,53 +504,56 @@ def _attention(q, k, v, see, dt):
 def _select(s):
     """Selected pages of every sequence and kv head, and how many."""
     c = s["case"]
-    sel, n_sel = s["sel"].clone(), s["n_sel"].clone()
-    nkv, G, page, budget = c["nkv"], c["nh"] // c["nkv"], c["page"], c["budget"]
-    for b, n in enumerate(_counts(c)[0]):
-        q = s["q"][b * c["T"]:(b + 1) * c["T"]].double().view(c["T"], nkv, G, D)
-        qp, qm = q.clamp(min=0).sum((0, 2)), q.clamp(max=0).sum((0, 2))     # [nkv][128]
-        np_ = _ceil(n, page)
-        bd = s["bounds"][0, s["table"][b, :np_].long()].double()            # [pages][nkv][2][128]
-        score = (bd[:, :, 1] * qp + bd[:, :, 0] * qm).sum(-1).t()           # [nkv][pages]
-        at = torch.arange(np_, device=score.device)
-        score = torch.where((at < c["first"]) | (at >= np_ - c["last"]), torch.full_like(score, float("inf")), score)
-        m = min(np_, budget)
-        best = torch.sort(score, dim=1, descending=True, stable=True)[1][:, :m]
-        sel[b, :, :m] = torch.sort(best, dim=1)[0].int()
-        n_sel[b] = m
-    return sel, n_sel
+    B, T, nkv, page, budget = c["B"], c["T"], c["nkv"], c["page"], c["budget"]
+    q = s["q"].double().view(B, T, nkv, -1, D)
+    qp, qm = q.clamp(min=0).sum((1, 3)), q.clamp(max=0).sum((1, 3))          # [B][nkv][128]
+    np_ = (s["len"].long() + page - 1) // page
+    most = _ceil(c["L"], page)
+    bd = s["bounds"][0, s["table"][:, :most].long()].double()               # [B][pages][nkv][2][128]
+    score = (bd[:, :, :, 1] * qp[:, None] + bd[:, :, :, 0] * qm[:, None]).sum(-1).transpose(1, 2)
+    at, inf = torch.arange(most, device=q.device), float("inf")
+    kept = (at < c["first"]) | (at >= np_[:, None] - c["last"])
+    score = torch.where(kept[:, None], torch.full_like(score, inf), score)
+    score = torch.where((at < np_[:, None])[:, None], score, torch.full_like(score, -inf))
+    best = torch.sort(score, dim=2, descending=True, stable=True)[1][:, :, :budget]
+    n_sel = np_.clamp(max=budget)
+    m = torch.arange(best.shape[2], device=q.device)
+    live = (m < n_sel[:, None])[:, None]
+    best = torch.sort(torch.where(live, best, torch.full_like(best, most)), dim=2)[0]
+    sel = s["sel"].clone()
+    sel[:, :, : best.shape[2]] = torch.where(live, best.int(), sel[:, :, : best.shape[2]])
+    return sel, n_sel.int()
 
 
-def _run_attention(s, sel=None):
+def _run_attention(s, sel=None, n_sel=None):
     c = s["case"]
-    nkv, nh, T, page = c["nkv"], c["nh"], c["T"], c["page"]
+    B, T, nkv, nh, page = c["B"], c["T"], c["nkv"], c["nh"], c["page"]
     G = nh // nkv
-    dt = s["q"].dtype
-    out, lse = torch.zeros_like(s["out"]), torch.zeros_like(s["lse"])
-    for b, n in enumerate(_counts(c)[0]):
-        r0 = b * T
-        q = s["q"][r0:r0 + T].float().view(T, nkv, G, D).transpose(0, 1).reshape(nkv, T * G, D)
-        np_ = _ceil(n, page)
-        phys = s["table"][b, :np_].long()
-        if sel is None:
-            k, v = _unpack(s["pages"][0, phys].transpose(0, 1).reshape(nkv, -1, 2, 4096))
-            k, v = k[:, :n], v[:, :n]
-            seen = torch.ones((1, 1, n), dtype=torch.bool, device=q.device)
-        else:
-            pick = sel[b, :, : min(np_, c["budget"])].long()                 # [nkv][m]
-            head = torch.arange(nkv, device=q.device)[:, None]
-            k, v = _unpack(s["pages"][0, phys[pick], head].reshape(nkv, -1, 2, 4096))
-            pos = pick[:, :, None] * page + torch.arange(page, device=q.device)
-            seen = (pos < n).reshape(nkv, 1, -1)
-            v = torch.where(seen[:, 0, :, None], v, torch.zeros_like(v))
-        k = torch.cat((k, s["tk"][0, :, r0:r0 + T]), 1).float()
-        v = torch.cat((v, s["tv"][0, :, :, r0:r0 + T].transpose(1, 2)), 1).float()
-        tree = _bits(s["mask"][r0:r0 + T], T).repeat_interleave(G, 0)[None]
-        see = torch.cat((seen.expand(nkv, T * G, -1), tree.expand(nkv, -1, -1)), 2)
-        o, l = _attention(q, k, v, see, dt)
-        out[r0:r0 + T] = o.view(nkv, T, G, D).transpose(0, 1).reshape(T, nh, D)
-        lse[r0:r0 + T] = l.view(nkv, T, G).transpose(0, 1).reshape(T, nh)
-    return out, lse
+    dev = s["q"].device
+    q = s["q"].float().view(B, T, nkv, G, D).permute(0, 2, 1, 3, 4).reshape(B * nkv, T * G, D)
+    most = _ceil(c["L"], page)
+    # logical pages [B][nkv or 1][m] and whether they count
+    if sel is None:
+        pick = torch.arange(most, device=dev).expand(B, 1, most)
+        counts = torch.ones_like(pick, dtype=torch.bool)
+        blocks = s["pages"][0, s["table"][:, :most].long()].transpose(1, 2)
+    else:
+        counts = (torch.arange(sel.shape[2], device=dev) < n_sel[:, None])[:, None].expand_as(sel)
+        pick = torch.where(counts, sel, torch.zeros_like(sel)).long()
+        phys = s["table"].long()[torch.arange(B, device=dev)[:, None, None], pick]
+        blocks = s["pages"][0, phys, torch.arange(nkv, device=dev)[:, None]]
+    k, v = _unpack(blocks.reshape(B, nkv, -1, 2, 4096))
+    pos = pick[..., None] * page + torch.arange(page, device=dev)
+    seen = ((pos < s["len"][:, None, None, None]) & counts[..., None]).reshape(B, -1, 1, k.shape[2]).expand(B, nkv, T * G, -1)
+    rows = B * T
+    tk = s["tk"][0, :, :rows].view(nkv, B, T, D).transpose(0, 1)
+    tv = s["tv"][0, :, :, :rows].view(nkv, D, B, T).permute(2, 0, 3, 1)
+    k, v = torch.cat((k, tk), 2).float(), torch.cat((v, tv), 2).float()
+    tree = _bits(s["mask"], T).view(B, 1, T, 1, T).expand(B, nkv, T, G, T).reshape(B, nkv, T * G, T)
+    see = torch.cat((seen, tree), 3).reshape(B * nkv, T * G, -1)
+    o, l = _attention(q, k.reshape(B * nkv, -1, D), v.reshape(B * nkv, -1, D), see, s["q"].dtype)
+    out = o.view(B, nkv, T, G, D).permute(0, 2, 1, 3, 4).reshape(rows, nh, D)
+    return out, l.view(B, nkv, T, G).permute(0, 2, 1, 3).reshape(rows, nh)
 
 
 def run(state):
@@ -565,7 +568,7 @@ def run(state):
         out, lse = _run_attention(state)
         return dict(out=out, lse=lse)
     sel, n_sel = _select(state)
-    out, lse = _run_attention(state, sel)
+    out, lse = _run_attention(state, sel, n_sel)
     return dict(sel=sel, n_sel=n_sel, out=out, lse=lse)
 
 
