@@ -19,7 +19,8 @@
  *                        step's outputs (Section 3, step (1))
  *
  * ppd_accept_sample takes ppd_accept's place for decoding at a temperature, and
- * the ppd_kvq calls that of the bf16 cache for one held in 4 bits.
+ * the ppd_kvq calls that of the bf16 cache for one held in 4 bits; the ppd_paged
+ * calls serve many sequences from one pool of pages, with lengths on the device.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -89,6 +90,9 @@ typedef enum { PPD_F32 = 0, PPD_BF16 = 1 } ppd_dtype;
 #define PPD_DEV_SYNC_TIMEOUT 16u /* a workgroup gave up waiting for the other
                                     workgroups of its tile (bounded wait); the
                                     step's outputs are then invalid          */
+#define PPD_DEV_NO_PAGES 32u    /* ppd_paged_tables refused a sequence its tokens */
+#define PPD_DEV_BAD_LENGTH 64u  /* a length, count or row offset on the device was
+                                    out of range and was clamped             */
 
 /*
  * Llama-style decoder (the paper's MobileLLaMA / Vicuna family): pre-RMSNorm
@@ -505,6 +509,168 @@ ppd_status ppd_kvq_score(const ppd_kvq *kv, int32_t L, int32_t n_heads, int32_t 
  */
 ppd_status ppd_kvq_evict(const ppd_kvq *src, const ppd_kvq *dst, int32_t L, int32_t budget, int32_t n_sink,
                          int32_t n_recent, const float *score, float *score_out, int32_t *kept, void *stream);
+
+/*
+ * A KV cache in pages that many sequences share (bf16 models, head_dim 128).
+ * Lengths, tables and slot maps live on the device and are advanced there, so
+ * one captured step can be replayed while the sequences grow:
+ *   verify   ppd_verify_batch_paged   tree rows to `tail`, attention over both
+ *   accept   ppd_accept or ppd_accept_sample, per sequence
+ *   tables   ppd_paged_tables         pages for the accepted rows, their slots
+ *   store    ppd_paged_store          accepted rows of `tail` into the pages
+ * Pages hold `page` positions (32, 64, 128 or 256) of every layer and kv head:
+ *   pages   device bfloat16 [n_layers][n_pages][n_kv_heads][page / 32][2][4096],
+ *           a block of 32 positions as its keys (after RoPE) and its values in
+ *           the operand order of the matrix instructions: position u, dim d is
+ *             keys    (((u / 4 % 2) 4 + d / 32) 64 + 16 (d / 8 % 4) + 4 (u / 8) + u % 4) 8 + d % 8
+ *             values  ((d / 16) 64 + 16 (u / 8) + d % 16) 8 + u % 8
+ *   bounds  device bfloat16 [n_layers][n_pages][n_kv_heads][2][128]: each page's
+ *           smallest and largest key element of every dim, or NULL (then
+ *           ppd_paged_select is refused)
+ * What pages hold behind a sequence's length is never used (it may be NaN).
+ * Pages may appear in several tables as long as no call writes to them.
+ */
+#define PPD_PAGED_BLOCK 32
+#define PPD_PAGED_PAGE_MAX 256
+#define PPD_PAGED_SEQS_MAX 4096
+typedef struct {
+  void *pages;     /* 16-byte aligned */
+  void *bounds;    /* 16-byte aligned, or NULL */
+  int32_t n_layers, n_kv_heads, n_pages, page;
+  ppd_kv tail;     /* bfloat16 staging of the new tokens' rows, all sequences': row i at position i of
+                      [n_layers][n_kv_heads][tail.capacity][128] keys and [..][128][tail.capacity] values,
+                      tail.capacity a multiple of 8; all zero for calls that name no tail */
+} ppd_paged;
+
+/* The sequences' page tables and the pages that no sequence holds.  Sequence s
+ * holds ceil(len[s] / page) pages, the first entries of its table row. */
+typedef struct {
+  int32_t *table;       /* device [n_seqs][max_pages] */
+  int32_t *len;         /* device [n_seqs]: cached tokens */
+  int32_t *free_pages;  /* device [n_pages]: a ring of free pages */
+  int32_t *free_state;  /* device [2]: index of the ring's first entry, entries.  At first 0 and
+                           n_pages, the ring 0 .. n_pages - 1 */
+  int32_t n_seqs, max_pages, n_pages, page;
+} ppd_page_tables;
+
+/* Bytes of `pages` and of `bounds`; 0 on invalid sizes. */
+size_t ppd_paged_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t n_pages, int32_t page);
+size_t ppd_paged_bounds_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t n_pages);
+
+/*
+ * Tables and slot map from the sequences' lengths: every sequence s gets add[s]
+ * more tokens (device int32; as ppd_accept's n_path gives them), or has ended
+ * (add[s] < 0) and gives its pages back.
+ *   start   device int32[n_seqs + 1]: where each sequence's new rows start among
+ *           all of them, and their number (ended sequences have none; at most
+ *           2^31 - 1)
+ *   slots   device int32[n_slots]: of row start[s] + t, the place (page x
+ *           positions of a page + position in it) of token len[s] + t; entries
+ *           behind start[n_seqs] are left as they were
+ *   len_out, free_state_out   device, may be pt->len and pt->free_state: lengths
+ *           (0 of ended sequences) and the ring's state afterwards
+ * Pages are taken from the ring in order of sequences and tokens and written to
+ * pt->table; pages given back are appended in order and are first taken by
+ * the next call.  All or nothing: a sequence keeps its length and its slots
+ * are -1 (PPD_DEV_NO_PAGES) where its new length passes max_pages pages or its
+ * rows n_slots, and from the first of the others that the free pages do not
+ * suffice for on, where it needs a page.
+ *   ws      device workspace, 16-byte aligned, of
+ *           ppd_paged_tables_workspace_bytes(n_seqs) (its header the status word)
+ */
+size_t ppd_paged_tables_workspace_bytes(int32_t n_seqs);
+ppd_status ppd_paged_tables(const ppd_page_tables *pt, const int32_t *add, int32_t *len_out, int32_t *free_state_out,
+                            int32_t *start, int32_t *slots, int32_t n_slots, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Rows into pages, every layer and kv head, and the pages' bounds, if kept.  Row
+ * start[s] + k (start as ppd_paged_tables gives it, n_seqs + 1 offsets) goes to
+ * slots[start[s] + k] from row
+ *   row_start[s] + path[row_start[s] + k]   of src (accepted nodes of a tree), or
+ *   row_start[s] + k                        where path is NULL (a prompt)
+ * Rows at and behind n_rows, and slots outside the pages, are left out; source rows
+ * are clamped to src.  A page's bounds start anew with its first position
+ * and else widen; a NaN has no part in them.  Rows of one sequence have rising
+ * positions, and no page is written for two sequences.
+ *   src        the tail or another bfloat16 cache of the same layers and heads
+ *   row_start  device int32[n_seqs]; path device int32 (n_path entries) or NULL
+ *   slots      device int32[n_rows]
+ */
+ppd_status ppd_paged_store(const ppd_paged *kv, const ppd_kv *src, int32_t n_seqs, const int32_t *start,
+                           const int32_t *row_start, const int32_t *path, int32_t n_path, const int32_t *slots,
+                           int32_t n_rows, void *stream);
+
+/*
+ * Attention of one layer: the new rows of every sequence -- one token, or the
+ * nodes of a tree -- over its pages and its own rows in kv->tail.  Sequence s has
+ * rows [row_start[s], row_start[s + 1]) of q, mask, out, lse and the tail
+ * (device int32[n_seqs + 1], not falling; up to PPD_T_MAX rows a sequence,
+ * none allowed).  Row t of head h attends to positions [0, len[s]) of kv head h /
+ * (n_heads / n_kv_heads), or those of them in the listed pages, and to the
+ * sequence's rows whose mask bit is set (bits over its own rows; mask NULL: its
+ * rows up to t), scale 1 / sqrt(128).  Sums are float32; probabilities and
+ * float32 queries enter the products as two bfloat16 parts (bfloat16 calls) or
+ * three (float32 calls).  A row that sees nothing gets zeros, and minus
+ * infinity in lse; NaN and infinities reach only rows that see them.
+ *   n_rows   rows that the buffers hold (rows behind row_start[n_seqs] are left
+ *            as they were); n_rows <= tail.capacity
+ *   q, out   device [n_rows][n_heads][128] of type dtype (PPD_BF16 or PPD_F32),
+ *            16-byte aligned, not the same buffer
+ *   lse      device float32 [n_rows][n_heads]: ln sum exp of the row's scores, or NULL
+ *   sel, n_sel   pages by their place in the table, device int32
+ *            [n_seqs][n_kv_heads][budget] and how many of them count, device
+ *            int32[n_seqs] (as ppd_paged_select gives them; none twice), or NULL
+ *   ws       device workspace, 16-byte aligned, of
+ *            ppd_paged_attention_workspace_bytes(n_heads, n_kv_heads, n_seqs, n_rows),
+ *            one for each stream that calls may overlap on (its header the status word)
+ */
+size_t ppd_paged_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t n_rows);
+ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,
+                               const int32_t *row_start, int32_t n_rows, const void *q, int32_t dtype,
+                               const uint64_t *mask, void *out, float *lse, const int32_t *sel, const int32_t *n_sel,
+                               int32_t budget, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The pages of each sequence and kv head that matter most to its new rows, for
+ * ppd_paged_attention: of its n = ceil(len / page) pages min(n, budget), the
+ * first n_first and the last n_last of them always, and of the others those
+ * of the largest score
+ *     sum over dims d of  Qp[d] largest[d] + Qm[d] smallest[d],
+ * Qp and Qm the sums over the sequence's rows and the kv head's query heads of
+ * max(q, 0) and min(q, 0): the sum of what each query's product with a key of the
+ * page can be at most.  All sums in 64 bits, as an order hangs on them (equal
+ * scores: the smaller page; NaN after every number).  A call for each query alone
+ * is one with a sequence for each (tables may share pages).
+ *   q, dtype, row_start, n_rows, layer   as for ppd_paged_attention
+ *   budget   1 .. max_pages or more; 0 <= n_first + n_last <= budget
+ *   sel      device int32 [n_seqs][n_kv_heads][budget]: rising; entries behind the
+ *            selected ones are left as they were
+ *   n_sel    device int32[n_seqs]
+ *   ws       device workspace, 16-byte aligned, of
+ *            ppd_paged_select_workspace_bytes(n_kv_heads, n_seqs, max_pages)
+ */
+size_t ppd_paged_select_workspace_bytes(int32_t n_kv_heads, int32_t n_seqs, int32_t max_pages);
+ppd_status ppd_paged_select(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,
+                            const int32_t *row_start, int32_t n_rows, const void *q, int32_t dtype, int32_t budget,
+                            int32_t n_first, int32_t n_last, int32_t *sel, int32_t *n_sel, void *ws, size_t ws_bytes,
+                            void *stream);
+
+/*
+ * ppd_verify_batch on pages: sequence s of pt has rows [row_start[s],
+ * row_start[s + 1]) of ids, depth, mask, logits and pred (device int32[n_seqs +
+ * 1], rising to n_rows = all tree tokens <= PPD_T_MAX; sequences without rows
+ * sit the step out), its root at position len[s].  Lengths and offsets are read
+ * on the device: a captured step serves whatever they are when it is replayed.
+ * The rows go to kv->tail.  budget > 0: every layer attends to the pages that
+ * ppd_paged_select picks (budget, n_first, n_last as there); 0: to all.
+ *   ws   ppd_paged_workspace_bytes(model, n_seqs, max_pages, n_rows, budget)
+ */
+size_t ppd_paged_workspace_bytes(const ppd_model *model, int32_t n_seqs, int32_t max_pages, int32_t n_rows,
+                                 int32_t budget);
+ppd_status ppd_verify_batch_paged(const ppd_model *model, const ppd_paged *kv, const ppd_page_tables *pt,
+                                  const int32_t *row_start, int32_t n_rows, const int32_t *ids, const int32_t *depth,
+                                  const uint64_t *mask, int32_t budget, int32_t n_first, int32_t n_last, void *ws,
+                                  size_t ws_bytes, float *logits, int32_t *pred, void *stream);
 
 /*
  * Verification of drafted tokens against the target's probabilities (beside

@@ -25,7 +25,9 @@ PPD_F32, PPD_BF16 = 0, 1
 PPD_T_MAX = 128
 PPD_MASK_WORDS = 2
 PPD_DEV_BAD_TOKEN, PPD_DEV_BAD_PARENT, PPD_DEV_NAN_LOGIT = 1, 2, 4
+PPD_DEV_NO_PAGES, PPD_DEV_BAD_LENGTH = 32, 64
 PPD_KVQ_BLOCK, PPD_KVQ_BLOCK_BYTES = 32, 4608
+PPD_PAGED_BLOCK, PPD_PAGED_PAGE_MAX = 32, 256
 PPD_W_QKV, PPD_W_O, PPD_W_GATE_UP, PPD_W_DOWN, PPD_W_LM_HEAD = range(5)
 
 _STATUS_NAMES = {0: "PPD_OK", 1: "PPD_EINVAL", 2: "PPD_ETREE", 3: "PPD_ECAPACITY",
@@ -58,6 +60,16 @@ class ppd_kv(C.Structure):
 class ppd_kvq(C.Structure):
     _fields_ = [("blocks", C.c_void_p), ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("capacity", C.c_int32), ("tail", ppd_kv)]
+
+
+class ppd_paged(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("bounds", C.c_void_p), ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("n_pages", C.c_int32), ("page", C.c_int32), ("tail", ppd_kv)]
+
+
+class ppd_page_tables(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("len", C.c_void_p), ("free_pages", C.c_void_p), ("free_state", C.c_void_p),
+                ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page", C.c_int32)]
 
 
 _lib = None
@@ -114,6 +126,24 @@ def lib() -> C.CDLL:
         L.ppd_accept_sample.argtypes = [i32, vp, vp, i32, vp, C.c_float, vp, vp, vp, vp, vp, vp, sz, vp]
         for f in ("ppd_kvq_quantize", "ppd_kvq_dequantize", "ppd_kvq_commit", "ppd_kvq_attention",
                   "ppd_verify_batch_kvq", "ppd_verify_step_kvq", "ppd_kvq_score", "ppd_kvq_evict", "ppd_accept_sample"):
+            getattr(L, f).restype = C.c_int
+        pp, pt = P(ppd_paged), P(ppd_page_tables)
+        L.ppd_paged_bytes.argtypes = [i32, i32, i32, i32]
+        L.ppd_paged_bounds_bytes.argtypes = [i32, i32, i32]
+        L.ppd_paged_tables_workspace_bytes.argtypes = [i32]
+        L.ppd_paged_attention_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.ppd_paged_select_workspace_bytes.argtypes = [i32, i32, i32]
+        L.ppd_paged_workspace_bytes.argtypes = [P(ppd_model), i32, i32, i32, i32]
+        for f in ("ppd_paged_bytes", "ppd_paged_bounds_bytes", "ppd_paged_tables_workspace_bytes",
+                  "ppd_paged_attention_workspace_bytes", "ppd_paged_select_workspace_bytes", "ppd_paged_workspace_bytes"):
+            getattr(L, f).restype = sz
+        L.ppd_paged_tables.argtypes = [pt, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+        L.ppd_paged_store.argtypes = [pp, P(ppd_kv), i32, vp, vp, vp, i32, vp, i32, vp]
+        L.ppd_paged_attention.argtypes = [i32, pp, i32, pt, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+        L.ppd_paged_select.argtypes = [i32, pp, i32, pt, vp, i32, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.ppd_verify_batch_paged.argtypes = [P(ppd_model), pp, pt, vp, i32, vp, vp, vp, i32, i32, i32, vp, sz, vp, vp, vp]
+        for f in ("ppd_paged_tables", "ppd_paged_store", "ppd_paged_attention", "ppd_paged_select",
+                  "ppd_verify_batch_paged"):
             getattr(L, f).restype = C.c_int
         for f in ("ppd_verify_step_static", "ppd_next_tree", "ppd_sparse_template", "ppd_verify_batch", "ppd_pack_weight", "ppd_workspace_init", "ppd_build_tree_mask", "ppd_verify_step", "ppd_accept",
                   "ppd_kv_compact", "ppd_device_status", "ppd_set_kernel_timer", "ppd_read_probe"):
@@ -360,6 +390,83 @@ class KVQCache:
         """The cache, and the call's other tensors, are on the current device."""
         tail = self.tail
         _tensors(self.device, (self.blocks, None, "blocks"), (tail.k if tail is not None else None, None, "tail"), *checks)
+
+
+class PagedCache:
+    """A cache in pages: pages bf16 [layers][n_pages][kv_heads][page / 32][2][4096]
+    (layout in include/ppd.h), bounds bf16 [layers][n_pages][kv_heads][2][128] of
+    the pages' keys (None: ppd_paged_select is refused) and, for the calls that
+    read or write new tokens' rows, their bf16 staging cache `tail` (a KVCache of
+    the same layers and heads)."""
+
+    def __init__(self, pages, bounds=None, tail: Optional[KVCache] = None):
+        import torch
+        if pages.dim() != 6 or pages.shape[4:] != (2, 4096) or pages.dtype != torch.bfloat16:
+            raise ValueError("pages must be bf16 [layers][n_pages][kv_heads][page / 32][2][4096]")
+        if not pages.is_contiguous():
+            raise ValueError("pages must be contiguous")
+        self.n_layers, self.n_pages, self.n_kv_heads = (int(n) for n in pages.shape[:3])
+        self.page = int(pages.shape[3]) * PPD_PAGED_BLOCK
+        if bounds is not None:
+            if bounds.shape != (*pages.shape[:3], 2, 128) or bounds.dtype != torch.bfloat16 or not bounds.is_contiguous():
+                raise ValueError("bounds must be contiguous bf16 [layers][n_pages][kv_heads][2][128]")
+        if tail is not None:
+            KVQCache._check_rows(tail, (self.n_layers, self.n_kv_heads), "tail")
+        self.pages, self.bounds, self.tail = pages, bounds, tail
+        self.device = pages.get_device()
+        self.desc = ppd_paged(_ptr(pages), _ptr(bounds) or None, self.n_layers, self.n_kv_heads, self.n_pages, self.page,
+                              tail.desc if tail is not None else ppd_kv())
+
+    @classmethod
+    def empty(cls, n_layers: int, n_kv_heads: int, n_pages: int, page: int, tail_capacity: int = PPD_T_MAX,
+              bounds: bool = True, device="cuda"):
+        """A pool of n_pages pages of `page` positions and its staging cache, uninitialised."""
+        import torch
+        if page not in (32, 64, 128, 256):
+            raise ValueError(f"pages hold 32, 64, 128 or 256 positions, not {page}")
+
+        def new(*shape):
+            return torch.empty(shape, dtype=torch.bfloat16, device=device)
+        tail = KVCache(new(n_layers, n_kv_heads, tail_capacity, 128), new(n_layers, n_kv_heads, 128, tail_capacity))
+        return cls(new(n_layers, n_pages, n_kv_heads, page // PPD_PAGED_BLOCK, 2, 4096),
+                   new(n_layers, n_pages, n_kv_heads, 2, 128) if bounds else None, tail)
+
+    def _on_device(self, *checks):
+        """The cache, and the call's other tensors, are on the current device."""
+        tail = self.tail
+        _tensors(self.device, (self.pages, None, "pages"), (self.bounds, None, "bounds"),
+                 (tail.k if tail is not None else None, None, "tail"), *checks)
+
+
+class PageTables:
+    """Page tables of n_seqs sequences, all int32: table [n_seqs][max_pages], len
+    [n_seqs], the ring of free pages [n_pages] and its state [2] (first entry,
+    entries)."""
+
+    def __init__(self, table, len, free_pages, free_state, page: int):
+        import torch
+        if table.dim() != 2 or len.shape != table.shape[:1] or free_pages.dim() != 1 or free_state.shape != (2,):
+            raise ValueError("table must be [n_seqs][max_pages], len [n_seqs], free_pages [n_pages], free_state [2]")
+        for t in (table, len, free_pages, free_state):
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != table.get_device():
+                raise ValueError("page tables must be contiguous int32 tensors of one device")
+        self.table, self.len, self.free_pages, self.free_state = table, len, free_pages, free_state
+        self.n_seqs, self.max_pages = (int(n) for n in table.shape)
+        self.n_pages, self.page = int(free_pages.shape[0]), int(page)
+        self.device = table.get_device()
+        self.desc = ppd_page_tables(_ptr(table), _ptr(len), _ptr(free_pages), _ptr(free_state), self.n_seqs,
+                                    self.max_pages, self.n_pages, self.page)
+
+    @classmethod
+    def empty(cls, n_seqs: int, max_pages: int, n_pages: int, page: int, device="cuda"):
+        """n_seqs sequences without tokens, every page free."""
+        import torch
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.zeros((n_seqs, max_pages), **i32), torch.zeros(n_seqs, **i32), torch.arange(n_pages, **i32),
+                   torch.tensor([0, n_pages], **i32), page)
+
+    def _on_device(self, *checks):
+        _tensors(self.device, (self.table, None, "table"), *checks)
 
 
 # ---------------------------------------------------------------------------
@@ -688,6 +795,135 @@ def ppd_kvq_evict(src: KVQCache, dst: KVQCache, L: int, budget: int, n_sink: int
     _check(lib().ppd_kvq_evict(C.byref(src.desc), C.byref(dst.desc), int(L), int(budget), int(n_sink), int(n_recent),
                                _ptr(score), _ptr(score_out), _ptr(kept), _stream(stream)))
     return min(int(L), int(budget))
+
+
+def ppd_paged_bytes(n_layers: int, n_kv_heads: int, n_pages: int, page: int) -> int:
+    return _bytes(lib().ppd_paged_bytes(int(n_layers), int(n_kv_heads), int(n_pages), int(page)))
+
+
+def ppd_paged_bounds_bytes(n_layers: int, n_kv_heads: int, n_pages: int) -> int:
+    return _bytes(lib().ppd_paged_bounds_bytes(int(n_layers), int(n_kv_heads), int(n_pages)))
+
+
+def ppd_paged_tables_workspace_bytes(n_seqs: int) -> int:
+    return _bytes(lib().ppd_paged_tables_workspace_bytes(int(n_seqs)))
+
+
+def ppd_paged_tables(pt: PageTables, add, start, slots, ws, len_out=None, free_state_out=None, stream=None):
+    """Pages for add [n_seqs] more tokens of every sequence (negative: it has
+    ended); start [n_seqs + 1] and slots get the rows' offsets and places.
+    Lengths and the ring's state are written to pt unless given elsewhere."""
+    i32 = _i32_dtype()
+    len_out = pt.len if len_out is None else len_out
+    free_state_out = pt.free_state if free_state_out is None else free_state_out
+    pt._on_device((add, i32, "add"), (start, i32, "start"), (slots, i32, "slots"), (ws, None, "ws"),
+                  (len_out, i32, "len_out"), (free_state_out, i32, "free_state_out"))
+    n = pt.n_seqs
+    if add.numel() != n or len_out.numel() != n or start.numel() != n + 1 or free_state_out.numel() != 2:
+        raise ValueError(f"add and len_out must be [{n}], start [{n + 1}], free_state_out [2]")
+    _check(lib().ppd_paged_tables(C.byref(pt.desc), _ptr(add), _ptr(len_out), _ptr(free_state_out), _ptr(start),
+                                  _ptr(slots), slots.numel(), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def ppd_paged_store(kv: PagedCache, src: KVCache, start, row_start, path, slots, stream=None):
+    """Rows of src into pages: row start[s] + k to slots[start[s] + k], from src's
+    row row_start[s] + path[row_start[s] + k] (path None: row_start[s] + k)."""
+    i32 = _i32_dtype()
+    KVQCache._check_rows(src, (kv.n_layers, kv.n_kv_heads), "src")
+    kv._on_device((src.k, None, "src"), (start, i32, "start"), (row_start, i32, "row_start"), (path, i32, "path"),
+                  (slots, i32, "slots"))
+    n = start.numel() - 1
+    if row_start.numel() < n:
+        raise ValueError(f"row_start holds {row_start.numel()} offsets, not {n}")
+    _check(lib().ppd_paged_store(C.byref(kv.desc), C.byref(src.desc), n, _ptr(start), _ptr(row_start), _ptr(path) or None,
+                                 0 if path is None else path.numel(), _ptr(slots), slots.numel(), _stream(stream)))
+
+
+def ppd_paged_attention_workspace_bytes(n_heads: int, n_kv_heads: int, n_seqs: int, n_rows: int) -> int:
+    return _bytes(lib().ppd_paged_attention_workspace_bytes(int(n_heads), int(n_kv_heads), int(n_seqs), int(n_rows)))
+
+
+def _i32_dtype():
+    t = _torch
+    if t is None:
+        import torch as t
+    return t.int32
+
+
+def _paged_rows(kv, pt, row_start, q, sel, n_sel, budget, *checks):
+    """The checks that attention and selection share; the rows' type as PPD_F32 or PPD_BF16."""
+    i32 = _i32_dtype()
+    bf16, f32 = _dtypes()
+    kv._on_device((pt.table, None, "table"), (row_start, i32, "row_start"), (q, None, "q"), (sel, i32, "sel"),
+                  (n_sel, i32, "n_sel"), *checks)
+    n = pt.n_seqs
+    if row_start.numel() != n + 1:
+        raise ValueError(f"row_start must be [{n + 1}]")
+    if q.dim() != 3 or q.shape[2] != 128 or q.dtype not in (bf16, f32):
+        raise ValueError("q must be bf16 or float32 [rows][heads][128]")
+    if sel is not None and (sel.shape != (n, kv.n_kv_heads, budget) or n_sel is None or n_sel.numel() != n):
+        raise ValueError(f"sel must be [{n}][{kv.n_kv_heads}][budget], n_sel [{n}]")
+    return PPD_F32 if q.dtype is f32 else PPD_BF16
+
+
+def ppd_paged_attention(kv: PagedCache, layer: int, pt: PageTables, row_start, q, mask, out, ws, lse=None, sel=None,
+                        n_sel=None, stream=None):
+    """Attention of one layer's new rows over their sequences' pages (all, or those
+    of sel) and kv.tail: q, out bf16 or float32 [rows][heads][128], mask int64 /
+    uint64 [rows][2] (None: a row sees its sequence's rows up to itself), lse
+    float32 [rows][heads] (optional)."""
+    budget = sel.shape[2] if sel is not None and sel.dim() == 3 else 0
+    dt = _paged_rows(kv, pt, row_start, q, sel, n_sel, budget, (out, q.dtype, "out"), (lse, _dtypes()[1], "lse"),
+                     (mask, None, "mask"), (ws, None, "ws"))
+    n, nh, _ = q.shape
+    if out.shape != q.shape or (lse is not None and lse.shape != (n, nh)):
+        raise ValueError(f"out must be [{n}][{nh}][128], lse [{n}][{nh}]")
+    if mask is not None and mask.numel() * mask.element_size() < 16 * n:
+        raise ValueError(f"mask must be [{n}][2] words of 64 bits")
+    _check(lib().ppd_paged_attention(nh, C.byref(kv.desc), int(layer), C.byref(pt.desc), _ptr(row_start), n, _ptr(q), dt,
+                                     _ptr(mask) or None, _ptr(out), _ptr(lse) or None, _ptr(sel) or None,
+                                     _ptr(n_sel) if sel is not None else None, budget, _ptr(ws),
+                                     ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def ppd_paged_select_workspace_bytes(n_kv_heads: int, n_seqs: int, max_pages: int) -> int:
+    return _bytes(lib().ppd_paged_select_workspace_bytes(int(n_kv_heads), int(n_seqs), int(max_pages)))
+
+
+def ppd_paged_select(kv: PagedCache, layer: int, pt: PageTables, row_start, q, budget: int, n_first: int, n_last: int, sel,
+                     n_sel, ws, stream=None):
+    """The pages that matter most to each sequence's rows, a list for each kv head:
+    sel int32 [n_seqs][kv_heads][budget], n_sel int32 [n_seqs]."""
+    dt = _paged_rows(kv, pt, row_start, q, sel, n_sel, budget, (ws, None, "ws"))
+    _check(lib().ppd_paged_select(q.shape[1], C.byref(kv.desc), int(layer), C.byref(pt.desc), _ptr(row_start), q.shape[0],
+                                  _ptr(q), dt, int(budget), int(n_first), int(n_last), _ptr(sel), _ptr(n_sel), _ptr(ws),
+                                  ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def ppd_paged_workspace_bytes(model: Model, n_seqs: int, max_pages: int, n_rows: int, budget: int = 0) -> int:
+    return _bytes(lib().ppd_paged_workspace_bytes(C.byref(model.desc), int(n_seqs), int(max_pages), int(n_rows), int(budget)))
+
+
+def ppd_verify_batch_paged(model: Model, kv: PagedCache, pt: PageTables, row_start, ids, depth, mask, ws, logits, pred,
+                           budget: int = 0, n_first: int = 0, n_last: int = 0, stream=None):
+    """ppd_verify_batch on pages: the rows of all sequences, as many as ids holds;
+    budget > 0: attention to the pages that ppd_paged_select picks."""
+    import torch
+    i32 = torch.int32
+    kv._on_device((pt.table, None, "table"), (row_start, i32, "row_start"), (ids, i32, "ids"), (depth, i32, "depth"),
+                  (mask, None, "mask"), (ws, None, "ws"), (logits, torch.float32, "logits"), (pred, i32, "pred"))
+    n = ids.numel()
+    if row_start.numel() != pt.n_seqs + 1:
+        raise ValueError(f"row_start must be [{pt.n_seqs + 1}]")
+    for t, name, least in ((depth, "depth", n), (pred, "pred", n), (logits, "logits", n * model.shape.vocab)):
+        if t is not None and t.numel() < least:
+            raise ValueError(f"{name} holds {t.numel()} elements, not {least}")
+    if mask.numel() * mask.element_size() < 16 * n:
+        raise ValueError(f"mask must be [{n}][2] words of 64 bits")
+    _check(lib().ppd_verify_batch_paged(C.byref(model.desc), C.byref(kv.desc), C.byref(pt.desc), _ptr(row_start), n,
+                                        _ptr(ids), _ptr(depth), _ptr(mask), int(budget), int(n_first), int(n_last),
+                                        _ptr(ws), ws.numel() * ws.element_size(), _ptr(logits) or None, _ptr(pred),
+                                        _stream(stream)))
 
 
 def ppd_accept_sample_workspace_bytes(T: int, vocab: int) -> int:

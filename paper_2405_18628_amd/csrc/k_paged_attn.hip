@@ -1,0 +1,651 @@
+// Attention over a paged prefix and the new rows, lengths on the device.
+//
+// Rows.  The heads that share a kv head read the same keys, so a kv head's rows
+// are new row x head, r = t G + a (a < G), in 16-row tiles.
+//
+// Products (v_mfma_f32_16x16x32_bf16): S^T = K Q^T with the 32 keys of a block as
+// two 16-row A operands, O^T += V^T P^T with 16 dims as the A operand.  Pages hold
+// blocks in the order of these operands: 16 loads of 1 KB, straight into the
+// registers of the wave that multiplies them.  A wave's rows of S^T are the keys
+// that its lanes hold as the B operand of the second product.
+//
+// Work decomposition.  A workgroup takes a sequence, a kv head, up to RW rows and
+// one of KS key splits; its eight waves are QW side by side over tiles, NQ tiles
+// each, and PARS over blocks, with no barrier in the loop.  The grid is fixed by
+// what the host knows (sequences, rows); which part a workgroup takes it finds
+// from the lengths, every wave for itself: a sequence's share of kPagedSlots
+// workgroups follows its blocks, and sequences that get more than one leave
+// partial rows that a second launch adds in order.
+#include <algorithm>
+
+#include "ppd_paged.h"
+
+namespace {
+
+constexpr int NT = 512;              // eight waves
+constexpr int OROW = PPD_ATTN_OROW;  // partial row: 128 dims, m, l, padding (floats)
+constexpr float kLn2 = 0.69314718055994531f;
+
+// parts of a query and of a probability on the matrix cores: bfloat16 outputs
+// round to 2^-9, two parts of a probability leave 2^-17 of it; float32 calls
+// carry three parts of both, 2^-25
+__host__ __device__ constexpr int q_parts(int qt) { return qt == PAGED_Q_BF16 ? 1 : qt == PAGED_Q_F32 ? 3 : 2; }
+__host__ __device__ constexpr int p_parts(int qt) { return qt == PAGED_Q_F32 ? 3 : 2; }
+
+struct PTile {
+  uint64_t mk0, mk1;
+  floatx4 o[8];  // O^T: dims 16 dt + 4 (lane / 16) + e, row lane % 16
+  float m_run, l_run;
+};
+
+// v in PARTS bf16 parts, the largest first
+template <int PARTS>
+__device__ __forceinline__ void split8(const float (&v)[8], u32x4 (&out)[PARTS]) {
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = v[e];
+#pragma unroll
+  for (int part = 0; part < PARTS; ++part) {
+    out[part] = u32x4{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]), pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7])};
+    if (part + 1 < PARTS)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        r[e] -= __uint_as_float(e & 1 ? out[part][e >> 1] & 0xffff0000u : out[part][e >> 1] << 16);
+  }
+}
+
+// One block's scores (unscaled, hidden keys at -inf) into the running softmax:
+// the reference moves only when a maximum passes it by 8 (log2), P in pv.
+__device__ __forceinline__ void softmax_step(PTile &R, const float (&sv)[8], float c, float (&pv)[8]) {
+  const float lmax = c * fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])),
+                               fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+  if (__ballot(lmax > R.m_run + 8.f)) {
+    const float bmax = quad_max(lmax);
+    const bool need = bmax > R.m_run + 8.f;
+    const float alpha = need ? __builtin_amdgcn_exp2f(R.m_run - bmax) : 1.f;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) R.o[dt] *= alpha;
+    R.l_run *= alpha;
+    R.m_run = need ? bmax : R.m_run;
+  }
+  const float m_eff = R.m_run == -INFINITY ? 0.f : R.m_run;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    pv[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], c, -m_eff));
+    R.l_run += pv[e];
+  }
+}
+
+__device__ __forceinline__ int wave_incl(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o, 64);
+    v += lane >= o ? u : 0;
+  }
+  return v;
+}
+
+// a sequence's work: blocks of the prefix and of its rows, row groups
+struct Load {
+  int n4, nblk, grps, units;
+};
+__device__ __forceinline__ Load load_of(const PagedAttnLaunch &p, int s, const PagedSeq &q, int RW, bool *bad) {
+  Load w;
+  const int lb = p.sq.lp - 5, pages = (q.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
+  int n = (q.L + kPB - 1) / kPB;
+  if (p.sel) {
+    const int m = p.n_sel[s], most = min(pages, p.budget);
+    *bad |= m < 0 || m > most;
+    n = max(0, min(m, most)) << lb;
+  }
+  w.n4 = n;
+  w.nblk = n + (q.T + kPB - 1) / kPB;
+  w.grps = (q.T * (p.nh / p.nkv) + RW - 1) / RW;
+  w.units = w.grps * p.nkv;
+  return w;
+}
+// its splits: its share of kPagedSlots, PARS blocks a split at least.  Rounded
+// down, so the splits of all that have several are at most kPagedSlots.
+__device__ __forceinline__ int splits_of(const Load &w, int64_t total, int PARS) {
+  if (w.units == 0) return 0;
+  const int64_t share = (int64_t)kPagedSlots * w.nblk / max(total, (int64_t)1);
+  const int want = (int)max((int64_t)1, min(share, (int64_t)(w.nblk / PARS)));
+  const int chunk = (w.nblk + want - 1) / want;
+  return (w.nblk + chunk - 1) / chunk;
+}
+
+struct Place {
+  int sq, local, KS, part0;
+  PagedSeq q;
+  Load w;
+};
+// the workgroup's sequence and place in it; false: it has no part.  A wave's lanes
+// take a sequence each.
+__device__ bool find_place(const PagedAttnLaunch &p, int slot, int RW, int PARS, Place *out, bool *bad) {
+  const int lane = threadIdx.x & 63;
+  int64_t total = 0;
+  PagedSeq q{};
+  Load w{};
+  for (int base = 0; base < p.sq.B; base += 64) {
+    const int s = base + lane;
+    if (s < p.sq.B) {
+      q = paged_seq(p.sq, s, bad);
+      w = load_of(p, s, q, RW, bad);
+      total += (int64_t)w.units * w.nblk;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+  int slots0 = 0, parts0 = 0;
+  for (int base = 0; base < p.sq.B; base += 64) {
+    const int s = base + lane;
+    int KS = 0;
+    if (s < p.sq.B) {
+      if (p.sq.B > 64) {
+        q = paged_seq(p.sq, s, bad);
+        w = load_of(p, s, q, RW, bad);
+      }
+      KS = splits_of(w, total, PARS);
+    }
+    const int mine = s < p.sq.B ? w.units * KS : 0, parted = KS > 1 ? mine : 0;
+    const int upto = slots0 + wave_incl(mine), parts = parts0 + wave_incl(parted);
+    const uint64_t hit = __ballot(slot < upto);
+    if (hit) {
+      const int at = __builtin_ctzll(hit);
+      out->sq = base + at;
+      out->local = slot - __shfl(upto - mine, at, 64);
+      out->KS = __shfl(KS, at, 64);
+      out->part0 = __shfl(parts - parted, at, 64);
+      out->q = PagedSeq{__shfl(q.t0, at, 64), __shfl(q.T, at, 64), __shfl(q.L, at, 64)};
+      out->w = Load{__shfl(w.n4, at, 64), __shfl(w.nblk, at, 64), __shfl(w.grps, at, 64), __shfl(w.units, at, 64)};
+      return true;
+    }
+    slots0 = __shfl(upto, 63, 64);
+    parts0 = __shfl(parts, 63, 64);
+  }
+  return false;
+}
+
+template <int QT>
+__device__ __forceinline__ void load_query(const PagedAttnLaunch &p, int tok, int head, int lg, u32x4 (&q)[4][q_parts(QT)]) {
+#pragma unroll
+  for (int ds = 0; ds < 4; ++ds) {
+    if constexpr (QT == PAGED_Q_PLANES) {
+      const unsigned char *src = (const unsigned char *)p.q + plane_off(p.T_pad >> 4, tok, head * 128 + ds * 32 + lg * 8);
+      q[ds][0] = *(const u32x4 *)src;
+      q[ds][1] = *(const u32x4 *)(src + kPlaneLo);
+    } else if constexpr (QT == PAGED_Q_BF16) {
+      q[ds][0] = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + ds * 32 + lg * 8);
+    } else {
+      const float *src = (const float *)p.q + ((size_t)tok * p.nh + head) * 128 + ds * 32 + lg * 8;
+      const floatx4 a = *(const floatx4 *)src, b = *(const floatx4 *)(src + 4);
+      split8<3>({a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}, q[ds]);
+    }
+  }
+}
+
+template <int QT>
+__device__ __forceinline__ void store_out4(const PagedAttnLaunch &p, int tok, int head, int d4, floatx4 o) {
+  if constexpr (QT == PAGED_Q_PLANES)
+    store_plane4((unsigned char *)p.out, p.T_pad >> 4, tok, head * 128 + d4, {o[0], o[1], o[2], o[3]});
+  else if constexpr (QT == PAGED_Q_BF16)
+    *(u32x2 *)((bf16_t *)p.out + ((size_t)tok * p.nh + head) * 128 + d4) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+  else
+    *(floatx4 *)((float *)p.out + ((size_t)tok * p.nh + head) * 128 + d4) = o;
+}
+
+// table entries are read through the scalar cache: they are alike in a wave
+__device__ __forceinline__ int uniform_load(const int32_t *p, int64_t i) {
+  typedef const __attribute__((address_space(4))) int32_t cint;
+  return ((cint *)(uintptr_t)p)[i];
+}
+
+// NQ tiles a wave, QW waves side by side over tiles, PARS over blocks
+template <int NQ, int QW, int PARS, int QT>
+__global__ __launch_bounds__(NT, 1) void paged_attention_kernel(PagedAttnLaunch p) {
+  static_assert(QW * PARS * 64 == NT, "eight waves");
+  constexpr int RW = QW * NQ * 16;  // rows of the workgroup
+  constexpr int QP = q_parts(QT), PP = p_parts(QT);
+  constexpr bool QLDS = NQ > 1 || QP > 2;  // no registers left for the queries
+  // the waves' rows, after the main loop; before, the queries that lie in LDS
+  __shared__ __attribute__((aligned(16))) float rows_s[PARS][RW][OROW];
+  u32x4 *q_s = (u32x4 *)rows_s;  // [tile][ds][part][lane]
+  static_assert((size_t)QW * NQ * 4 * QP * 1024 <= sizeof(rows_s), "queries fit");
+  __shared__ float fac_s[RW][PARS];  // what a row's waves are added with
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qw = wave % QW, par = wave / QW;
+  const int lr = lane & 15, lg = lane >> 4;
+  Place pl;
+  bool bad = false;
+  const bool mine = find_place(p, blockIdx.x, RW, PARS, &pl, &bad);
+  if (bad && blockIdx.x == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
+  if (!mine) return;
+  const int sq = __builtin_amdgcn_readfirstlane(pl.sq), KS = __builtin_amdgcn_readfirstlane(pl.KS);
+  const int t0 = __builtin_amdgcn_readfirstlane(pl.q.t0), T = __builtin_amdgcn_readfirstlane(pl.q.T);
+  const int L = __builtin_amdgcn_readfirstlane(pl.q.L);
+  const int n4 = __builtin_amdgcn_readfirstlane(pl.w.n4), nblk = __builtin_amdgcn_readfirstlane(pl.w.nblk);
+  const int n_grp = __builtin_amdgcn_readfirstlane(pl.w.grps);
+  const int part0 = __builtin_amdgcn_readfirstlane(pl.part0);
+  int local = __builtin_amdgcn_readfirstlane(pl.local);
+  if (local == 0 && tid == 0) p.rec[sq] = int2{KS, part0};
+  const int my_part = part0 + local;
+  const int G = p.nh / p.nkv, R = T * G;
+  const int ks = local % KS;
+  local /= KS;
+  const int grp = local % n_grp, kvh = local / n_grp;
+  const int chunk = (nblk + KS - 1) / KS;
+  const int b0 = min(nblk, ks * chunk), b1 = min(nblk, b0 + chunk);
+  const int row0 = grp * RW;
+  const int lb = p.sq.lp - 5, n_pages = p.sq.n_pages;
+  const int last_page = max(0, ((L + (1 << p.sq.lp) - 1) >> p.sq.lp) - 1);
+  const int32_t *table = p.sq.table + (size_t)sq * p.sq.max_pages;
+  const int32_t *sel = p.sel ? p.sel + ((size_t)sq * p.nkv + kvh) * p.budget : nullptr;
+  const unsigned char *pages = p.pages + (size_t)kvh * ((size_t)kPBytes << lb);
+  const size_t page_bytes = (size_t)p.nkv * ((size_t)kPBytes << lb);
+
+  // a block of the prefix: its page's place in the table, then its address.  Past
+  // the wave's blocks the first one again (the same loads on every path)
+  const int end4 = min(b1, n4);
+  auto place_of = [&](int blk) {
+    const int i = (blk < end4 ? blk : min(b0, max(0, n4 - 1))) >> lb;
+    return sel ? max(0, min(uniform_load(sel, i), last_page)) : i;
+  };
+  auto address_of = [&](int blk, int place) {
+    const int b = blk < end4 ? blk : min(b0, max(0, n4 - 1));
+    const int page = paged_clamp(uniform_load(table, place), n_pages);
+    return pages + (size_t)page * page_bytes + (size_t)(b & ((1 << lb) - 1)) * kPBytes;
+  };
+  u32x4 kf[2][4], vf[8];
+  auto load_keys = [&](const unsigned char *src) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int ds = 0; ds < 4; ++ds) kf[t][ds] = *(const u32x4 *)(src + (t * 4 + ds) * 1024 + lane * 16);
+  };
+  auto load_values = [&](const unsigned char *src) {
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) vf[dt] = *(const u32x4 *)(src + 2 * kPElems + dt * 1024 + lane * 16);
+  };
+  int blk = b0 + par;
+  int place = 0, next_place = 0;
+  const unsigned char *addr = pages, *next_addr = pages;
+  if (n4 > 0) {
+    place = place_of(blk);
+    next_place = place_of(blk + PARS);
+    addr = address_of(blk, place);
+    load_keys(addr);
+    load_values(addr);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+
+  PTile rt[NQ];
+  u32x4 qr[4][QP];  // the queries, where registers hold them
+  const int n_live = min(NQ, ((min(R - row0, RW) + 15) / 16 - qw + QW - 1) / QW);
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int r = row0 + (qw + QW * i) * 16 + lr, rc = min(r, R - 1);
+    const int t = rc / G, tok = t0 + t, head = kvh * G + rc % G;
+    const bool live = r < R;
+    u32x4 q[4][QP];
+    load_query<QT>(p, tok, head, lg, q);
+    uint64_t m0, m1;
+    if (p.mask) {
+      m0 = p.mask[2 * (size_t)tok];
+      m1 = p.mask[2 * (size_t)tok + 1];
+    } else {  // its sequence's rows up to itself
+      m0 = t >= 63 ? ~0ull : (2ull << t) - 1;
+      m1 = t < 64 ? 0ull : t >= 127 ? ~0ull : (2ull << (t - 64)) - 1;
+    }
+    rt[i].mk0 = live ? m0 : 0ull;
+    rt[i].mk1 = live ? m1 : 0ull;
+#pragma unroll
+    for (int ds = 0; ds < 4; ++ds)
+#pragma unroll
+      for (int part = 0; part < QP; ++part) {
+        if constexpr (!QLDS)
+          qr[ds][part] = q[ds][part];
+        else if (par == 0)
+          q_s[(((qw + QW * i) * 4 + ds) * QP + part) * 64 + lane] = q[ds][part];
+      }
+    if constexpr (QLDS) __builtin_amdgcn_sched_barrier(0);  // (registers: a tile's queries at a time)
+  }
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) rt[i].o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    rt[i].m_run = -INFINITY;
+    rt[i].l_run = 0.f;
+  }
+  if constexpr (QLDS) __syncthreads();  // the queries are in LDS
+  auto query = [&](int i, int ds, int part) {
+    if constexpr (!QLDS)
+      return as_bf16x8(qr[ds][part]);
+    else
+      return as_bf16x8(q_s[(((qw + QW * i) * 4 + ds) * QP + part) * 64 + lane]);
+  };
+  const float c = p.scale_log2;
+  // S^T of the keys in kf, smallest parts first
+  auto scores = [&](float (&sv)[NQ][8]) {
+    floatx4 acc[NQ][2];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) acc[i][0] = acc[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int part = QP - 1; part >= 0; --part) {
+#pragma unroll
+      for (int ds = 0; ds < 4; ++ds)
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          const bf16x8 q = query(i, ds, part);
+          acc[i][0] = mfma16x16x32(as_bf16x8(kf[0][ds]), q, acc[i][0]);
+          acc[i][1] = mfma16x16x32(as_bf16x8(kf[1][ds]), q, acc[i][1]);
+        }
+      if constexpr (QLDS && QP > 1) __builtin_amdgcn_sched_barrier(0);  // (registers: one part's queries at a time)
+    }
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sv[i][u] = acc[i][u >> 2][u & 3];
+  };
+  // O^T += V^T P^T of the values in vf
+  auto products = [&](const u32x4 (&pf)[NQ][PP]) {
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+      for (int part = PP - 1; part >= 0; --part)
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+          rt[i].o[dt] = mfma16x16x32(as_bf16x8(vf[dt]), as_bf16x8(pf[i][part]), rt[i].o[dt]);
+  };
+
+  if (n_live > 0) {
+    for (; blk < end4; blk += PARS) {
+      // the block after next's place, the next one's address
+      next_addr = address_of(blk + PARS, next_place);
+      const int after = place_of(blk + 2 * PARS);
+      float sv[NQ][8];
+      scores(sv);
+      __builtin_amdgcn_sched_barrier(0);
+      load_keys(next_addr);
+      __builtin_amdgcn_sched_barrier(0);
+      const int pos = (place << p.sq.lp) + (blk & ((1 << lb) - 1)) * kPB;
+      const int vis = L - pos - 8 * lg;  // the lane's keys below the length
+      if (pos + kPB > L) {  // the prefix ends in this block, or before it
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+          for (int u = 0; u < 8; ++u) sv[i][u] = u < vis ? sv[i][u] : -INFINITY;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)  // (0 times what lies there may be NaN)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) vf[dt][w] &= (2 * w < vis ? 0xffffu : 0u) | (2 * w + 1 < vis ? 0xffff0000u : 0u);
+      }
+      u32x4 pf[NQ][PP];
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        float pv[8];
+        softmax_step(rt[i], sv[i], c, pv);
+        split8<PP>(pv, pf[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      products(pf);
+      __builtin_amdgcn_sched_barrier(0);
+      load_values(next_addr);
+      __builtin_amdgcn_sched_barrier(0);
+      place = next_place;
+      next_place = after;
+    }
+    // the new rows, straight from the tail
+    const bf16_t *tk = p.tk + (size_t)kvh * p.tcap * 128, *tv = p.tv + (size_t)kvh * 128 * p.tcap;
+    for (; blk < b1; blk += PARS) {
+      const int k0 = (blk - n4) * kPB;
+      const int j0 = k0 + 8 * lg, keep_n = max(0, min(8, T - j0));  // keys of the lane that exist
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16_t *row = tk + (size_t)min(t0 + k0 + paged_key_of(t, lr), p.tcap - 1) * 128 + lg * 8;
+#pragma unroll
+        for (int ds = 0; ds < 4; ++ds) kf[t][ds] = *(const u32x4 *)(row + ds * 32);
+      }
+      // (a sequence's rows start anywhere: elements one by one where not by eights)
+      const int c0 = t0 + j0;
+      if (t0 % 8 == 0) {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+          vf[dt] = *(const u32x4 *)(tv + (size_t)(16 * dt + lr) * p.tcap + min(c0, p.tcap - 8));
+      } else {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          const bf16_t *row = tv + (size_t)(16 * dt + lr) * p.tcap;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            vf[dt][w] = row[min(c0 + 2 * w, p.tcap - 1)] | (uint32_t)row[min(c0 + 2 * w + 1, p.tcap - 1)] << 16;
+        }
+      }
+      float sv[NQ][8];
+      scores(sv);
+      u32x4 pf[NQ][PP];
+      uint32_t seen[NQ];
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const uint64_t win = j0 >= 128 ? 0ull : j0 >= 64 ? rt[i].mk1 >> (j0 - 64) : rt[i].mk0 >> j0;
+        seen[i] = (uint32_t)win & ((1u << keep_n) - 1u);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sv[i][u] = (seen[i] >> u) & 1u ? sv[i][u] : -INFINITY;
+        float pv[8];
+        softmax_step(rt[i], sv[i], c, pv);
+        split8<PP>(pv, pf[i]);
+      }
+      uint32_t end = 0;  // bit 15 of a half: an exponent of all ones
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          vf[dt][w] &= (2 * w < keep_n ? 0xffffu : 0u) | (2 * w + 1 < keep_n ? 0xffff0000u : 0u);
+          end |= (vf[dt][w] & 0x7fff7fffu) + 0x00800080u;
+        }
+      if (__ballot(end & 0x80008000u)) {
+        // infinities and NaN must not reach the rows that do not see them (0
+        // times them is NaN): they are taken out, and the rows that see one
+        // get NaN
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          u32x4 odd;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            odd[w] = ((((vf[dt][w] & 0x7fff7fffu) + 0x00800080u) >> 15) & 0x00010001u) * 0x3f80u;  // 1.0 where one is
+            vf[dt][w] &= ~(odd[w] / 0x3f80u * 0xffffu);
+          }
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) {
+            u32x4 on;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              on[w] = (seen[i] >> (2 * w) & 1u ? 0x3f80u : 0u) | (seen[i] >> (2 * w + 1) & 1u ? 0x3f800000u : 0u);
+            const floatx4 n = mfma16x16x32(as_bf16x8(odd), as_bf16x8(on), floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rt[i].o[dt][e] = n[e] > 0.f ? NAN : rt[i].o[dt][e];
+          }
+        }
+      }
+      products(pf);
+    }
+  }
+
+  if constexpr (QLDS) __syncthreads();  // the queries' LDS is free
+  // ---- the waves meet in LDS: thread -> row tid / 32 + 16 n, dims 4 (tid % 32) .. + 3
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const float l = quad_sum(rt[i].l_run);
+    if (i < n_live) {
+      float *row = rows_s[par][(qw + QW * i) * 16 + lr];
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) *(floatx4 *)(row + dt * 16 + lg * 4) = rt[i].o[dt];
+      if (lg == 0) *(float2 *)(row + 128) = float2{rt[i].m_run, l};
+    }
+  }
+  __syncthreads();
+  const int n_rows = min(R - row0, RW);
+  float *part = p.part + (size_t)my_part * RW * OROW;  // (only with several splits)
+  if (tid < n_rows) {
+    float2 ml[PARS];
+    float M = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) {
+      ml[w] = *(const float2 *)(rows_s[w][tid] + 128);
+      M = fmaxf(M, ml[w].x);
+    }
+    float f[PARS];
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) {
+      // (a wave that sees NaN alone has no maximum: its sum is kept as it is)
+      f[w] = ml[w].x == -INFINITY ? (ml[w].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[w].x - M);
+      l += f[w] * ml[w].y;
+    }
+    const float inv = KS > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) fac_s[tid][w] = f[w] * inv;
+    if (KS > 1) {
+      *(float2 *)(part + (size_t)tid * OROW + 128) = float2{M, l};
+    } else if (p.lse) {
+      const int r = row0 + tid;
+      p.lse[(size_t)(t0 + r / G) * p.nh + kvh * G + r % G] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+    }
+  }
+  __syncthreads();
+  const int d4 = (tid & 31) * 4;
+#pragma unroll 2
+  for (int rl = tid >> 5; rl < n_rows; rl += NT / 32) {
+    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < PARS; ++w) o += fac_s[rl][w] * *(const floatx4 *)(rows_s[w][rl] + d4);
+    if (KS > 1) {
+      *(floatx4 *)(part + (size_t)rl * OROW + d4) = o;
+    } else {
+      const int r = row0 + rl;
+      store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, o);
+    }
+  }
+}
+
+// the splits of a row, added in order; 32 threads a row
+template <int QT>
+__global__ __launch_bounds__(NT) void paged_merge_kernel(PagedAttnLaunch p, int RW) {
+  const int64_t first = (int64_t)blockIdx.x * (NT / 32) + 2 * (threadIdx.x >> 6);  // the wave's first row
+  const int64_t n_rows = (int64_t)p.sq.n_rows * p.nh;
+  const int d4 = (threadIdx.x & 31) * 4;
+  int sq = -1, tok = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t at = first + h;
+    if (at >= n_rows) break;
+    const int t = (int)(at / p.nh), s = paged_seq_of(p.sq.row_start, p.sq.B, t);
+    if ((int)(threadIdx.x >> 5 & 1) == h) sq = s, tok = t;
+  }
+  if (sq < 0) return;
+  bool bad = false;
+  const PagedSeq q = paged_seq(p.sq, sq, &bad);
+  const int2 rec = p.rec[sq];
+  const int head = (int)(first + (threadIdx.x >> 5 & 1) - (int64_t)tok * p.nh), t = tok - q.t0;
+  const int KS = rec.x, G = p.nh / p.nkv;
+  if (t < 0 || t >= q.T || KS <= 1) return;  // no sequence's row, or already final
+  const int kvh = head / G, r = t * G + head % G, grps = (q.T * G + RW - 1) / RW;
+  const int slot0 = rec.y + (kvh * grps + r / RW) * KS;
+  const float *part = p.part + ((size_t)slot0 * RW + r % RW) * OROW;
+  const size_t stride = (size_t)RW * OROW;
+  constexpr int N = 8;  // rows in flight: one round trip for all of them
+  float M = -INFINITY, l = 0.f;
+  floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < KS; s0 += N) {
+    float2 ml[N];
+    floatx4 x[N];
+#pragma unroll
+    for (int v = 0; v < N; ++v) {
+      const float *row = part + min(s0 + v, KS - 1) * stride;
+      ml[v] = *(const float2 *)(row + 128);
+      x[v] = *(const floatx4 *)(row + d4);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    float m = M;
+#pragma unroll
+    for (int v = 0; v < N; ++v) m = fmaxf(m, ml[v].x);  // (the last row repeats)
+    const float keep = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - m);
+    o *= keep;
+    l *= keep;
+    M = m;
+#pragma unroll
+    for (int v = 0; v < N; ++v) {
+      const float f = ml[v].x == -INFINITY ? (ml[v].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[v].x - M);
+      l += s0 + v < KS ? f * ml[v].y : 0.f;
+      if (s0 + v < KS) o += f * x[v];
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  store_out4<QT>(p, tok, head, d4, o * inv);
+  if (p.lse && d4 == 0) p.lse[(size_t)tok * p.nh + head] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+}
+
+}  // namespace
+
+// 16-row tiles a wave holds and waves side by side, by the tiles of a kv head
+static void paged_shape(int tiles, int *nq, int *qw) {
+  *nq = tiles <= 1 ? 1 : 2;
+  *qw = tiles <= 2 ? 1 : tiles <= 4 ? 2 : 4;
+}
+// (a rule on the rows of an average sequence: how many a single one has is only
+// known on the device, and any shape serves any number)
+static int paged_tiles(int nh, int nkv, int B, int n_rows) {
+  const int64_t rows = std::min<int64_t>((n_rows + B - 1) / B, PPD_T_MAX) * (nh / nkv);
+  return (int)std::min<int64_t>(64, (rows + 15) / 16);
+}
+
+size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows) {
+  int nq, qw;
+  paged_shape(paged_tiles(nh, nkv, B, n_rows), &nq, &qw);
+  return (size_t)kPagedSlots * 16 * nq * qw * OROW * sizeof(float);
+}
+
+void paged_attn_shape(PagedAttnLaunch &a) {
+  a.tiles = paged_tiles(a.nh, a.nkv, a.sq.B, a.sq.n_rows);
+  int nq, qw;
+  paged_shape(a.tiles, &nq, &qw);
+  const int most = a.sel ? std::min(a.budget, a.sq.max_pages) : a.sq.max_pages;
+  a.may_split = ((int64_t)most << (a.sq.lp - 5)) + PPD_T_MAX / kPB >= 2 * (8 / qw);
+}
+
+template <int QT>
+static hipError_t launch_attn(const PagedAttnLaunch &a, hipStream_t s) {
+  auto kernel = a.tiles <= 1   ? paged_attention_kernel<1, 1, 8, QT>
+                : a.tiles <= 2 ? paged_attention_kernel<2, 1, 8, QT>
+                : a.tiles <= 4 ? paged_attention_kernel<2, 2, 4, QT>
+                               : paged_attention_kernel<2, 4, 2, QT>;
+  int nq, qw;
+  paged_shape(a.tiles, &nq, &qw);
+  const int rw = 16 * nq * qw;
+  // row groups of all sequences at most, and the splits of those that have several
+  const int64_t rows = (int64_t)a.sq.n_rows * (a.nh / a.nkv);
+  const int64_t units = a.nkv * (std::min<int64_t>(a.sq.B, a.sq.n_rows) + rows / rw);
+  const int64_t grid = units + (a.may_split ? kPagedSlots : 0);
+  const hipEvent_t ev0 = (hipEvent_t)a.ev_start, ev1 = (hipEvent_t)a.ev_stop;
+  if (ev0)
+    hipExtLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NT), 0, s, ev0, a.may_split ? (hipEvent_t) nullptr : ev1, 0, a);
+  else
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NT), 0, s, a);
+  if (a.may_split) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const dim3 merge((unsigned)(((int64_t)a.sq.n_rows * a.nh + NT / 32 - 1) / (NT / 32)));
+    if (ev1)
+      hipExtLaunchKernelGGL(paged_merge_kernel<QT>, merge, dim3(NT), 0, s, (hipEvent_t) nullptr, ev1, 0, a, rw);
+    else
+      hipLaunchKernelGGL(paged_merge_kernel<QT>, merge, dim3(NT), 0, s, a, rw);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_attn(const PagedAttnLaunch &a, hipStream_t s) {
+  return a.q_type == PAGED_Q_PLANES ? launch_attn<PAGED_Q_PLANES>(a, s)
+         : a.q_type == PAGED_Q_F32  ? launch_attn<PAGED_Q_F32>(a, s)
+                                    : launch_attn<PAGED_Q_BF16>(a, s);
+}

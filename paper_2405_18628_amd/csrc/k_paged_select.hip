@@ -1,0 +1,285 @@
+// Pages of a long prefix by a score of their key bounds.
+//
+// A page's keys k of a head lie between its bounds, so a query's product with any
+// of them is at most sum_d max(q_d, 0) largest_d + min(q_d, 0) smallest_d; summed
+// over the rows and heads that share the choice, with Qp and Qm the sums of their
+// positive and negative parts, it is one product of 256 elements a page whatever
+// the number of rows.  Its sums are float64: pages' scores lie close together,
+// and whole numbers hang on their order.
+//
+// Scores: a wave takes 16 pages, two at a time (512 bytes of bounds a page, 16
+// bytes a lane), all requested before the first is used; bound by reading them.
+// Selection: a workgroup for each (sequence, kv head) narrows the threshold
+// among the scores' ordered 64-bit keys 8 bits at a time, from the first bit in
+// which any two differ on (scores share sign and most of the exponent).
+#include <algorithm>
+
+#include "ppd_paged.h"
+
+namespace {
+
+typedef unsigned long long u64;
+
+constexpr int ST = 256;    // threads of the scores' workgroup
+constexpr int PAGES = 16;  // pages of a wave
+constexpr int CH = PAGES * (ST / 64);
+
+// the order of numbers as unsigned keys; NaN first of all
+__device__ __forceinline__ u64 key_of(double v) {
+  if (v != v) return 0;
+  const u64 b = __builtin_bit_cast(u64, v + 0.0);  // -0 as 0
+  return b >> 63 ? ~b : b | 0x8000000000000000ull;
+}
+
+// 8 elements of a query row
+template <int QT>
+__device__ __forceinline__ void query8(const PagedSelectLaunch &p, int tok, int head, int d, float (&v)[8]) {
+  if constexpr (QT == PAGED_Q_F32) {
+    const float *src = (const float *)p.q + ((size_t)tok * p.nh + head) * 128 + d;
+    const floatx4 a = *(const floatx4 *)src, b = *(const floatx4 *)(src + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+  } else if constexpr (QT == PAGED_Q_BF16) {
+    const u32x4 a = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? a[e >> 1] & 0xffff0000u : a[e >> 1] << 16);
+  } else {
+    const unsigned char *src = (const unsigned char *)p.q + plane_off(p.T_pad >> 4, tok, head * 128 + d);
+    const u32x4 a = *(const u32x4 *)src, b = *(const u32x4 *)(src + kPlaneLo);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      v[e] = __uint_as_float(e & 1 ? a[e >> 1] & 0xffff0000u : a[e >> 1] << 16) +
+             __uint_as_float(e & 1 ? b[e >> 1] & 0xffff0000u : b[e >> 1] << 16);
+  }
+}
+
+template <int QT>
+__global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, int chunks) {
+  __shared__ double sum_s[ST / 16][2][128];
+  __shared__ double q_s[2][128];  // Qm, Qp
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int c = blockIdx.x % chunks, kvh = blockIdx.x / chunks % p.nkv, sq = blockIdx.x / chunks / p.nkv;
+  bool bad = false;
+  const PagedSeq s = paged_seq(p.sq, sq, &bad);
+  if (bad && c == 0 && tid == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
+  const int n = (s.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
+  if (n <= p.budget || c * CH >= n) return;  // all are taken
+  const int page0 = c * CH + (tid >> 6) * PAGES;
+  // ---- this wave's bounds
+  const int32_t *table = p.sq.table + (size_t)sq * p.sq.max_pages;
+  const int phys = paged_clamp(table[min(page0 + (lane & (PAGES - 1)), n - 1)], p.sq.n_pages);
+  u32x4 w[PAGES / 2];
+#pragma unroll
+  for (int i = 0; i < PAGES / 2; ++i) {
+    const int page = __shfl(phys, 2 * i + (lane >> 5), 64);
+    w[i] = *(const u32x4 *)(p.bounds + ((size_t)page * p.nkv + kvh) * 256 + (lane & 31) * 8);
+  }
+  // ---- sums of the queries' positive and negative parts
+  const int G = p.nh / p.nkv, R = s.T * G, d8 = (tid & 15) * 8;
+  double qp[8], qm[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) qp[e] = qm[e] = 0.0;
+#pragma unroll 4
+  for (int r = tid >> 4; r < R; r += ST / 16) {
+    float v[8];
+    query8<QT>(p, s.t0 + r / G, kvh * G + r % G, d8, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      qp[e] += (double)(v[e] <= 0.f ? 0.f : v[e]);  // (a NaN stays one)
+      qm[e] += (double)(v[e] >= 0.f ? 0.f : v[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    sum_s[tid >> 4][0][d8 + e] = qm[e];
+    sum_s[tid >> 4][1][d8 + e] = qp[e];
+  }
+  __syncthreads();
+  {
+    double x = 0.0;
+#pragma unroll
+    for (int i = 0; i < ST / 16; ++i) x += sum_s[i][tid >> 7][tid & 127];
+    q_s[tid >> 7][tid & 127] = x;
+  }
+  __syncthreads();
+  double q[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q[e] = q_s[lane >> 4 & 1][(lane & 15) * 8 + e];
+  // ---- products, summed over a page's 32 lanes
+  double v[PAGES / 2];
+#pragma unroll
+  for (int i = 0; i < PAGES / 2; ++i) {
+    double x = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      x = fma(q[e], (double)__uint_as_float(e & 1 ? w[i][e >> 1] & 0xffff0000u : w[i][e >> 1] << 16), x);
+    v[i] = x;
+  }
+  // each step halves the pages a lane holds: after three, lane bits 4, 3, 2 say which
+#pragma unroll
+  for (int step = 0; step < 3; ++step) {
+    const int o = 16 >> step, half = (PAGES / 4) >> step;
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const bool up = lane & o;
+      const double mine = up ? v[i + half] : v[i], other = up ? v[i] : v[i + half];
+      v[i] = mine + __shfl_xor(other, o, 64);
+    }
+  }
+  double x = v[0];
+  x += __shfl_xor(x, 2, 64);
+  x += __shfl_xor(x, 1, 64);
+  const int i = (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1);
+  const int page = page0 + 2 * i + (lane >> 5);
+  if ((lane & 3) == 0 && page < n) {
+    const bool kept = page < p.n_first || page >= n - p.n_last;
+    p.keys[((size_t)sq * p.nkv + kvh) * p.sq.max_pages + page] = kept ? ~0ull : key_of(x);
+  }
+}
+
+constexpr int KT = 1024;  // threads of the selection
+constexpr int REG = 8;    // keys a thread holds; of more, the passes read them again
+
+__global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
+  __shared__ u64 red_s[2][KT / 64];
+  __shared__ unsigned hist_s[256];
+  __shared__ int cnt_s[KT / 64], bin_s, above_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int kvh = blockIdx.x % p.nkv, sq = blockIdx.x / p.nkv;
+  bool bad = false;
+  const PagedSeq s = paged_seq(p.sq, sq, &bad);
+  const int n = (s.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
+  int32_t *sel = p.sel + ((size_t)sq * p.nkv + kvh) * p.budget;
+  if (kvh == 0 && tid == 0) p.n_sel[sq] = min(n, p.budget);
+  if (n <= p.budget) {
+    for (int i = tid; i < n; i += KT) sel[i] = i;
+    return;
+  }
+  const u64 *keys = p.keys + ((size_t)sq * p.nkv + kvh) * p.sq.max_pages;
+  u64 kr[REG];
+#pragma unroll
+  for (int j = 0; j < REG; ++j) kr[j] = keys[min(j * KT + tid, n - 1)];
+  const int rounds = (n + KT - 1) / KT;
+  // f(key, index) of this thread's pages, rising
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < REG; ++j)
+      if (j * KT + tid < n) f(kr[j], j * KT + tid);
+    for (int j = REG; j < rounds; ++j)
+      if (j * KT + tid < n) f(keys[j * KT + tid], j * KT + tid);
+  };
+  // ---- the bits in which keys differ
+  u64 all = ~0ull, any = 0;
+  each([&](u64 k, int) { all &= k, any |= k; });
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    all &= __shfl_xor(all, o, 64);
+    any |= __shfl_xor(any, o, 64);
+  }
+  if (lane == 0) red_s[0][wave] = all, red_s[1][wave] = any;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < KT / 64; ++i) all &= red_s[0][i], any |= red_s[1][i];
+  const u64 diff = all ^ any;
+  // ---- the threshold: keys whose bits from `shift` up are above `prefix` are taken,
+  // of those that equal it `left` (from the smallest index on)
+  int shift = diff ? 64 - __builtin_clzll(diff) : 0, left = p.budget;
+  u64 prefix = shift == 64 ? 0 : all >> shift;
+  bool split = diff != 0;  // keys at the threshold are not all taken
+  while (split && shift > 0) {
+    const int bits = min(8, shift), low = shift - bits;
+    if (tid < 256) hist_s[tid] = 0;
+    __syncthreads();
+    each([&](u64 k, int) {
+      if (shift == 64 || k >> shift == prefix) atomicAdd(&hist_s[(k >> low) & ((1u << bits) - 1)], 1u);
+    });
+    __syncthreads();
+    if (wave == 0) {  // lane: bins 255 - 4 lane .. 252 - 4 lane, the largest first
+      unsigned h[4], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += h[j] = hist_s[255 - 4 * lane - j];
+      unsigned upto = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const unsigned u = __shfl_up(upto, o, 64);
+        upto += lane >= o ? u : 0;
+      }
+      unsigned before = upto - sum;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (before < (unsigned)left && before + h[j] >= (unsigned)left) {
+          bin_s = 255 - 4 * lane - j;
+          above_s = (int)before;
+        }
+        before += h[j];
+      }
+    }
+    __syncthreads();
+    const int bin = bin_s;
+    left -= above_s;
+    split = hist_s[bin] != (unsigned)left;
+    prefix = (shift == 64 ? 0 : prefix << bits) | (u64)bin;
+    shift = low;
+    __syncthreads();
+  }
+  // ---- the taken pages in order
+  int done = 0, ties = 0;  // written, and met at the threshold, in the rounds before
+  for (int j = 0; j < rounds; ++j) {
+    const int i = j * KT + tid;
+    u64 k = 0;
+    if (j < REG) {
+#pragma unroll
+      for (int r = 0; r < REG; ++r) k = r == j ? kr[r] : k;
+    } else if (i < n) {
+      k = keys[i];
+    }
+    const u64 top = shift == 64 ? 0 : k >> shift;
+    const bool tie = i < n && top == prefix;
+    bool take = i < n && top > prefix;
+    const u64 tb = __ballot(tie);
+    if (lane == 0) cnt_s[wave] = __popcll(tb);
+    __syncthreads();
+    int before = ties, sum = 0;
+#pragma unroll
+    for (int w = 0; w < KT / 64; ++w) {
+      before += w < wave ? cnt_s[w] : 0;
+      sum += cnt_s[w];
+    }
+    ties += sum;
+    take |= tie && before + __popcll(tb & ((1ull << lane) - 1)) < left;
+    __syncthreads();
+    const u64 b = __ballot(take);
+    if (lane == 0) cnt_s[wave] = __popcll(b);
+    __syncthreads();
+    int at = done;
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < KT / 64; ++w) {
+      at += w < wave ? cnt_s[w] : 0;
+      sum += cnt_s[w];
+    }
+    done += sum;
+    at += __popcll(b & ((1ull << lane) - 1));
+    if (take) sel[at] = i;
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+size_t paged_select_key_bytes(int nkv, int B, int max_pages) { return (size_t)B * nkv * max_pages * sizeof(u64); }
+
+hipError_t launch_paged_select(const PagedSelectLaunch &p, hipStream_t s) {
+  if (p.sq.max_pages > p.budget) {
+    const int chunks = (p.sq.max_pages + CH - 1) / CH;
+    const dim3 grid((unsigned)((int64_t)chunks * p.nkv * p.sq.B));
+    auto kernel = p.q_type == PAGED_Q_PLANES ? paged_score_kernel<PAGED_Q_PLANES>
+                  : p.q_type == PAGED_Q_F32  ? paged_score_kernel<PAGED_Q_F32>
+                                             : paged_score_kernel<PAGED_Q_BF16>;
+    hipLaunchKernelGGL(kernel, grid, dim3(ST), 0, s, p, chunks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(paged_pick_kernel, dim3(p.nkv * p.sq.B), dim3(KT), 0, s, p);
+  return hipGetLastError();
+}

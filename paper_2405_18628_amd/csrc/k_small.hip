@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const WT *__restrict__ tok_e
                                                     const WT *__restrict__ prompt_emb,
                                                     const int32_t *__restrict__ ids,
                                                     const int32_t *__restrict__ depth, SeqBatch sb,
-                                                    int d, float base, float2 *__restrict__ rope,
+                                                    DevSeqs dev, int d, float base, float2 *__restrict__ rope,
                                                     int vocab, int n_prompt, int H,
                                                     float *__restrict__ x,
                                                     const bf16_t *__restrict__ gain,
@@ -36,6 +36,14 @@ __global__ __launch_bounds__(256) void embed_kernel(const WT *__restrict__ tok_e
   {
     int L = sb.L[0];  // the cached length of token t's sequence
     for (int j = 1; j < sb.B; ++j) L = t >= sb.t0[j] ? sb.L[j] : L;
+    if (dev.row_start) {  // the last sequence that starts at or before t
+      int n = 0;
+      for (int j = 0; j < dev.B; j += PPD_WAVE) {
+        const int s = j + (threadIdx.x & (PPD_WAVE - 1));
+        n += __popcll(__ballot(s < dev.B && dev.row_start[min(s, dev.B - 1)] <= t));
+      }
+      L = max(0, min(dev.len[max(0, n - 1)], PPD_CAPACITY_MAX));
+    }
     for (int i = threadIdx.x; i < d / 2; i += blockDim.x) {
       const double pos = t < T ? (double)L + (double)depth[t] : 0.0;
       const double inv = exp(-(2.0 * i / d) * log((double)base));
@@ -112,18 +120,18 @@ __global__ __launch_bounds__(256) void embed_kernel(const WT *__restrict__ tok_e
 }
 
 hipError_t launch_embed(int dtype, const void *tok_emb, const void *prompt_emb, const int32_t *ids,
-                        const int32_t *depth, const SeqBatch &sb, int d, float base, float2 *rope,
-                        int vocab, int n_prompt, int H, float *x, const bf16_t *gain,
+                        const int32_t *depth, const SeqBatch &sb, const DevSeqs &dev, int d, float base,
+                        float2 *rope, int vocab, int n_prompt, int H, float *x, const bf16_t *gain,
                         unsigned char *planes, float *ss, uint32_t *ctr, size_t n_ctr,
                         uint32_t *status, hipStream_t s) {
   const int T_pad = (sb.t0[sb.B] + 15) & ~15;
   if (dtype == PPD_BF16) {
     hipLaunchKernelGGL(embed_kernel<bf16_t>, dim3(T_pad), dim3(256), 0, s, (const bf16_t *)tok_emb,
-                       (const bf16_t *)prompt_emb, ids, depth, sb, d, base, rope, vocab, n_prompt, H, x,
+                       (const bf16_t *)prompt_emb, ids, depth, sb, dev, d, base, rope, vocab, n_prompt, H, x,
                        gain, planes, ss, ctr, n_ctr, status);
   } else {
     hipLaunchKernelGGL(embed_kernel<float>, dim3(T_pad), dim3(256), 0, s, (const float *)tok_emb,
-                       (const float *)prompt_emb, ids, depth, sb, d, base, rope, vocab, n_prompt, H, x,
+                       (const float *)prompt_emb, ids, depth, sb, dev, d, base, rope, vocab, n_prompt, H, x,
                        (const bf16_t *)nullptr, (unsigned char *)nullptr, (float *)nullptr,
                        (uint32_t *)nullptr, (size_t)0, status);
   }

@@ -13,6 +13,7 @@
 #include <string>
 
 #include "ppd_kvq.h"
+#include "ppd_paged.h"
 #include "ppd_sample.h"
 
 namespace {
@@ -430,12 +431,35 @@ SeqBatch seq_batch(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t *
   return sb;
 }
 
-// the step on 4-bit caches (kvq set): the caches of `kvs` are the staging
-// caches, in which the trees start at position 0 (Ls = 0)
+// the memory behind a step's own that the paged one needs, by offsets from there
+struct PagedWs {
+  size_t rec, part, keys, sel, n_sel, total;
+};
+PagedWs paged_layout(const ppd_model *m, int n_seqs, int max_pages, int n_rows, int budget) {
+  PagedWs w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += align_up(bytes);
+    return o;
+  };
+  w.rec = take(sizeof(int2) * n_seqs);
+  w.part = take(paged_attn_part_bytes(m->n_heads, m->n_kv_heads, n_seqs, n_rows));
+  w.keys = take(budget ? paged_select_key_bytes(m->n_kv_heads, n_seqs, max_pages) : 0);
+  w.sel = take(budget ? sizeof(int32_t) * n_seqs * m->n_kv_heads * budget : 0);
+  w.n_sel = take(budget ? sizeof(int32_t) * n_seqs : 0);
+  w.total = off;
+  return w;
+}
+
+// the step on 4-bit caches (kvq set) or on pages (paged set): the caches of
+// `kvs` are the staging caches, in which the rows start at position 0 (Ls = 0);
+// on pages there is one for all sequences, B = 1
 ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t *Ls,
                      const int32_t *Ts, const int32_t *ids, const int32_t *depth,
                      const uint64_t *mask, void *ws, const WsLayout &w, float *logits,
-                     int32_t *pred, hipStream_t s, const KvqStep *kvq = nullptr) {
+                     int32_t *pred, hipStream_t s, const KvqStep *kvq = nullptr,
+                     const PagedStep *paged = nullptr) {
   const int H = m->hidden, nh = m->n_heads, nkv = m->n_kv_heads;
   int T = 0;
   for (int j = 0; j < B; ++j) T += Ts[j];
@@ -479,7 +503,9 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
   // embedding, the first norm's operand and sums of squares (one partial per
   // row), rotary table, zeroed counters
   PPD_TRY_HIP(launch_embed(PPD_BF16, m->tok_emb, m->prompt_emb, ids, depth,
-                           seq_batch(m, B, kvs, kvq ? kvq->pos : Ls, Ts, 0), m->head_dim, m->rope_base, rope,
+                           seq_batch(m, B, kvs, kvq ? kvq->pos : Ls, Ts, 0),
+                           paged ? DevSeqs{paged->row_start, paged->pt->len, paged->pt->n_seqs} : DevSeqs{},
+                           m->head_dim, m->rope_base, rope,
                            m->vocab, m->n_prompt, H, x, (const bf16_t *)m->attn_norm[0], xg, ss, ctr,
                            w.n_ctr, status, s));
   int n_ss = 1;
@@ -497,6 +523,8 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt(128.0));
   a.sb = seq_batch(m, B, kvs, Ls, Ts, 0);
   KvqAttnLaunch qa{};
+  PagedAttnLaunch pa{};
+  PagedSelectLaunch ps{};
   if (kvq) {
     qa.q = q;
     qa.out = attn_o;
@@ -509,6 +537,31 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
     qa.scale_log2 = a.scale_log2;
     qa.sb = kvq_seqs(B, kvq->kvs, kvq->L, Ts, 0);
     kvq_attn_plan(qa);
+  } else if (paged) {
+    const PagedWs pw = paged_layout(m, paged->pt->n_seqs, paged->pt->max_pages, T, paged->budget);
+    char *more = at<char>(ws, w.total);
+    pa.sq = ps.sq = paged_seqs(paged->pt, paged->row_start, T);
+    pa.tcap = paged->kv->tail.capacity;
+    pa.q = ps.q = q;
+    pa.out = attn_o;
+    pa.q_type = ps.q_type = PAGED_Q_PLANES;
+    pa.T_pad = ps.T_pad = Tp;
+    pa.mask = mask;
+    pa.budget = ps.budget = paged->budget;
+    pa.nh = ps.nh = nh;
+    pa.nkv = ps.nkv = nkv;
+    pa.rec = (int2 *)(more + pw.rec);
+    pa.part = (float *)(more + pw.part);
+    pa.status = ps.status = status;
+    pa.scale_log2 = a.scale_log2;
+    ps.n_first = paged->n_first;
+    ps.n_last = paged->n_last;
+    ps.keys = (unsigned long long *)(more + pw.keys);
+    if (paged->budget) {
+      pa.sel = ps.sel = (int32_t *)(more + pw.sel);
+      pa.n_sel = ps.n_sel = (int32_t *)(more + pw.n_sel);
+    }
+    paged_attn_shape(pa);
   } else {
     set_attn_plan(a, Ls, Ts, sync);
   }
@@ -546,6 +599,18 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
       qa.lse = kvq->lse_out ? kvq->lse_out + (size_t)l * T * nh : nullptr;
       timer_events(TK_ATTN, &qa.ev_start, &qa.ev_stop);
       PPD_TRY_HIP(launch_kvq_attn(qa, s));
+    } else if (paged) {
+      const ppd_paged &kv = *paged->kv;
+      const size_t layer_pages = (size_t)l * kv.n_pages * nkv;
+      if (paged->budget) {
+        ps.bounds = (const bf16_t *)kv.bounds + layer_pages * 256;
+        PPD_TRY_HIP(launch_paged_select(ps, s));
+      }
+      pa.pages = (const unsigned char *)kv.pages + layer_pages * (kv.page / kPB) * kPBytes;
+      pa.tk = sb.k[0];
+      pa.tv = sb.v[0];
+      timer_events(TK_ATTN, &pa.ev_start, &pa.ev_stop);
+      PPD_TRY_HIP(launch_paged_attn(pa, s));
     } else {
       a.sb = sb;
       a.ctr = attn_ctr + (size_t)l * 256;
@@ -626,7 +691,7 @@ ppd_status step_f32(const ppd_model *m, const ppd_kv *kv, int L, int T, const in
   one.B = 1;
   one.t0[1] = T;
   one.L[0] = L;
-  PPD_TRY_HIP(launch_embed(PPD_F32, m->tok_emb, m->prompt_emb, ids, depth, one, d, m->rope_base, rope,
+  PPD_TRY_HIP(launch_embed(PPD_F32, m->tok_emb, m->prompt_emb, ids, depth, one, DevSeqs{}, d, m->rope_base, rope,
                            m->vocab, m->n_prompt, H, x, nullptr, nullptr, nullptr, nullptr, 0, status, s));
   F32Gemm g{};
   g.T = T;
@@ -820,6 +885,44 @@ ppd_status ppd_verify_step_kvq(const ppd_model *model, const ppd_kvq *kv, int32_
                                void *stream) {
   return ppd_verify_batch_kvq(model, 1, kv, &L, &pos, &T, ids, depth, mask, ws, ws_bytes, logits, pred, q_out,
                               lse_out, stream);
+}
+
+size_t ppd_paged_workspace_bytes(const ppd_model *model, int32_t n_seqs, int32_t max_pages, int32_t n_rows,
+                                 int32_t budget) {
+  if (check_model(model) != PPD_OK) return 0;
+  if (n_rows < 1 || n_rows > PPD_T_MAX || model->dtype != PPD_BF16 || budget < 0) {
+    fail(PPD_EINVAL, "n_rows must be in [1, %d], budget >= 0, the model bf16", PPD_T_MAX);
+    return 0;
+  }
+  if (!ppd_paged_select_workspace_bytes(model->n_kv_heads, n_seqs, max_pages)) return 0;
+  return layout_of(model, n_rows).total + paged_layout(model, n_seqs, max_pages, n_rows, budget).total;
+}
+
+ppd_status ppd_verify_batch_paged(const ppd_model *model, const ppd_paged *kv, const ppd_page_tables *pt,
+                                  const int32_t *row_start, int32_t n_rows, const int32_t *ids, const int32_t *depth,
+                                  const uint64_t *mask, int32_t budget, int32_t n_first, int32_t n_last, void *ws,
+                                  size_t ws_bytes, float *logits, int32_t *pred, void *stream) {
+  ppd_status st = check_model(model);
+  if (st != PPD_OK) return st;
+  if (model->dtype != PPD_BF16) return fail(PPD_EUNSUPPORTED, "pages need a bf16 model");
+  if ((st = paged_check(kv, pt, true)) != PPD_OK) return st;
+  if (kv->n_layers != model->n_layers || kv->n_kv_heads != model->n_kv_heads)
+    return fail(PPD_EINVAL, "a cache of %d layers and %d heads, not the model's", kv->n_layers, kv->n_kv_heads);
+  if (n_rows < 1 || n_rows > PPD_T_MAX) return fail(PPD_EINVAL, "n_rows=%d outside [1, %d]", n_rows, PPD_T_MAX);
+  if ((st = paged_check_rows(kv, row_start, n_rows)) != PPD_OK) return st;
+  if (budget < 0) return fail(PPD_EINVAL, "budget must be >= 0");
+  if (budget && (st = paged_check_select(kv, budget, n_first, n_last)) != PPD_OK) return st;
+  if (!ids || !depth || !mask || !pred) return fail(PPD_EINVAL, "NULL tree or output pointer");
+  const size_t need = ppd_paged_workspace_bytes(model, pt->n_seqs, pt->max_pages, n_rows, budget);
+  if (!need) return PPD_EINVAL;
+  if (!ws || ws_bytes < need)
+    return fail(PPD_EWORKSPACE, "workspace of %zu bytes is smaller than the %zu required", ws_bytes, need);
+  g_timer.next = 0;
+  const WsLayout w = layout_of(model, n_rows);
+  const PagedStep step{kv, pt, row_start, budget, n_first, n_last};
+  const int32_t zero = 0;
+  return step_bf16(model, 1, &kv->tail, &zero, &n_rows, ids, depth, mask, ws, w, logits, pred, (hipStream_t)stream,
+                   nullptr, &step);
 }
 
 ppd_status ppd_verify_step(const ppd_model *model, const ppd_kv *kv, int32_t L, int32_t T,

@@ -302,9 +302,14 @@ ppd_status ppd_fail(ppd_status s, const char *fmt, ...);
 // embedding rows into x (fp32), rows T..T_pad-1 zero, and the rotary
 // table [T_pad][d / 2] (cos, sin); bf16 models also write the first norm's
 // operand planes (x * gain) and sums of squares (ss, one per row) and zero
-// the n_ctr tile / head counters
+// the n_ctr tile / head counters.  dev (its row_start set): token t's sequence
+// and cached length come from the device instead of sb
+struct DevSeqs {
+  const int32_t *row_start, *len;  // [B + 1], [B]
+  int B;
+};
 hipError_t launch_embed(int dtype, const void *tok_emb, const void *prompt_emb, const int32_t *ids,
-                        const int32_t *depth, const SeqBatch &sb, int d, float base, float2 *rope,
+                        const int32_t *depth, const SeqBatch &sb, const DevSeqs &dev, int d, float base, float2 *rope,
                         int vocab, int n_prompt, int H, float *x, const bf16_t *gain,
                         unsigned char *planes, float *ss, uint32_t *ctr, size_t n_ctr,
                         uint32_t *status, hipStream_t s);

@@ -1,0 +1,131 @@
+// The paged cache (ppd_paged, ppd_page_tables): layout, the division of an
+// attention call's work from lengths on the device, and launchers.
+#pragma once
+
+#include "ppd_internal.h"
+
+constexpr int kPB = PPD_PAGED_BLOCK;              // positions of a block
+constexpr int kPElems = kPB * 128;                // elements of a block's keys (or values)
+constexpr int kPBytes = 2 * kPElems * 2;          // bytes of a block: keys, then values
+
+// element of a block's keys, and of its values, at position u (of the block), dim d
+__host__ __device__ __forceinline__ int paged_key_at(int u, int d) {
+  return ((((u >> 2) & 1) * 4 + (d >> 5)) * 64 + 16 * ((d >> 3) & 3) + 4 * (u >> 3) + (u & 3)) * 8 + (d & 7);
+}
+__host__ __device__ __forceinline__ int paged_value_at(int u, int d) {
+  return ((d >> 4) * 64 + 16 * (u >> 3) + (d & 15)) * 8 + (u & 7);
+}
+// position (of its block) that row m of key tile t holds
+__host__ __device__ __forceinline__ int paged_key_of(int t, int m) { return 8 * (m >> 2) + 4 * t + (m & 3); }
+
+// the sequences as the device sees them
+struct PagedSeqs {
+  const int32_t *table, *len, *row_start;
+  int B, max_pages, n_pages;
+  int lp;      // log2 of the page's positions
+  int n_rows;  // rows that the call's buffers hold
+};
+
+// A sequence's own numbers, clamped so that no index that follows from them
+// leaves its buffer; *bad where one had to be.
+struct PagedSeq {
+  int t0, T, L;
+};
+__device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs &p, int s, bool *bad) {
+  const int n = p.len[s], a = p.row_start[s], b = p.row_start[s + 1];
+  PagedSeq q;
+  q.L = max(0, min((int64_t)n, (int64_t)p.max_pages << p.lp));
+  q.t0 = max(0, min(a, p.n_rows));
+  q.T = max(0, min(min(b, p.n_rows) - q.t0, PPD_T_MAX));
+  *bad |= n != q.L || a != q.t0 || b - a != q.T;
+  return q;
+}
+__device__ __forceinline__ int paged_clamp(int page, int n_pages) { return max(0, min(page, n_pages - 1)); }
+
+// The sequence of a row: the last one whose rows start at or before it.  Called
+// by a whole wave, `tok` alike in its lanes.
+__device__ __forceinline__ int paged_seq_of(const int32_t *row_start, int B, int tok) {
+  int n = 0;
+  for (int base = 0; base < B; base += 64) {
+    const int s = base + (int)(threadIdx.x & 63);
+    n += __popcll(__ballot(s < B && row_start[min(s, B - 1)] <= tok));
+  }
+  return n - 1;
+}
+
+struct PagedTablesLaunch {
+  int32_t *table, *free_pages;
+  const int32_t *len, *free_state, *add;
+  int32_t *len_out, *free_state_out, *start, *slots;
+  int B, max_pages, n_pages, lp, n_slots;
+  int4 *plan;        // [B]: length, pages held, first of the ring's entries, what becomes of it
+  uint32_t *status;
+};
+hipError_t launch_paged_tables(const PagedTablesLaunch &p, hipStream_t s);
+
+struct PagedStoreLaunch {
+  unsigned char *pages;
+  bf16_t *bounds;       // or null
+  const bf16_t *k, *v;  // [heads][scap][128], [heads][128][scap]
+  int layers, nkv, n_pages, lp, scap;
+  int B, n_rows;
+  int n_path;
+  int chunks;           // parts of the rows, workgroups a head (the launcher's)
+  const int32_t *start, *row_start, *path, *slots;
+};
+hipError_t launch_paged_store(PagedStoreLaunch p, hipStream_t s);
+
+enum { PAGED_Q_BF16 = 0, PAGED_Q_F32 = 1, PAGED_Q_PLANES = 2 };
+
+struct PagedAttnLaunch {
+  PagedSeqs sq;
+  const unsigned char *pages;  // this layer's
+  const bf16_t *tk, *tv;       // this layer's new rows, row i at position i
+  int tcap;
+  const void *q;               // rows [n_rows][nh][128] of a type, or operand planes
+  void *out;                   // likewise
+  int q_type, T_pad;
+  const uint64_t *mask;        // [n_rows][2], or null: a row sees its sequence's rows up to itself
+  float *lse;                  // [n_rows][nh], or null
+  const int32_t *sel, *n_sel;  // [B][nkv][budget], [B], or null
+  int budget;
+  int nh, nkv;
+  float *part;                 // [kPagedSlots][rows of a workgroup][PPD_ATTN_OROW]
+  int2 *rec;                   // [B]: splits, first of the partial rows' workgroups
+  uint32_t *status;
+  float scale_log2;
+  int tiles;                   // 16-row tiles of a kv head's rows, by which the kernel's shape is chosen
+  int may_split;               // a sequence can be long enough for more than one workgroup
+  void *ev_start, *ev_stop;
+};
+// workgroups that share a call's keys; also bounds those that leave partial rows
+constexpr int kPagedSlots = 256;
+size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows);
+void paged_attn_shape(PagedAttnLaunch &a);  // fills tiles, may_split
+hipError_t launch_paged_attn(const PagedAttnLaunch &a, hipStream_t s);
+
+struct PagedSelectLaunch {
+  PagedSeqs sq;
+  const bf16_t *bounds;  // this layer's [n_pages][nkv][2][128]
+  const void *q;
+  int q_type, T_pad, nh, nkv;
+  int budget, n_first, n_last;
+  unsigned long long *keys;  // [B][nkv][max_pages]
+  int32_t *sel, *n_sel;
+  uint32_t *status;
+};
+hipError_t launch_paged_select(const PagedSelectLaunch &p, hipStream_t s);
+
+// The step of ppd_api.cpp on pages
+struct PagedStep {
+  const ppd_paged *kv;
+  const ppd_page_tables *pt;
+  const int32_t *row_start;
+  int budget, n_first, n_last;  // budget 0: every page
+};
+PagedSeqs paged_seqs(const ppd_page_tables *pt, const int32_t *row_start, int n_rows);
+// the arguments that the calls on pages share (ppd_paged.cpp)
+ppd_status paged_check(const ppd_paged *kv, const ppd_page_tables *pt, bool tail);
+ppd_status paged_check_rows(const ppd_paged *kv, const int32_t *row_start, int n_rows);
+ppd_status paged_check_select(const ppd_paged *kv, int budget, int n_first, int n_last);
+size_t paged_select_key_bytes(int nkv, int B, int max_pages);
