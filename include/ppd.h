@@ -185,9 +185,10 @@ typedef struct {
  * nodes and caches of up to max_len positions.  0 on invalid input. */
 size_t ppd_workspace_bytes(const ppd_model *model, int32_t t_max, int32_t max_len);
 
-/* Zero the workspace's header, its first 256 bytes, which hold the status word
- * (enqueued on `stream`).  Call once after allocating a workspace; later calls
- * never write the header except for status bits. */
+/* Zero the workspace's header, its first 256 bytes, which hold the status word,
+ * and of what it has behind them 512 bytes more, the counters of a
+ * ppd_paged_attention workspace (enqueued on `stream`).  Call once after allocating
+ * a workspace; later calls never write the header except for status bits. */
 ppd_status ppd_workspace_init(void *ws, size_t ws_bytes, void *stream);
 
 /*
@@ -622,7 +623,9 @@ ppd_status ppd_paged_store(const ppd_paged *kv, const ppd_kv *src, int32_t n_seq
  *            int32[n_seqs] (as ppd_paged_select gives them; none twice), or NULL
  *   ws       device workspace, 16-byte aligned, of
  *            ppd_paged_attention_workspace_bytes(n_heads, n_kv_heads, n_seqs, n_rows),
- *            one for each stream that calls may overlap on (its header the status word)
+ *            one for each stream that calls may overlap on, prepared once with
+ *            ppd_workspace_init (its header the status word, then counters that
+ *            every call leaves zero)
  */
 size_t ppd_paged_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t n_rows);
 ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,

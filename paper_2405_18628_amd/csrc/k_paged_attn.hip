@@ -22,7 +22,8 @@
 
 namespace {
 
-constexpr int NT = 512;              // eight waves
+constexpr int NT = 512;              // threads of the second launch
+constexpr int kLeast = 2;            // blocks of a wave, at least, where a prefix is split
 constexpr int OROW = PPD_ATTN_OROW;  // partial row: 128 dims, m, l, padding (floats)
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -76,16 +77,6 @@ __device__ __forceinline__ void softmax_step(PTile &R, const float (&sv)[8], flo
   }
 }
 
-__device__ __forceinline__ int wave_incl(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    v += lane >= o ? u : 0;
-  }
-  return v;
-}
-
 // a sequence's work: blocks of the prefix and of its rows, row groups
 struct Load {
   int n4, nblk, grps, units;
@@ -105,14 +96,17 @@ __device__ __forceinline__ Load load_of(const PagedAttnLaunch &p, int s, const P
   w.units = w.grps * p.nkv;
   return w;
 }
-// its splits: its share of kPagedSlots, PARS blocks a split at least.  Rounded
-// down, so the splits of all that have several are at most kPagedSlots.
-__device__ __forceinline__ int splits_of(const Load &w, int64_t total, int PARS) {
-  if (w.units == 0) return 0;
-  const int64_t share = (int64_t)kPagedSlots * w.nblk / max(total, (int64_t)1);
-  const int want = (int)max((int64_t)1, min(share, (int64_t)(w.nblk / PARS)));
-  const int chunk = (w.nblk + want - 1) / want;
-  return (w.nblk + chunk - 1) / chunk;
+// Blocks of a workgroup at most: all of them over the call's slots, LEAST at least.
+// With c of them, a row group of n blocks is cut into ceil(n / c) splits: at most
+// units + SLOTS workgroups in all, at most 2 SLOTS of them of groups that have
+// several, of which there are less than SLOTS (each holds more than c blocks).
+template <int SLOTS, int LEAST>
+__device__ __forceinline__ int blocks_each(int64_t total) {
+  return (int)max((total + SLOTS - 1) / SLOTS, (int64_t)LEAST);
+}
+__device__ __forceinline__ int splits_of(const Load &w, int c) {
+  c = max(c, (w.nblk + kPagedSplits - 1) / kPagedSplits);
+  return w.units ? (w.nblk + c - 1) / c : 0;
 }
 
 struct Place {
@@ -122,7 +116,16 @@ struct Place {
 };
 // the workgroup's sequence and place in it; false: it has no part.  A wave's lanes
 // take a sequence each.
-__device__ bool find_place(const PagedAttnLaunch &p, int slot, int RW, int PARS, Place *out, bool *bad) {
+template <int RW, int SLOTS, int LEAST>
+__device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, Place *out, bool *bad) {
+  if (p.sq.B == 1) {  // alike in all lanes
+    out->sq = out->part0 = 0;
+    out->q = paged_seq(p.sq, 0, bad);
+    out->w = load_of(p, 0, out->q, RW, bad);
+    out->KS = splits_of(out->w, blocks_each<SLOTS, LEAST>((int64_t)out->w.units * out->w.nblk));
+    out->local = slot;
+    return slot < out->w.units * out->KS;
+  }
   const int lane = threadIdx.x & 63;
   int64_t total = 0;
   PagedSeq q{};
@@ -135,8 +138,9 @@ __device__ bool find_place(const PagedAttnLaunch &p, int slot, int RW, int PARS,
       total += (int64_t)w.units * w.nblk;
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+  total = wave_total(total);
+  // (of many groups, each is rounded up: over three quarters of the slots, most fit at once)
+  const int c = blocks_each<SLOTS * 3 / 4, LEAST>(total);
   int slots0 = 0, parts0 = 0;
   for (int base = 0; base < p.sq.B; base += 64) {
     const int s = base + lane;
@@ -146,7 +150,7 @@ __device__ bool find_place(const PagedAttnLaunch &p, int slot, int RW, int PARS,
         q = paged_seq(p.sq, s, bad);
         w = load_of(p, s, q, RW, bad);
       }
-      KS = splits_of(w, total, PARS);
+      KS = splits_of(w, c);
     }
     const int mine = s < p.sq.B ? w.units * KS : 0, parted = KS > 1 ? mine : 0;
     const int upto = slots0 + wave_incl(mine), parts = parts0 + wave_incl(parted);
@@ -154,15 +158,15 @@ __device__ bool find_place(const PagedAttnLaunch &p, int slot, int RW, int PARS,
     if (hit) {
       const int at = __builtin_ctzll(hit);
       out->sq = base + at;
-      out->local = slot - __shfl(upto - mine, at, 64);
-      out->KS = __shfl(KS, at, 64);
-      out->part0 = __shfl(parts - parted, at, 64);
-      out->q = PagedSeq{__shfl(q.t0, at, 64), __shfl(q.T, at, 64), __shfl(q.L, at, 64)};
-      out->w = Load{__shfl(w.n4, at, 64), __shfl(w.nblk, at, 64), __shfl(w.grps, at, 64), __shfl(w.units, at, 64)};
+      out->local = slot - lane_of(upto - mine, at);
+      out->KS = lane_of(KS, at);
+      out->part0 = lane_of(parts - parted, at);
+      out->q = PagedSeq{lane_of(q.t0, at), lane_of(q.T, at), lane_of(q.L, at)};
+      out->w = Load{lane_of(w.n4, at), lane_of(w.nblk, at), lane_of(w.grps, at), lane_of(w.units, at)};
       return true;
     }
-    slots0 = __shfl(upto, 63, 64);
-    parts0 = __shfl(parts, 63, 64);
+    slots0 = lane_of(upto, 63);
+    parts0 = lane_of(parts, 63);
   }
   return false;
 }
@@ -195,6 +199,31 @@ __device__ __forceinline__ void store_out4(const PagedAttnLaunch &p, int tok, in
     *(floatx4 *)((float *)p.out + ((size_t)tok * p.nh + head) * 128 + d4) = o;
 }
 
+// what a split's row is added with, M the largest maximum (a split that sees NaN
+// alone has none: its sum is kept as it is)
+__device__ __forceinline__ float factor_of(float2 ml, float M) {
+  return ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - M);
+}
+
+// two floats of a partial row; FAR: to and from where every XCD sees them
+template <bool FAR>
+__device__ __forceinline__ void put_part(float *p, float2 v) {
+  if constexpr (FAR)
+    __hip_atomic_store((uint64_t *)p, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  else
+    *(float2 *)p = v;
+}
+__device__ __forceinline__ float2 get_part(const float *p) {
+  return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// ONCE: no other wave of the call reads it
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_page(const unsigned char *p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4 *)p);
+  return *(const u32x4 *)p;
+}
+
 // table entries are read through the scalar cache: they are alike in a wave
 __device__ __forceinline__ int uniform_load(const int32_t *p, int64_t i) {
   typedef const __attribute__((address_space(4))) int32_t cint;
@@ -203,8 +232,10 @@ __device__ __forceinline__ int uniform_load(const int32_t *p, int64_t i) {
 
 // NQ tiles a wave, QW waves side by side over tiles, PARS over blocks
 template <int NQ, int QW, int PARS, int QT>
-__global__ __launch_bounds__(NT, 1) void paged_attention_kernel(PagedAttnLaunch p) {
-  static_assert(QW * PARS * 64 == NT, "eight waves");
+__global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(PagedAttnLaunch p) {
+  constexpr int NT = 64 * QW * PARS;
+  constexpr bool JOIN = NQ * QW == 1;  // the last of a row group's splits adds them
+  constexpr int SLOTS = paged_slots(NQ * QW);
   constexpr int RW = QW * NQ * 16;  // rows of the workgroup
   constexpr int QP = q_parts(QT), PP = p_parts(QT);
   constexpr bool QLDS = NQ > 1 || QP > 2;  // no registers left for the queries
@@ -220,7 +251,7 @@ __global__ __launch_bounds__(NT, 1) void paged_attention_kernel(PagedAttnLaunch 
   const int lr = lane & 15, lg = lane >> 4;
   Place pl;
   bool bad = false;
-  const bool mine = find_place(p, blockIdx.x, RW, PARS, &pl, &bad);
+  const bool mine = find_place<RW, SLOTS, kLeast * PARS>(p, blockIdx.x, &pl, &bad);
   if (bad && blockIdx.x == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   if (!mine) return;
   const int sq = __builtin_amdgcn_readfirstlane(pl.sq), KS = __builtin_amdgcn_readfirstlane(pl.KS);
@@ -230,13 +261,13 @@ __global__ __launch_bounds__(NT, 1) void paged_attention_kernel(PagedAttnLaunch 
   const int n_grp = __builtin_amdgcn_readfirstlane(pl.w.grps);
   const int part0 = __builtin_amdgcn_readfirstlane(pl.part0);
   int local = __builtin_amdgcn_readfirstlane(pl.local);
-  if (local == 0 && tid == 0) p.rec[sq] = int2{KS, part0};
-  const int my_part = part0 + local;
+  if (!JOIN && local == 0 && tid == 0) p.rec[sq] = int2{KS, part0};
+  const int my_part = part0 + local;  // the workgroup's place among those that leave partial rows
   const int G = p.nh / p.nkv, R = T * G;
   const int ks = local % KS;
   local /= KS;
   const int grp = local % n_grp, kvh = local / n_grp;
-  const int chunk = (nblk + KS - 1) / KS;
+  const int chunk = (nblk + KS - 1) / KS;  // (the last splits may be left without blocks)
   const int b0 = min(nblk, ks * chunk), b1 = min(nblk, b0 + chunk);
   const int row0 = grp * RW;
   const int lb = p.sq.lp - 5, n_pages = p.sq.n_pages;
@@ -263,11 +294,11 @@ __global__ __launch_bounds__(NT, 1) void paged_attention_kernel(PagedAttnLaunch 
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int ds = 0; ds < 4; ++ds) kf[t][ds] = *(const u32x4 *)(src + (t * 4 + ds) * 1024 + lane * 16);
+      for (int ds = 0; ds < 4; ++ds) kf[t][ds] = load_page<QW == 1>(src + (t * 4 + ds) * 1024 + lane * 16);
   };
   auto load_values = [&](const unsigned char *src) {
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) vf[dt] = *(const u32x4 *)(src + 2 * kPElems + dt * 1024 + lane * 16);
+    for (int dt = 0; dt < 8; ++dt) vf[dt] = load_page<QW == 1>(src + 2 * kPElems + dt * 1024 + lane * 16);
   };
   int blk = b0 + par;
   int place = 0, next_place = 0;
@@ -499,15 +530,14 @@ __global__ __launch_bounds__(NT, 1) void paged_attention_kernel(PagedAttnLaunch 
     float f[PARS];
 #pragma unroll
     for (int w = 0; w < PARS; ++w) {
-      // (a wave that sees NaN alone has no maximum: its sum is kept as it is)
-      f[w] = ml[w].x == -INFINITY ? (ml[w].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[w].x - M);
+      f[w] = factor_of(ml[w], M);
       l += f[w] * ml[w].y;
     }
     const float inv = KS > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int w = 0; w < PARS; ++w) fac_s[tid][w] = f[w] * inv;
     if (KS > 1) {
-      *(float2 *)(part + (size_t)tid * OROW + 128) = float2{M, l};
+      put_part<JOIN>(part + (size_t)tid * OROW + 128, float2{M, l});
     } else if (p.lse) {
       const int r = row0 + tid;
       p.lse[(size_t)(t0 + r / G) * p.nh + kvh * G + r % G] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
@@ -521,10 +551,98 @@ __global__ __launch_bounds__(NT, 1) void paged_attention_kernel(PagedAttnLaunch 
 #pragma unroll
     for (int w = 0; w < PARS; ++w) o += fac_s[rl][w] * *(const floatx4 *)(rows_s[w][rl] + d4);
     if (KS > 1) {
-      *(floatx4 *)(part + (size_t)rl * OROW + d4) = o;
+      put_part<JOIN>(part + (size_t)rl * OROW + d4, float2{o[0], o[1]});
+      put_part<JOIN>(part + (size_t)rl * OROW + d4 + 2, float2{o[2], o[3]});
     } else {
       const int r = row0 + rl;
       store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, o);
+    }
+  }
+  if constexpr (JOIN) {
+    if (KS == 1) return;
+    // ---- the last of the splits to arrive adds them all, in order.  Their rows
+    // are written and read past the XCDs' caches, so no cache is written back
+    // or dropped for them.
+    __shared__ int last_s;
+    __builtin_amdgcn_s_waitcnt(0);  // this thread's rows are in memory
+    __syncthreads();
+    if (tid == 0) {
+      const int i = (my_part - ks) >> 1, shift = 8 * (i & 3);  // (two splits at least: no two groups share i)
+      uint32_t *ctr = p.ctr + (i >> 2);
+      const uint32_t n = __hip_atomic_fetch_add(ctr, 1u << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> shift & 0xffu;
+      last_s = n + 1 == (uint32_t)KS;
+      if (last_s) __hip_atomic_fetch_sub(ctr, (uint32_t)KS << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last_s) return;
+    part = p.part + (size_t)(my_part - ks) * RW * OROW;
+    constexpr size_t stride = (size_t)RW * OROW;
+    // a split's factor for a row, in LDS
+    float(*wt_s)[kPagedSplits] = (float(*)[kPagedSplits])rows_s;
+    constexpr int TR = NT / RW;  // threads a row
+    static_assert(TR <= 64 && kPagedSplits % TR == 0 && sizeof(float) * RW * kPagedSplits <= sizeof(rows_s), "weights fit");
+    {
+      const int rl = tid / TR, j0 = tid % TR;
+      float2 ml[kPagedSplits / TR];
+      float M = -INFINITY, l = 0.f;
+      if (rl < n_rows) {
+#pragma unroll
+        for (int j = 0; j < kPagedSplits / TR; ++j)
+          ml[j] = j0 + TR * j < KS ? get_part(part + (j0 + TR * j) * stride + (size_t)rl * OROW + 128) : float2{-INFINITY, 0.f};
+#pragma unroll
+        for (int j = 0; j < kPagedSplits / TR; ++j) M = fmaxf(M, ml[j].x);
+#pragma unroll
+        for (int o = TR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+#pragma unroll
+        for (int j = 0; j < kPagedSplits / TR; ++j) {
+          const float f = factor_of(ml[j], M);
+          l += f * ml[j].y;
+          if (j0 + TR * j < KS) wt_s[rl][j0 + TR * j] = f;
+        }
+#pragma unroll
+        for (int o = TR / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+        if (j0 == 0) {
+          fac_s[rl][0] = l == 0.f ? 0.f : 1.f / l;
+          const int r = row0 + rl;
+          if (p.lse) p.lse[(size_t)(t0 + r / G) * p.nh + kvh * G + r % G] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+        }
+      }
+    }
+    __syncthreads();
+    // rows' sums: 32 threads a row; of few rows several such groups share one
+    constexpr int GR = NT / 32;
+    const int ways = n_rows >= 5 ? 1 : n_rows >= 3 ? GR / 4 : n_rows == 2 ? GR / 2 : GR;
+    floatx4 *sum_s = (floatx4 *)((char *)rows_s + sizeof(float) * RW * kPagedSplits);  // [GR][32]
+    static_assert(sizeof(float) * RW * kPagedSplits + GR * 512 <= sizeof(rows_s), "sums fit");
+    const int grp32 = tid >> 5, sub = grp32 % ways;
+    for (int rl = grp32 / ways; rl < n_rows; rl += GR / ways) {
+      constexpr int N = 16;  // splits in flight
+      floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int s0 = sub; s0 < KS; s0 += N * ways) {
+        float2 x[N][2];
+#pragma unroll
+        for (int v = 0; v < N; ++v) {
+          const float *row = part + min(s0 + v * ways, KS - 1) * stride + (size_t)rl * OROW + d4;
+          x[v][0] = get_part(row);
+          x[v][1] = get_part(row + 2);
+        }
+#pragma unroll
+        for (int v = 0; v < N; ++v)
+          if (s0 + v * ways < KS) o += wt_s[rl][s0 + v * ways] * floatx4{x[v][0].x, x[v][0].y, x[v][1].x, x[v][1].y};
+      }
+      if (ways > 1) sum_s[grp32 * 32 + (tid & 31)] = o;
+      if (ways == 1) {
+        const int r = row0 + rl;
+        store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, o * fac_s[rl][0]);
+      }
+    }
+    if (ways == 1) return;
+    __syncthreads();
+    if (sub == 0 && grp32 / ways < n_rows) {
+      const int rl = grp32 / ways, r = row0 + rl;
+      floatx4 o = sum_s[grp32 * 32 + (tid & 31)];
+      for (int w = 1; w < ways; ++w) o += sum_s[(grp32 + w) * 32 + (tid & 31)];
+      store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, o * fac_s[rl][0]);
     }
   }
 }
@@ -576,7 +694,7 @@ __global__ __launch_bounds__(NT) void paged_merge_kernel(PagedAttnLaunch p, int 
     M = m;
 #pragma unroll
     for (int v = 0; v < N; ++v) {
-      const float f = ml[v].x == -INFINITY ? (ml[v].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[v].x - M);
+      const float f = factor_of(ml[v], M);
       l += s0 + v < KS ? f * ml[v].y : 0.f;
       if (s0 + v < KS) o += f * x[v];
     }
@@ -589,9 +707,12 @@ __global__ __launch_bounds__(NT) void paged_merge_kernel(PagedAttnLaunch p, int 
 }  // namespace
 
 // 16-row tiles a wave holds and waves side by side, by the tiles of a kv head
-static void paged_shape(int tiles, int *nq, int *qw) {
-  *nq = tiles <= 1 ? 1 : 2;
-  *qw = tiles <= 2 ? 1 : tiles <= 4 ? 2 : 4;
+struct Shape {
+  int nq, qw, pars;
+  int rows() const { return 16 * nq * qw; }
+};
+static Shape paged_shape(int tiles) {
+  return tiles <= 1 ? Shape{1, 1, 4} : tiles <= 2 ? Shape{2, 1, 8} : tiles <= 4 ? Shape{2, 2, 4} : Shape{2, 4, 2};
 }
 // (a rule on the rows of an average sequence: how many a single one has is only
 // known on the device, and any shape serves any number)
@@ -601,45 +722,42 @@ static int paged_tiles(int nh, int nkv, int B, int n_rows) {
 }
 
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows) {
-  int nq, qw;
-  paged_shape(paged_tiles(nh, nkv, B, n_rows), &nq, &qw);
-  return (size_t)kPagedSlots * 16 * nq * qw * OROW * sizeof(float);
+  const Shape sh = paged_shape(paged_tiles(nh, nkv, B, n_rows));
+  return 2 * (size_t)paged_slots(sh.nq * sh.qw) * sh.rows() * OROW * sizeof(float);
 }
 
 void paged_attn_shape(PagedAttnLaunch &a) {
   a.tiles = paged_tiles(a.nh, a.nkv, a.sq.B, a.sq.n_rows);
-  int nq, qw;
-  paged_shape(a.tiles, &nq, &qw);
   const int most = a.sel ? std::min(a.budget, a.sq.max_pages) : a.sq.max_pages;
-  a.may_split = ((int64_t)most << (a.sq.lp - 5)) + PPD_T_MAX / kPB >= 2 * (8 / qw);
+  a.may_split = ((int64_t)most << (a.sq.lp - 5)) + PPD_T_MAX / kPB > kLeast * paged_shape(a.tiles).pars;
 }
 
 template <int QT>
 static hipError_t launch_attn(const PagedAttnLaunch &a, hipStream_t s) {
-  auto kernel = a.tiles <= 1   ? paged_attention_kernel<1, 1, 8, QT>
+  auto kernel = a.tiles <= 1   ? paged_attention_kernel<1, 1, 4, QT>
                 : a.tiles <= 2 ? paged_attention_kernel<2, 1, 8, QT>
                 : a.tiles <= 4 ? paged_attention_kernel<2, 2, 4, QT>
                                : paged_attention_kernel<2, 4, 2, QT>;
-  int nq, qw;
-  paged_shape(a.tiles, &nq, &qw);
-  const int rw = 16 * nq * qw;
+  const Shape sh = paged_shape(a.tiles);
+  const int rw = sh.rows();
   // row groups of all sequences at most, and the splits of those that have several
   const int64_t rows = (int64_t)a.sq.n_rows * (a.nh / a.nkv);
   const int64_t units = a.nkv * (std::min<int64_t>(a.sq.B, a.sq.n_rows) + rows / rw);
-  const int64_t grid = units + (a.may_split ? kPagedSlots : 0);
+  const dim3 grid((unsigned)(units + (a.may_split ? paged_slots(sh.nq * sh.qw) : 0))), block(64 * sh.qw * sh.pars);
+  const bool merge = a.may_split && sh.nq * sh.qw > 1;
   const hipEvent_t ev0 = (hipEvent_t)a.ev_start, ev1 = (hipEvent_t)a.ev_stop;
   if (ev0)
-    hipExtLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NT), 0, s, ev0, a.may_split ? (hipEvent_t) nullptr : ev1, 0, a);
+    hipExtLaunchKernelGGL(kernel, grid, block, 0, s, ev0, merge ? (hipEvent_t) nullptr : ev1, 0, a);
   else
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NT), 0, s, a);
-  if (a.may_split) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
+  if (merge) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const dim3 merge((unsigned)(((int64_t)a.sq.n_rows * a.nh + NT / 32 - 1) / (NT / 32)));
+    const dim3 rows16((unsigned)(((int64_t)a.sq.n_rows * a.nh + NT / 32 - 1) / (NT / 32)));
     if (ev1)
-      hipExtLaunchKernelGGL(paged_merge_kernel<QT>, merge, dim3(NT), 0, s, (hipEvent_t) nullptr, ev1, 0, a, rw);
+      hipExtLaunchKernelGGL(paged_merge_kernel<QT>, rows16, dim3(NT), 0, s, (hipEvent_t) nullptr, ev1, 0, a, rw);
     else
-      hipLaunchKernelGGL(paged_merge_kernel<QT>, merge, dim3(NT), 0, s, a, rw);
+      hipLaunchKernelGGL(paged_merge_kernel<QT>, rows16, dim3(NT), 0, s, a, rw);
   }
   return hipGetLastError();
 }

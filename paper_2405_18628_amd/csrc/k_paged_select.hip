@@ -24,6 +24,8 @@ constexpr int ST = 256;    // threads of the scores' workgroup
 constexpr int PAGES = 16;  // pages of a wave
 constexpr int CH = PAGES * (ST / 64);
 
+constexpr u64 kKept = ~0ull;  // the key of a page that is always taken: no number's
+
 // the order of numbers as unsigned keys; NaN first of all
 __device__ __forceinline__ u64 key_of(double v) {
   if (v != v) return 0;
@@ -59,15 +61,16 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
   __shared__ double q_s[2][128];  // Qm, Qp
   const int tid = threadIdx.x, lane = tid & 63;
   const int c = blockIdx.x % chunks, kvh = blockIdx.x / chunks % p.nkv, sq = blockIdx.x / chunks / p.nkv;
+  const int page0 = c * CH + (tid >> 6) * PAGES;
+  // ---- this wave's bounds (the table's entries are requested beside the length)
+  const int32_t *table = p.sq.table + (size_t)sq * p.sq.max_pages;
+  const int entry = table[min(page0 + (lane & (PAGES - 1)), p.sq.max_pages - 1)];
   bool bad = false;
   const PagedSeq s = paged_seq(p.sq, sq, &bad);
   if (bad && c == 0 && tid == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   const int n = (s.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
   if (n <= p.budget || c * CH >= n) return;  // all are taken
-  const int page0 = c * CH + (tid >> 6) * PAGES;
-  // ---- this wave's bounds
-  const int32_t *table = p.sq.table + (size_t)sq * p.sq.max_pages;
-  const int phys = paged_clamp(table[min(page0 + (lane & (PAGES - 1)), n - 1)], p.sq.n_pages);
+  const int phys = paged_clamp(entry, p.sq.n_pages);
   u32x4 w[PAGES / 2];
 #pragma unroll
   for (int i = 0; i < PAGES / 2; ++i) {
@@ -133,19 +136,25 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
   const int page = page0 + 2 * i + (lane >> 5);
   if ((lane & 3) == 0 && page < n) {
     const bool kept = page < p.n_first || page >= n - p.n_last;
-    p.keys[((size_t)sq * p.nkv + kvh) * p.sq.max_pages + page] = kept ? ~0ull : key_of(x);
+    p.keys[((size_t)sq * p.nkv + kvh) * p.sq.max_pages + page] = kept ? kKept : key_of(x);
   }
 }
 
 constexpr int KT = 1024;  // threads of the selection
 constexpr int REG = 8;    // keys a thread holds; of more, the passes read them again
+constexpr int KW = KT / 64;
 
 __global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
-  __shared__ u64 red_s[2][KT / 64];
+  __shared__ uint32_t red_s[2][KW];
+  __shared__ u64 list_s[64], pick_s;
   __shared__ unsigned hist_s[256];
-  __shared__ int cnt_s[KT / 64], bin_s, above_s;
+  __shared__ int cnt_s[2][REG][KW], bin_s, above_s, in_s, n_list;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int kvh = blockIdx.x % p.nkv, sq = blockIdx.x / p.nkv;
+  const u64 *keys = p.keys + ((size_t)sq * p.nkv + kvh) * p.sq.max_pages;
+  u64 kr[REG];  // (requested before the length is known: of this head's keys, or its last one)
+#pragma unroll
+  for (int j = 0; j < REG; ++j) kr[j] = keys[min(j * KT + tid, p.sq.max_pages - 1)];
   bool bad = false;
   const PagedSeq s = paged_seq(p.sq, sq, &bad);
   const int n = (s.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
@@ -155,113 +164,132 @@ __global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
     for (int i = tid; i < n; i += KT) sel[i] = i;
     return;
   }
-  const u64 *keys = p.keys + ((size_t)sq * p.nkv + kvh) * p.sq.max_pages;
-  u64 kr[REG];
-#pragma unroll
-  for (int j = 0; j < REG; ++j) kr[j] = keys[min(j * KT + tid, n - 1)];
   const int rounds = (n + KT - 1) / KT;
-  // f(key, index) of this thread's pages, rising
+  // f(key, index) of this thread's pages that are ranked
   auto each = [&](auto f) {
 #pragma unroll
     for (int j = 0; j < REG; ++j)
-      if (j * KT + tid < n) f(kr[j], j * KT + tid);
-    for (int j = REG; j < rounds; ++j)
-      if (j * KT + tid < n) f(keys[j * KT + tid], j * KT + tid);
+      if (j * KT + tid < n && kr[j] != kKept) f(kr[j]);
+    for (int j = REG; j < rounds; ++j) {
+      const int i = j * KT + tid;
+      const u64 k = keys[min(i, n - 1)];
+      if (i < n && k != kKept) f(k);
+    }
   };
-  // ---- the bits in which keys differ
-  u64 all = ~0ull, any = 0;
-  each([&](u64 k, int) { all &= k, any |= k; });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    all &= __shfl_xor(all, o, 64);
-    any |= __shfl_xor(any, o, 64);
-  }
+  // ---- the bits in which ranked keys' upper halves differ
+  uint32_t all = ~0u, any = 0;
+  each([&](u64 k) { all &= (uint32_t)(k >> 32), any |= (uint32_t)(k >> 32); });
+  all = wave_all(all, [](uint32_t a, uint32_t b) { return a & b; });
+  any = wave_all(any, [](uint32_t a, uint32_t b) { return a | b; });
   if (lane == 0) red_s[0][wave] = all, red_s[1][wave] = any;
+  if (tid < 256) hist_s[tid] = 0;
+  if (tid == 0) n_list = 0;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < KT / 64; ++i) all &= red_s[0][i], any |= red_s[1][i];
-  const u64 diff = all ^ any;
+  for (int i = 0; i < KW; ++i) all &= red_s[0][i], any |= red_s[1][i];
   // ---- the threshold: keys whose bits from `shift` up are above `prefix` are taken,
   // of those that equal it `left` (from the smallest index on)
-  int shift = diff ? 64 - __builtin_clzll(diff) : 0, left = p.budget;
-  u64 prefix = shift == 64 ? 0 : all >> shift;
-  bool split = diff != 0;  // keys at the threshold are not all taken
+  const int kept = min(n, p.n_first) + min(max(0, n - p.n_first), p.n_last);
+  int shift = 64 - __builtin_clz((all ^ any) | 1), left = p.budget - kept;
+  u64 prefix = shift == 64 ? 0 : (u64)all << 32 >> shift;
+  bool split = left > 0;  // of the keys at the threshold some are taken, or none at all
   while (split && shift > 0) {
     const int bits = min(8, shift), low = shift - bits;
-    if (tid < 256) hist_s[tid] = 0;
-    __syncthreads();
-    each([&](u64 k, int) {
+    each([&](u64 k) {
       if (shift == 64 || k >> shift == prefix) atomicAdd(&hist_s[(k >> low) & ((1u << bits) - 1)], 1u);
     });
     __syncthreads();
     if (wave == 0) {  // lane: bins 255 - 4 lane .. 252 - 4 lane, the largest first
-      unsigned h[4], sum = 0;
+      int h[4], sum = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum += h[j] = hist_s[255 - 4 * lane - j];
-      unsigned upto = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const unsigned u = __shfl_up(upto, o, 64);
-        upto += lane >= o ? u : 0;
-      }
-      unsigned before = upto - sum;
+      for (int j = 0; j < 4; ++j) sum += h[j] = (int)hist_s[255 - 4 * lane - j];
+      int before = wave_incl(sum) - sum;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (before < (unsigned)left && before + h[j] >= (unsigned)left) {
+        if (before < left && before + h[j] >= left) {
           bin_s = 255 - 4 * lane - j;
-          above_s = (int)before;
+          above_s = before;
+          in_s = h[j];
         }
         before += h[j];
+        hist_s[255 - 4 * lane - j] = 0;
       }
     }
     __syncthreads();
-    const int bin = bin_s;
     left -= above_s;
-    split = hist_s[bin] != (unsigned)left;
-    prefix = (shift == 64 ? 0 : prefix << bits) | (u64)bin;
+    split = in_s != left;
+    prefix = (shift == 64 ? 0 : prefix << bits) | (u64)bin_s;
     shift = low;
-    __syncthreads();
+    if (split && shift > 0 && in_s <= 64) {
+      // a wave's worth of keys at the threshold: the left-th largest of them
+      each([&](u64 k) {
+        if (k >> shift == prefix) list_s[atomicAdd(&n_list, 1)] = k;
+      });
+      __syncthreads();
+      if (wave == 0) {
+        const u64 mine = list_s[min(lane, in_s - 1)];
+        int above = 0, same = 0;
+        for (int i = 0; i < in_s; ++i) {
+          const u64 k = list_s[i];
+          above += k > mine;
+          same += k == mine;
+        }
+        if (lane < in_s && above < left && above + same >= left) {  // (alike in all lanes that hold it)
+          pick_s = mine;
+          above_s = above;
+        }
+      }
+      __syncthreads();
+      prefix = pick_s;
+      left -= above_s;
+      shift = 0;
+    }
   }
-  // ---- the taken pages in order
-  int done = 0, ties = 0;  // written, and met at the threshold, in the rounds before
-  for (int j = 0; j < rounds; ++j) {
-    const int i = j * KT + tid;
-    u64 k = 0;
-    if (j < REG) {
+  // ---- the taken pages in order, REG rounds of them at a time
+  int done = 0, ties = 0;  // written, and met at the threshold, before
+  for (int r0 = 0; r0 < rounds; r0 += REG) {
+    if (r0 > 0) {
 #pragma unroll
-      for (int r = 0; r < REG; ++r) k = r == j ? kr[r] : k;
-    } else if (i < n) {
-      k = keys[i];
+      for (int j = 0; j < REG; ++j) kr[j] = keys[min((r0 + j) * KT + tid, n - 1)];
+      __syncthreads();  // the counts of the rounds before are read
     }
-    const u64 top = shift == 64 ? 0 : k >> shift;
-    const bool tie = i < n && top == prefix;
-    bool take = i < n && top > prefix;
-    const u64 tb = __ballot(tie);
-    if (lane == 0) cnt_s[wave] = __popcll(tb);
-    __syncthreads();
-    int before = ties, sum = 0;
+    u64 tb[REG], ab[REG];  // the wave's pages at and above the threshold
 #pragma unroll
-    for (int w = 0; w < KT / 64; ++w) {
-      before += w < wave ? cnt_s[w] : 0;
-      sum += cnt_s[w];
+    for (int j = 0; j < REG; ++j) {
+      const bool on = (r0 + j) * KT + tid < n;
+      const u64 top = shift == 64 ? 0 : kr[j] >> shift;
+      tb[j] = __ballot(on && kr[j] != kKept && top == prefix);
+      ab[j] = __ballot(on && (kr[j] == kKept || top > prefix));
+      if (lane == 0) cnt_s[0][j][wave] = __popcll(tb[j]), cnt_s[1][j][wave] = __popcll(ab[j]);
     }
-    ties += sum;
-    take |= tie && before + __popcll(tb & ((1ull << lane) - 1)) < left;
     __syncthreads();
-    const u64 b = __ballot(take);
-    if (lane == 0) cnt_s[wave] = __popcll(b);
-    __syncthreads();
-    int at = done;
-    sum = 0;
+    // counts before each (round, wave): lane: round lane / 16 (+ 4), wave lane % 16
+    int t0 = 0, t1 = 0, a0 = 0, a1 = 0;
+    {
+      const int j = lane >> 4, w = lane & 15;
+      t0 = cnt_s[0][j][w], t1 = cnt_s[0][j + 4][w];
+      a0 = cnt_s[1][j][w], a1 = cnt_s[1][j + 4][w];
+    }
+    static_assert(REG == 8 && KW == 16, "two counts a lane");
+    const int ti0 = wave_incl(t0), ti1 = wave_incl(t1) + lane_of(ti0, 63);
+    // of a group of ties, those below `left` are taken
+    auto taken = [&](int upto, int n_ties) { return max(0, min(n_ties, left - (ties + upto - n_ties))); };
+    const int b0 = a0 + taken(ti0, t0), b1 = a1 + taken(ti1, t1);
+    const int bi0 = wave_incl(b0), bi1 = wave_incl(b1) + lane_of(bi0, 63);
 #pragma unroll
-    for (int w = 0; w < KT / 64; ++w) {
-      at += w < wave ? cnt_s[w] : 0;
-      sum += cnt_s[w];
+    for (int j = 0; j < REG; ++j) {
+      if (r0 + j >= rounds) break;
+      const int from = (j & 3) * 16 + __builtin_amdgcn_readfirstlane(wave);
+      const int t_before = ties + lane_of(j < 4 ? ti0 - t0 : ti1 - t1, from);
+      int at = done + lane_of(j < 4 ? bi0 - b0 : bi1 - b1, from);
+      const u64 below = (1ull << lane) - 1;
+      const int my_ties = __popcll(tb[j] & below);
+      const bool tie = tb[j] >> lane & 1, take = (ab[j] >> lane & 1) || (tie && t_before + my_ties < left);
+      at += __popcll(ab[j] & below) + max(0, min(my_ties, left - t_before));
+      if (take) sel[at] = (r0 + j) * KT + tid;
     }
-    done += sum;
-    at += __popcll(b & ((1ull << lane) - 1));
-    if (take) sel[at] = i;
-    __syncthreads();
+    ties += lane_of(ti1, 63);
+    done += lane_of(bi1, 63);
   }
 }
 

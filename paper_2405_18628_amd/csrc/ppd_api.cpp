@@ -609,6 +609,7 @@ ppd_status step_bf16(const ppd_model *m, int B, const ppd_kv *kvs, const int32_t
       pa.pages = (const unsigned char *)kv.pages + layer_pages * (kv.page / kPB) * kPBytes;
       pa.tk = sb.k[0];
       pa.tv = sb.v[0];
+      pa.ctr = attn_ctr + (size_t)l * 256;
       timer_events(TK_ATTN, &pa.ev_start, &pa.ev_stop);
       PPD_TRY_HIP(launch_paged_attn(pa, s));
     } else {
@@ -776,7 +777,9 @@ size_t ppd_workspace_bytes(const ppd_model *model, int32_t t_max, int32_t max_le
 ppd_status ppd_workspace_init(void *ws, size_t ws_bytes, void *stream) {
   const size_t need = align_up(16);  // the header: the status word
   if (!ws || ws_bytes < need) return fail(PPD_EWORKSPACE, "workspace needs at least %zu bytes", need);
-  PPD_TRY_HIP(launch_ws_init(ws, need / 4, (hipStream_t)stream));
+  // (with the counters of ppd_paged_attention's workspace)
+  const size_t bytes = std::min(ws_bytes, need + kPagedCounters) & ~(size_t)3;
+  PPD_TRY_HIP(launch_ws_init(ws, bytes / 4, (hipStream_t)stream));
   return PPD_OK;
 }
 

@@ -219,7 +219,7 @@ size_t ppd_paged_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, 
              PPD_PAGED_SEQS_MAX, kMaxRows);
     return 0;
   }
-  return kHeader + (size_t)PPD_PAGED_SEQS_MAX * sizeof(int2) + paged_attn_part_bytes(n_heads, n_kv_heads, n_seqs, n_rows);
+  return kHeader + kPagedCounters + (size_t)PPD_PAGED_SEQS_MAX * sizeof(int2) + paged_attn_part_bytes(n_heads, n_kv_heads, n_seqs, n_rows);
 }
 
 ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,
@@ -253,8 +253,9 @@ ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t lay
   a.nh = n_heads;
   a.nkv = kv->n_kv_heads;
   a.status = (uint32_t *)ws;
-  a.rec = (int2 *)((char *)ws + kHeader);
-  a.part = (float *)((char *)ws + kHeader + PPD_PAGED_SEQS_MAX * sizeof(int2));
+  a.ctr = (uint32_t *)((char *)ws + kHeader);  // (zeroed by ppd_workspace_init)
+  a.rec = (int2 *)((char *)ws + kHeader + kPagedCounters);
+  a.part = (float *)(a.rec + PPD_PAGED_SEQS_MAX);
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt(128.0));
   paged_attn_shape(a);
   PPD_TRY_HIP(launch_paged_attn(a, (hipStream_t)stream));

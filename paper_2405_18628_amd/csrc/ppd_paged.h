@@ -42,6 +42,42 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs &p, int s, bool *b
 }
 __device__ __forceinline__ int paged_clamp(int page, int n_pages) { return max(0, min(page, n_pages - 1)); }
 
+// ---- over a wave with cross-lane moves (no LDS round trips): inclusive sums, and
+// sums, ands and ors that every lane gets
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int lane_move(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_incl(int v) {
+  v += lane_move<0x111>(v);       // row_shr:1, 2, 4, 8
+  v += lane_move<0x112>(v);
+  v += lane_move<0x114>(v);
+  v += lane_move<0x118>(v);
+  v += lane_move<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+  v += lane_move<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+  return v;
+}
+template <typename F>
+__device__ __forceinline__ uint32_t wave_all(uint32_t v, F f) {
+  v = f(v, (uint32_t)lane_move<0xb1>((int)v));   // quad_perm: pairs, then pairs of pairs
+  v = f(v, (uint32_t)lane_move<0x4e>((int)v));
+  v = f(v, (uint32_t)lane_move<0x141>((int)v));  // row_half_mirror
+  v = f(v, (uint32_t)lane_move<0x140>((int)v));  // row_mirror
+  auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = f(a[0], a[1]);
+  auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(b[0], b[1]);
+}
+// (whole numbers below 2^53; 24 bits at a time, so that 64 of them fit)
+__device__ __forceinline__ int64_t wave_total(int64_t v) {
+  auto add = [](uint32_t a, uint32_t b) { return a + b; };
+  int64_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) sum += (int64_t)wave_all((uint32_t)(v >> 24 * i) & 0xffffffu, add) << 24 * i;
+  return sum;
+}
+__device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
 // The sequence of a row: the last one whose rows start at or before it.  Called
 // by a whole wave, `tok` alike in its lanes.
 __device__ __forceinline__ int paged_seq_of(const int32_t *row_start, int B, int tok) {
@@ -90,16 +126,20 @@ struct PagedAttnLaunch {
   const int32_t *sel, *n_sel;  // [B][nkv][budget], [B], or null
   int budget;
   int nh, nkv;
-  float *part;                 // [kPagedSlots][rows of a workgroup][PPD_ATTN_OROW]
+  float *part;                 // [2 paged_slots][rows of a workgroup][PPD_ATTN_OROW]
   int2 *rec;                   // [B]: splits, first of the partial rows' workgroups
+  uint32_t *ctr;               // arrivals of row groups' splits, a byte each: zero between launches
   uint32_t *status;
   float scale_log2;
   int tiles;                   // 16-row tiles of a kv head's rows, by which the kernel's shape is chosen
   int may_split;               // a sequence can be long enough for more than one workgroup
   void *ev_start, *ev_stop;
 };
-// workgroups that share a call's keys; also bounds those that leave partial rows
-constexpr int kPagedSlots = 256;
+// Workgroups that a call's keys are divided among, by the tiles of one: as many as
+// are on the device together
+constexpr int paged_slots(int tiles) { return tiles == 1 ? 512 : 256; }
+constexpr int kPagedSplits = 128;  // most splits of a row group (a byte counts them)
+constexpr size_t kPagedCounters = 512;  // bytes of them: paged_slots(1) row groups at most have several
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows);
 void paged_attn_shape(PagedAttnLaunch &a);  // fills tiles, may_split
 hipError_t launch_paged_attn(const PagedAttnLaunch &a, hipStream_t s);
