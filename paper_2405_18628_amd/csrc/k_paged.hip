@@ -186,143 +186,281 @@ __global__ __launch_bounds__(256) void paged_fill_kernel(PagedTablesLaunch p) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows into pages.  A run is the rows of one sequence that fall into one page; a
-// wave takes a run of one (layer, kv head), so a page's bounds have one writer
-// and no atomics.  Keys move as 16-byte pieces (8 dims of a position), values
-// are turned: 8 positions of a dim are 16 bytes of a block, read at once where the
-// source holds them side by side.
+// Rows into pages.  A run is the rows of one sequence that fall into one page; it
+// is one workgroup's for each (layer, kv head), so a page's bounds have one
+// writer and no atomics.  Keys move as 16-byte pieces (8 dims of a position, 16
+// lanes a row), values are turned: 8 positions of a dim are 16 bytes of a block.
+//
+// Accepted rows and single tokens (paged_put_kernel): a wave a run, eight rows at
+// a time, values element by element, a lane two dims; keys, values and bounds
+// requested together, since a call takes round trips and the lines it touches
+// in part rather than bytes.  Prompts (paged_fill_kernel): up to four waves a run,
+// a block of 32 positions each, values 16 bytes at a time -- of a source that is
+// not aligned by eights two neighbouring pieces shifted into one -- and the waves'
+// bounds joined in LDS.
 
-constexpr int SW = 4;    // waves of a workgroup
-constexpr int SR = 128;  // rows of a workgroup
+constexpr int SW = 4;     // waves of a workgroup
+constexpr int SB = 255;   // sequences whose offsets fit its LDS
+constexpr int FEW = 8;    // rows that a wave has in flight
 
 __device__ __forceinline__ float lo_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-__global__ __launch_bounds__(64 * SW) void paged_store_kernel(PagedStoreLaunch p) {
-  __shared__ int4 run_s[SR];  // first row, rows, sequence
-  __shared__ int n_run;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int P = 1 << p.lp;
-  const int n = max(0, min(p.start[p.B], p.n_rows));
+// smallest and largest of a lane's 8 dims (what is left of NaN alone: infinities)
+struct Bounds8 {
+  float mn[8], mx[8];
+  __device__ __forceinline__ Bounds8() {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mn[e] = INFINITY, mx[e] = -INFINITY;
+  }
+  __device__ __forceinline__ void add(u32x4 lo, u32x4 hi) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      mn[e] = fminf(mn[e], e & 1 ? hi_of(lo[e >> 1]) : lo_of(lo[e >> 1]));
+      mx[e] = fmaxf(mx[e], e & 1 ? hi_of(hi[e >> 1]) : lo_of(hi[e >> 1]));
+    }
+  }
+  // over the wave's four rows of 16 lanes
+  __device__ __forceinline__ void join() {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      mn[e] = -quad_max(-mn[e]);
+      mx[e] = quad_max(mx[e]);
+    }
+  }
+  __device__ __forceinline__ void store(u32x4 *smallest, u32x4 *largest) const {
+    u32x4 lo, hi;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      lo[e] = pack_bf16x2(mn[2 * e], mn[2 * e + 1]);
+      hi[e] = pack_bf16x2(mx[2 * e], mx[2 * e + 1]);
+    }
+    *smallest = lo;
+    *largest = hi;
+  }
+};
+
+// The runs that start among `rows` rows (SR at most), from row `at` on, in LDS;
+// false: there are no rows from there on.
+template <int SR>
+struct Runs {
+  int4 run[SR];  // first row, rows, sequence, slot
+  int start[SB + 1], rows[SB + 1];
+  int n;
+};
+template <int SR>
+__device__ __forceinline__ void load_offsets(Runs<SR> &s, const PagedStoreLaunch &p) {
+  const int tid = threadIdx.x;
+  if (p.B <= SB && tid <= p.B) {
+    s.start[tid] = p.start[tid];
+    s.rows[tid] = tid < p.B ? p.row_start[tid] : 0;
+  }
+}
+template <int SR>
+__device__ __forceinline__ bool find_runs(Runs<SR> &s, const PagedStoreLaunch &p, int64_t at, int rows) {
+  const int tid = threadIdx.x, P = 1 << p.lp;
+  const int32_t *start = p.B <= SB ? s.start : p.start;
+  const int i = (int)at + tid;
+  const int slot = tid < rows && i < p.n_rows ? p.slots[i] : -1;
+  __syncthreads();  // the offsets are there, the last rows' runs done
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  const int n = min(start[p.B], p.n_rows);
+  if (at >= n) return false;
+  if (tid < rows && i < n) {
+    int lo = 0, hi = p.B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (start[mid] <= i)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    const int first = start[lo];
+    if (i >= first && slot >= 0 && (slot >> p.lp) < p.n_pages && (i == first || (slot & (P - 1)) == 0)) {
+      const int m = min(P - (slot & (P - 1)), min(start[lo + 1], n) - i);
+      s.run[atomicAdd(&s.n, 1)] = int4{i, m, lo, slot};  // (runs are independent of one another)
+    }
+  }
+  __syncthreads();
+  return true;
+}
+
+// a run as a wave takes it
+struct Run {
+  int m, off;         // rows, position of the first in its page
+  int base, k0;       // the sequence's first row of the source, the run's first of its rows
+  unsigned char *dst;
+  bf16_t *bounds;
+};
+template <int SR>
+__device__ __forceinline__ Run take_run(const Runs<SR> &s, const PagedStoreLaunch &p, int r, int layer, int kvh) {
+  const int4 run = s.run[r];
+  const int sq = __builtin_amdgcn_readfirstlane(run.z), page = __builtin_amdgcn_readfirstlane(run.w >> p.lp);
+  Run x;
+  x.m = __builtin_amdgcn_readfirstlane(run.y);
+  x.off = __builtin_amdgcn_readfirstlane(run.w & ((1 << p.lp) - 1));
+  const bool near = p.B <= SB;
+  x.base = __builtin_amdgcn_readfirstlane(near ? s.rows[sq] : p.row_start[sq]);
+  x.k0 = __builtin_amdgcn_readfirstlane(run.x - (near ? s.start[sq] : p.start[sq]));
+  const size_t head = ((size_t)layer * p.n_pages + page) * p.nkv + kvh;
+  x.dst = p.pages + head * ((size_t)kPBytes << (p.lp - 5));
+  x.bounds = p.bounds ? p.bounds + head * 256 : nullptr;
+  return x;
+}
+
+constexpr int PUT_ROWS = 128;
+
+__global__ __launch_bounds__(64 * SW) void paged_put_kernel(PagedStoreLaunch p) {
+  __shared__ Runs<PUT_ROWS> runs;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  load_offsets(runs, p);
   const int lh = blockIdx.x / p.chunks, layer = lh / p.nkv, kvh = lh % p.nkv;
   const bf16_t *k = p.k + (size_t)lh * p.scap * 128, *v = p.v + (size_t)lh * 128 * p.scap;
-  for (int64_t at = (int64_t)(blockIdx.x % p.chunks) * SR; at < n; at += (int64_t)p.chunks * SR) {
-    const int i0 = (int)at;
-    __syncthreads();  // the last rows' runs are done
-    if (tid == 0) n_run = 0;
-    __syncthreads();
-    const int i = i0 + tid;
-    if (tid < SR && i < n) {
-      int lo = 0, hi = p.B - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.start[mid] <= i)
-          lo = mid;
-        else
-          hi = mid - 1;
+  const int piece = lane & 15;
+  for (int64_t at = (int64_t)(blockIdx.x % p.chunks) * PUT_ROWS; at < p.n_rows; at += (int64_t)p.chunks * PUT_ROWS) {
+    if (!find_runs(runs, p, at, PUT_ROWS)) return;
+    for (int r = wave; r < runs.n; r += SW) {
+      const Run run = take_run(runs, p, r, layer, kvh);
+      u32x4 was[2] = {};
+      if (run.bounds && run.off && lane < 16) {
+        was[0] = *((const u32x4 *)run.bounds + piece);
+        was[1] = *((const u32x4 *)run.bounds + 16 + piece);
       }
-      const int first = p.start[lo], slot = p.slots[i];
-      if (i >= first && slot >= 0 && (slot >> p.lp) < p.n_pages && (i == first || (slot & (P - 1)) == 0)) {
-        const int m = min(P - (slot & (P - 1)), min(p.start[lo + 1], n) - i);
-        run_s[atomicAdd(&n_run, 1)] = int4{i, m, lo, slot};  // (runs are independent of one another)
+      Bounds8 bd;
+      for (int j0 = 0; j0 < run.m; j0 += FEW) {
+        const int m = min(FEW, run.m - j0);
+        // lane j: the source's row of row j0 + j (past the last: the last again)
+        int64_t row = (int64_t)run.base + run.k0 + j0 + min(lane, m - 1);
+        if (p.path) row = (int64_t)run.base + p.path[max((int64_t)0, min(row, (int64_t)p.n_path - 1))];
+        const int mine = (int)max((int64_t)0, min(row, (int64_t)p.scap - 1));
+        u32x4 kw[FEW / 4];
+        bf16_t vw[FEW][2];
+#pragma unroll
+        for (int j = 0; j < FEW / 4; ++j)
+          kw[j] = *(const u32x4 *)(k + (size_t)__shfl(mine, min(4 * j + (lane >> 4), m - 1), 64) * 128 + piece * 8);
+#pragma unroll
+        for (int j = 0; j < FEW; ++j) {
+          const int from = lane_of(mine, j);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (j < m) vw[j][h] = v[(size_t)(lane + 64 * h) * p.scap + from];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < FEW / 4; ++j) {
+          const int pos = run.off + j0 + 4 * j + (lane >> 4);
+          if (4 * j + (lane >> 4) < m) {
+            *(u32x4 *)(run.dst + (size_t)(pos >> 5) * kPBytes + 2 * paged_key_at(pos & 31, piece * 8)) = kw[j];
+            bd.add(kw[j], kw[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < FEW; ++j) {
+          const int pos = run.off + j0 + j;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (j < m) ((bf16_t *)(run.dst + (size_t)(pos >> 5) * kPBytes))[kPElems + paged_value_at(pos & 31, lane + 64 * h)] = vw[j][h];
+        }
+      }
+      if (run.bounds) {
+        bd.join();
+        if (lane < 16) {
+          if (run.off) bd.add(was[0], was[1]);
+          bd.store((u32x4 *)run.bounds + piece, (u32x4 *)run.bounds + 16 + piece);
+        }
       }
     }
-    __syncthreads();
-    for (int r = wave; r < n_run; r += SW) {
-      const int4 run = run_s[r];
-      const int m = run.y, page = run.w >> p.lp, off = run.w & (P - 1);
-      const int first = p.start[run.z], base = p.row_start[run.z], k0 = run.x - first;
-      auto source = [&](int j) {  // the source's row of the run's row j
-        int row = base + k0 + j;
-        if (p.path) row = base + p.path[max(0, min(row, p.n_path - 1))];
-        return max(0, min(row, p.scap - 1));
-      };
-      unsigned char *dst = p.pages + (((size_t)layer * p.n_pages + page) * p.nkv + kvh) * ((size_t)kPBytes << (p.lp - 5));
-      // ---- keys: 16 lanes a row
-      const int piece = lane & 15;
-      float mn[8], mx[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mn[e] = INFINITY, mx[e] = -INFINITY;  // (what is left of NaN alone)
-      constexpr int U = 4;  // rows of a lane in flight
-      for (int j0 = lane >> 4; j0 < m; j0 += 4 * U) {
-        u32x4 w[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = *(const u32x4 *)(k + (size_t)source(min(j0 + 4 * u, m - 1)) * 128 + piece * 8);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int j = j0 + 4 * u;
-          if (j >= m) break;
-          const int pos = off + j;
-          *(u32x4 *)(dst + (size_t)(pos >> 5) * kPBytes + 2 * paged_key_at(pos & 31, piece * 8)) = w[u];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = e & 1 ? hi_of(w[u][e >> 1]) : lo_of(w[u][e >> 1]);
-            mn[e] = fminf(mn[e], x);
-            mx[e] = fmaxf(mx[e], x);
-          }
-        }
+  }
+}
+
+constexpr int FILL_ROWS = 256;
+
+__global__ __launch_bounds__(64 * SW) void paged_fill_rows_kernel(PagedStoreLaunch p) {
+  __shared__ Runs<FILL_ROWS> runs;
+  __shared__ __attribute__((aligned(16))) u32x4 join_s[SW][2][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int piece = lane & 15, lg = lane >> 4;
+  load_offsets(runs, p);
+  const int lh = blockIdx.x / p.chunks, layer = lh / p.nkv, kvh = lh % p.nkv;
+  const bf16_t *k = p.k + (size_t)lh * p.scap * 128, *v = p.v + (size_t)lh * 128 * p.scap;
+  const int each = min(SW, 1 << (p.lp - 5)), sub = wave % each;  // waves of a run, this one among them
+  const int rows = p.rows_each;
+  for (int64_t at = (int64_t)(blockIdx.x % p.chunks) * rows; at < p.n_rows; at += (int64_t)p.chunks * rows) {
+    if (!find_runs(runs, p, at, rows)) return;
+    for (int r0 = 0; r0 < runs.n; r0 += SW / each) {  // (alike in all waves: they meet below)
+      const bool on = r0 + wave / each < runs.n;
+      const Run run = take_run(runs, p, on ? r0 + wave / each : r0, layer, kvh);
+      Bounds8 bd;
+      u32x4 was[2] = {};
+      if (run.bounds && run.off && lane < 16) {
+        was[0] = *((const u32x4 *)run.bounds + piece);
+        was[1] = *((const u32x4 *)run.bounds + 16 + piece);
       }
-      if (p.bounds) {
-        bf16_t *b = p.bounds + (((size_t)layer * p.n_pages + page) * p.nkv + kvh) * 256 + piece * 8;
+      const int first = run.off >> 5, last = on ? (run.off + run.m - 1) >> 5 : -1;
+      const int64_t src = (int64_t)run.base + run.k0 - run.off;  // the source's row of the page's position 0
+      for (int blk = first + sub; blk <= last; blk += each) {
+        const int p0 = max(run.off, blk * 32), p1 = min(run.off + run.m, blk * 32 + 32);  // its positions
+        u32x4 kw[8], vw[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-#pragma unroll
-          for (int o = 16; o < 64; o <<= 1) {
-            mn[e] = fminf(mn[e], __shfl_xor(mn[e], o, 64));
-            mx[e] = fmaxf(mx[e], __shfl_xor(mx[e], o, 64));
-          }
+        for (int j = 0; j < 8; ++j) {
+          const int64_t row = src + max(p0, min(blk * 32 + 4 * j + lg, p1 - 1));
+          kw[j] = *(const u32x4 *)(k + (size_t)max((int64_t)0, min(row, (int64_t)p.scap - 1)) * 128 + piece * 8);
         }
-        if (lane < 16) {
-          if (off) {
-            const u32x4 a = *(const u32x4 *)b, c = *(const u32x4 *)(b + 128);
+        // values: dim 16 t + lane % 16, positions 8 lg .. + 7 of the block
+        const int64_t s0 = src + blk * 32 + 8 * lg;
+        const int part = (int)(s0 & 7);  // alike in the wave
+        const int64_t most = p.scap - 8, a0 = max((int64_t)0, min(s0 - part, most));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              mn[e] = fminf(mn[e], e & 1 ? hi_of(a[e >> 1]) : lo_of(a[e >> 1]));
-              mx[e] = fmaxf(mx[e], e & 1 ? hi_of(c[e >> 1]) : lo_of(c[e >> 1]));
-            }
-          }
-          u32x4 a, c;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            a[e] = pack_bf16x2(mn[2 * e], mn[2 * e + 1]);
-            c[e] = pack_bf16x2(mx[2 * e], mx[2 * e + 1]);
-          }
-          *(u32x4 *)b = a;
-          *(u32x4 *)(b + 128) = c;
-        }
-      }
-      // ---- values: blocks of 32 positions, lane: dim 16 w + lane % 16, positions 8 (lane / 16) ..
-      for (int blk = off >> 5; blk <= (off + m - 1) >> 5; ++blk) {
-        const int u0 = blk * 32 + 8 * (lane >> 4) - off;       // the run's row of the lane's first position
-        const int from = max(0, -u0), to = min(8, m - u0);     // its positions that are of the run
-        if (from >= to) continue;
-        const int s0 = p.path ? 0 : base + k0 + u0;
-        const bool whole = from == 0 && to == 8;
-        unsigned char *d = dst + (size_t)blk * kPBytes + 2 * kPElems + lane * 16;
-        if (whole && !p.path && s0 % 8 == 0 && s0 >= 0 && s0 + 8 <= p.scap) {
-          u32x4 w[8];
-#pragma unroll
-          for (int t = 0; t < 8; ++t) w[t] = *(const u32x4 *)(v + (size_t)(16 * t + (lane & 15)) * p.scap + s0);
-#pragma unroll
-          for (int t = 0; t < 8; ++t) *(u32x4 *)(d + t * 1024) = w[t];
-        } else {
-          int src[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) src[e] = source(max(0, min(u0 + e, m - 1)));
+        for (int t = 0; t < 8; ++t) vw[t] = *(const u32x4 *)(v + (size_t)(16 * t + piece) * p.scap + a0);
+        if (part) {
+          const int64_t a1 = max((int64_t)0, min(s0 - part + 8, most));
+          const int q = part >> 1, odd = 16 * (part & 1);
 #pragma unroll
           for (int t = 0; t < 8; ++t) {
-            const bf16_t *row = v + (size_t)(16 * t + (lane & 15)) * p.scap;
-            uint32_t x[8];
+            const u32x4 more = *(const u32x4 *)(v + (size_t)(16 * t + piece) * p.scap + a1);
+            const uint32_t w[9] = {vw[t][0], vw[t][1], vw[t][2], vw[t][3], more[0], more[1], more[2], more[3], 0u};
+            uint32_t x[5];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = row[src[e]];
-            if (whole) {
-              *(u32x4 *)(d + t * 1024) = u32x4{x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16};
-            } else {
+            for (int e = 0; e < 5; ++e) x[e] = q == 0 ? w[e] : q == 1 ? w[e + 1] : q == 2 ? w[e + 2] : w[e + 3];
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (e >= from && e < to) ((bf16_t *)(d + t * 1024))[e] = (bf16_t)x[e];
-            }
+            for (int e = 0; e < 4; ++e) vw[t][e] = __builtin_amdgcn_alignbit(x[e + 1], x[e], odd);
           }
+        }
+        unsigned char *d = run.dst + (size_t)blk * kPBytes;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int pos = blk * 32 + 4 * j + lg;
+          if (pos >= p0 && pos < p1) {
+            *(u32x4 *)(d + 2 * paged_key_at(pos & 31, piece * 8)) = kw[j];
+            bd.add(kw[j], kw[j]);
+          }
+        }
+        const int from = max(0, p0 - (blk * 32 + 8 * lg)), to = min(8, p1 - (blk * 32 + 8 * lg));
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          unsigned char *dv = d + 2 * kPElems + t * 1024 + lane * 16;
+          if (from == 0 && to == 8) {
+            *(u32x4 *)dv = vw[t];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e >= from && e < to) ((bf16_t *)dv)[e] = (bf16_t)(vw[t][e >> 1] >> 16 * (e & 1));
+          }
+        }
+      }
+      if (p.bounds) {  // (alike in all waves)
+        bd.join();
+        if (each > 1) {
+          if (lane < 16) bd.store(&join_s[wave][0][lane], &join_s[wave][1][lane]);
+          __syncthreads();
+          if (sub == 0 && lane < 16)
+            for (int w = 1; w < each; ++w) bd.add(join_s[wave + w][0][lane], join_s[wave + w][1][lane]);
+          __syncthreads();
+        }
+        if (on && sub == 0 && lane < 16) {
+          if (run.off) bd.add(was[0], was[1]);
+          bd.store((u32x4 *)run.bounds + piece, (u32x4 *)run.bounds + 16 + piece);
         }
       }
     }
@@ -349,7 +487,9 @@ hipError_t launch_paged_tables(const PagedTablesLaunch &p, hipStream_t s) {
 hipError_t launch_paged_store(PagedStoreLaunch p, hipStream_t s) {
   // (a launch's threads are counted in 32 bits: of very many rows a workgroup takes several parts)
   const int heads = p.layers * p.nkv;
-  p.chunks = std::min((p.n_rows - 1) / SR + 1, std::max(1, (1 << 22) / heads));
-  hipLaunchKernelGGL(paged_store_kernel, dim3(heads * p.chunks), dim3(64 * SW), 0, s, p);
+  const bool put = p.path || p.n_rows <= FEW * (int64_t)p.B;
+  p.rows_each = put ? PUT_ROWS : std::max(128, 1 << p.lp);
+  p.chunks = std::min((p.n_rows - 1) / p.rows_each + 1, std::max(1, (1 << 22) / heads));
+  hipLaunchKernelGGL(put ? paged_put_kernel : paged_fill_rows_kernel, dim3(heads * p.chunks), dim3(64 * SW), 0, s, p);
   return hipGetLastError();
 }

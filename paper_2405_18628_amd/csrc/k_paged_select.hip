@@ -33,31 +33,20 @@ __device__ __forceinline__ u64 key_of(double v) {
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
-// 8 elements of a query row
+// elements d, d + 1 of a query row
 template <int QT>
-__device__ __forceinline__ void query8(const PagedSelectLaunch &p, int tok, int head, int d, float (&v)[8]) {
-  if constexpr (QT == PAGED_Q_F32) {
-    const float *src = (const float *)p.q + ((size_t)tok * p.nh + head) * 128 + d;
-    const floatx4 a = *(const floatx4 *)src, b = *(const floatx4 *)(src + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
-  } else if constexpr (QT == PAGED_Q_BF16) {
-    const u32x4 a = *(const u32x4 *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + d);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? a[e >> 1] & 0xffff0000u : a[e >> 1] << 16);
-  } else {
-    const unsigned char *src = (const unsigned char *)p.q + plane_off(p.T_pad >> 4, tok, head * 128 + d);
-    const u32x4 a = *(const u32x4 *)src, b = *(const u32x4 *)(src + kPlaneLo);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      v[e] = __uint_as_float(e & 1 ? a[e >> 1] & 0xffff0000u : a[e >> 1] << 16) +
-             __uint_as_float(e & 1 ? b[e >> 1] & 0xffff0000u : b[e >> 1] << 16);
-  }
+__device__ __forceinline__ float2 query2(const PagedSelectLaunch &p, int tok, int head, int d) {
+  auto pair = [](uint32_t w) { return float2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; };
+  if constexpr (QT == PAGED_Q_F32) return *(const float2 *)((const float *)p.q + ((size_t)tok * p.nh + head) * 128 + d);
+  if constexpr (QT == PAGED_Q_BF16) return pair(*(const uint32_t *)((const bf16_t *)p.q + ((size_t)tok * p.nh + head) * 128 + d));
+  const unsigned char *src = (const unsigned char *)p.q + plane_off(p.T_pad >> 4, tok, head * 128 + d);
+  const float2 hi = pair(*(const uint32_t *)src), lo = pair(*(const uint32_t *)(src + kPlaneLo));
+  return float2{hi.x + lo.x, hi.y + lo.y};
 }
 
 template <int QT>
 __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, int chunks) {
-  __shared__ double sum_s[ST / 16][2][128];
+  __shared__ double sum_s[ST / 64][2][128];
   __shared__ double q_s[2][128];  // Qm, Qp
   const int tid = threadIdx.x, lane = tid & 63;
   const int c = blockIdx.x % chunks, kvh = blockIdx.x / chunks % p.nkv, sq = blockIdx.x / chunks / p.nkv;
@@ -78,30 +67,26 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
     w[i] = *(const u32x4 *)(p.bounds + ((size_t)page * p.nkv + kvh) * 256 + (lane & 31) * 8);
   }
   // ---- sums of the queries' positive and negative parts
-  const int G = p.nh / p.nkv, R = s.T * G, d8 = (tid & 15) * 8;
-  double qp[8], qm[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) qp[e] = qm[e] = 0.0;
-#pragma unroll 4
-  for (int r = tid >> 4; r < R; r += ST / 16) {
-    float v[8];
-    query8<QT>(p, s.t0 + r / G, kvh * G + r % G, d8, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      qp[e] += (double)(v[e] <= 0.f ? 0.f : v[e]);  // (a NaN stays one)
-      qm[e] += (double)(v[e] >= 0.f ? 0.f : v[e]);
-    }
+  const int G = p.nh / p.nkv, R = s.T * G, wave = tid >> 6;
+  double qp[2] = {0.0, 0.0}, qm[2] = {0.0, 0.0};
+#pragma unroll 8
+  for (int r = wave; r < R; r += ST / 64) {
+    const float2 x = query2<QT>(p, s.t0 + r / G, kvh * G + r % G, 2 * lane);
+    qp[0] += (double)(x.x <= 0.f ? 0.f : x.x);  // (a NaN stays one)
+    qp[1] += (double)(x.y <= 0.f ? 0.f : x.y);
+    qm[0] += (double)(x.x >= 0.f ? 0.f : x.x);
+    qm[1] += (double)(x.y >= 0.f ? 0.f : x.y);
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    sum_s[tid >> 4][0][d8 + e] = qm[e];
-    sum_s[tid >> 4][1][d8 + e] = qp[e];
+  for (int e = 0; e < 2; ++e) {
+    sum_s[wave][0][2 * lane + e] = qm[e];
+    sum_s[wave][1][2 * lane + e] = qp[e];
   }
   __syncthreads();
   {
     double x = 0.0;
 #pragma unroll
-    for (int i = 0; i < ST / 16; ++i) x += sum_s[i][tid >> 7][tid & 127];
+    for (int i = 0; i < ST / 64; ++i) x += sum_s[i][tid >> 7][tid & 127];
     q_s[tid >> 7][tid & 127] = x;
   }
   __syncthreads();
@@ -118,23 +103,24 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
       x = fma(q[e], (double)__uint_as_float(e & 1 ? w[i][e >> 1] & 0xffff0000u : w[i][e >> 1] << 16), x);
     v[i] = x;
   }
-  // each step halves the pages a lane holds: after three, lane bits 4, 3, 2 say which
+  // each step halves the pages a lane holds; which it is left with, its bits say
+  constexpr int NV = PAGES / 2;
+  int i = 0;
 #pragma unroll
-  for (int step = 0; step < 3; ++step) {
-    const int o = 16 >> step, half = (PAGES / 4) >> step;
+  for (int half = NV / 2, o = 16; half > 0; half /= 2, o /= 2) {
+    const bool up = lane & o;
 #pragma unroll
-    for (int i = 0; i < half; ++i) {
-      const bool up = lane & o;
-      const double mine = up ? v[i + half] : v[i], other = up ? v[i] : v[i + half];
-      v[i] = mine + __shfl_xor(other, o, 64);
+    for (int j = 0; j < half; ++j) {
+      const double mine = up ? v[j + half] : v[j], other = up ? v[j] : v[j + half];
+      v[j] = mine + __shfl_xor(other, o, 64);
     }
+    i = 2 * i + up;
   }
   double x = v[0];
-  x += __shfl_xor(x, 2, 64);
-  x += __shfl_xor(x, 1, 64);
-  const int i = (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2 + (lane >> 2 & 1);
+#pragma unroll
+  for (int o = 16 / NV; o > 0; o /= 2) x += __shfl_xor(x, o, 64);
   const int page = page0 + 2 * i + (lane >> 5);
-  if ((lane & 3) == 0 && page < n) {
+  if (lane % (32 / NV) == 0 && page < n) {
     const bool kept = page < p.n_first || page >= n - p.n_last;
     p.keys[((size_t)sq * p.nkv + kvh) * p.sq.max_pages + page] = kept ? kKept : key_of(x);
   }

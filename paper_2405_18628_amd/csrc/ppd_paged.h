@@ -106,7 +106,7 @@ struct PagedStoreLaunch {
   int layers, nkv, n_pages, lp, scap;
   int B, n_rows;
   int n_path;
-  int chunks;           // parts of the rows, workgroups a head (the launcher's)
+  int rows_each, chunks;  // rows of a part, parts that are workgroups of a head (the launcher's)
   const int32_t *start, *row_start, *path, *slots;
 };
 hipError_t launch_paged_store(PagedStoreLaunch p, hipStream_t s);
