@@ -577,7 +577,9 @@ size_t ppd_paged_bounds_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t n_pa
  * rows n_slots, and from the first of the others that the free pages do not
  * suffice for on, where it needs a page.
  *   ws      device workspace, 16-byte aligned, of
- *           ppd_paged_tables_workspace_bytes(n_seqs) (its header the status word)
+ *           ppd_paged_tables_workspace_bytes(n_seqs), one for each stream that
+ *           calls may overlap on, prepared once with ppd_workspace_init (the status
+ *           word and a counter that every call leaves zero)
  */
 size_t ppd_paged_tables_workspace_bytes(int32_t n_seqs);
 ppd_status ppd_paged_tables(const ppd_page_tables *pt, const int32_t *add, int32_t *len_out, int32_t *free_state_out,

@@ -10,179 +10,180 @@ namespace {
 // sequence gets follows from three running sums over the sequences: of added
 // rows (where its rows start), of new - old over those that fit the table and the
 // slot buffer (its first entry of the ring, and whether the ring suffices) and of
-// pages given back.  One workgroup forms them, a run of sequences a thread
-// (tables_plan); rows are then independent: a row finds its sequence by
-// bisection of the starts, and the first row of a new page writes the
-// table's entry, so every new page is written by exactly one row.
+// pages given back.  Every workgroup forms them for itself, a thread a sequence
+// (from 1025 sequences on several), in LDS: that takes less than another
+// launch.  Rows are then independent: a thread takes four, finds their sequence by
+// bisection of the starts, and the first row of a new page writes the table's
+// entry, so every new page is written by exactly one row.  Lengths and the ring's
+// state may be written where they are read: the last workgroup to have read
+// them does it.
 
 constexpr int TT = 1024;
 enum { kEnded = -1, kRefused = 0, kServed = 1 };
 
-// inclusive sum over the workgroup's threads; *all: of all of them
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *waves, int64_t *all) {
+struct TablesPlan {
+  int start[PPD_PAGED_SEQS_MAX + 1];
+  int len[PPD_PAGED_SEQS_MAX];
+  int at[PPD_PAGED_SEQS_MAX];  // ring index of the first new page, or place of the first given back; ~: refused
+  uint32_t ended[PPD_PAGED_SEQS_MAX / 32];
+};
+
+// inclusive sums over the workgroup's threads; all: of all of them
+template <int N>
+__device__ __forceinline__ void block_scan(int64_t (&v)[N], int64_t (&all)[N], int64_t (*waves)[N]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t u = __shfl_up(v, o, 64);
-    v += lane >= o ? u : 0;
+  for (int i = 0; i < N; ++i) {
+    v[i] = wave_incl64(v[i]);
+    if (lane == 63) waves[w][i] = v[i];
   }
-  if (lane == 63) waves[w] = v;
   __syncthreads();
-  int64_t before = 0, sum = 0;
 #pragma unroll
-  for (int i = 0; i < TT / 64; ++i) {
-    before += i < w ? waves[i] : 0;
-    sum += waves[i];
+  for (int i = 0; i < N; ++i) {
+    // lanes 0 .. 15: the waves' sums
+    const int64_t s = wave_incl64(lane < TT / 64 ? waves[min(lane, TT / 64 - 1)][i] : 0);
+    v[i] += w ? lane_of64(s, w - 1) : 0;
+    all[i] = lane_of64(s, TT / 64 - 1);
   }
-  __syncthreads();
-  *all = sum;
-  return v + before;
-}
-
-// a sequence's numbers as read, clamped
-struct TSeq {
-  int len, old, grow;
-  bool ended, bad;
-};
-__device__ __forceinline__ TSeq tables_seq(const PagedTablesLaunch &p, int s) {
-  TSeq q;
-  const int64_t most = (int64_t)p.max_pages << p.lp;
-  const int n = p.len[s], a = p.add[s];
-  q.len = (int)max((int64_t)0, min((int64_t)n, most));
-  q.bad = n != q.len;
-  q.old = (int)(((int64_t)q.len + (1 << p.lp) - 1) >> p.lp);
-  q.ended = a < 0;
-  q.grow = q.ended ? 0 : a;
-  return q;
 }
 __device__ __forceinline__ int64_t pages_of(int64_t n, int lp) { return (n + (1 << lp) - 1) >> lp; }
+// i of a ring of n, i < 2 n
+__device__ __forceinline__ int in_ring(int64_t i, int n) { return (int)(i >= n ? i - n : i); }
 
-// start, lengths, ring state and the plan [B] of {length, old pages, ring index of
-// the first new page or place of the first page given back, kServed ..}
-__device__ void tables_plan(const PagedTablesLaunch &p) {
-  __shared__ int64_t waves[TT / 64];
-  __shared__ int64_t taken_s;
-  const int tid = threadIdx.x;
-  const int per = (p.B + TT - 1) / TT, s0 = tid * per, s1 = min(p.B, s0 + per);
-  int first = p.free_state[0], count = p.free_state[1];
-  if (tid == 0) taken_s = 0;
+template <int PER>  // sequences of a thread
+__global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
+  __shared__ TablesPlan plan;
+  __shared__ int64_t sums_s[2][TT / 64][2];
+  __shared__ int taken_s, last_s;
+  const int tid = threadIdx.x, P = 1 << p.lp;
+  const int s0 = tid * PER, n_mine = max(0, min(PER, p.B - s0));
+  int len[PER], grow[PER], old[PER];
+  bool ended[PER];
   bool bad = false;
+  int first = p.free_state[0], count = p.free_state[1];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int n = i < n_mine ? p.len[s0 + i] : 0, a = i < n_mine ? p.add[s0 + i] : 0;
+    len[i] = (int)max((int64_t)0, min((int64_t)n, (int64_t)p.max_pages << p.lp));
+    bad |= n != len[i];
+    ended[i] = a < 0;
+    grow[i] = max(a, 0);
+    old[i] = (int)pages_of(len[i], p.lp);
+  }
   if (first < 0 || first >= p.n_pages || count < 0 || count > p.n_pages) {
     bad = true;
     first = max(0, min(first, p.n_pages - 1));
     count = max(0, min(count, p.n_pages));
   }
-  int64_t rows = 0, back = 0;
-  for (int s = s0; s < s1; ++s) {
-    const TSeq q = tables_seq(p, s);
-    rows += q.grow;
-    back += q.ended ? q.old : 0;
-    bad |= q.bad;
+  if (tid == 0) taken_s = 0;
+  for (int i = tid; i < PPD_PAGED_SEQS_MAX / 32; i += TT) plan.ended[i] = 0;
+  int64_t v[2] = {0, 0}, all[2];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[0] += grow[i], v[1] += ended[i] ? old[i] : 0;
+  const int64_t rows = v[0], back = v[1];
+  block_scan<2>(v, all, sums_s[0]);
+  int64_t start = v[0] - rows, given = v[1] - back;
+  const int64_t all_back = all[1];
+  // new pages of those that fit
+  int need[PER];
+  bool fits[PER];
+  int64_t at = start, mine[1] = {0}, all_need[1];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int64_t now = pages_of((int64_t)len[i] + grow[i], p.lp);
+    fits[i] = !ended[i] && now <= p.max_pages && at + grow[i] <= p.n_slots;
+    need[i] = fits[i] ? (int)(now - old[i]) : 0;
+    mine[0] += need[i];
+    at += grow[i];
   }
-  int64_t all_rows, all_back, all_need;
-  int64_t start = block_scan(rows, waves, &all_rows) - rows;
-  int64_t given = block_scan(back, waves, &all_back) - back;
-  const int64_t start0 = start;
-  auto fits = [&](const TSeq &q, int64_t from, int64_t *need) {
-    const int64_t now = pages_of((int64_t)q.len + q.grow, p.lp);
-    const bool ok = now <= p.max_pages && from + q.grow <= p.n_slots;
-    *need = ok ? now - q.old : 0;
-    return ok;
-  };
-  int64_t need = 0;
-  for (int s = s0; s < s1; ++s) {
-    const TSeq q = tables_seq(p, s);
-    int64_t n;
-    fits(q, start, &n);
-    need += n;
-    start += q.grow;
-  }
-  int64_t asked = block_scan(need, waves, &all_need) - need;
-  start = start0;
+  const int64_t wanted = mine[0];
+  block_scan<1>(mine, all_need, (int64_t(*)[1])sums_s[1]);
+  int64_t asked = mine[0] - wanted;
   bool refused = false;
-  for (int s = s0; s < s1; ++s) {
-    const TSeq q = tables_seq(p, s);
-    int64_t n;
-    bool ok = fits(q, start, &n);
-    asked += n;
-    ok = ok && (n == 0 || asked <= count);
-    const int64_t at = q.ended ? first + (int64_t)count + given : first + asked - n;
-    p.plan[s] = int4{q.len, q.old, (int)(at % p.n_pages), q.ended ? kEnded : ok ? kServed : kRefused};
-    p.start[s] = (int)min(start, (int64_t)INT32_MAX);
-    p.len_out[s] = q.ended ? 0 : q.len + (ok ? q.grow : 0);
-    // the last sequence served a page has the largest sum that the ring suffices for
-    if (ok && n) atomicMax((unsigned long long *)&taken_s, (unsigned long long)asked);
-    refused |= !ok;
-    given += q.ended ? q.old : 0;
-    start += q.grow;
-  }
-  if (s0 < p.B && s1 == p.B) p.start[p.B] = (int)min(start, (int64_t)INT32_MAX);
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (i < n_mine) {
+      asked += need[i];
+      const bool ok = ended[i] || (fits[i] && (need[i] == 0 || asked <= count));
+      plan.start[s0 + i] = (int)min(start, (int64_t)INT32_MAX);
+      plan.len[s0 + i] = len[i];
+      // (asked - need < count <= n_pages, given <= n_pages: below 3 rings)
+      const int64_t a = ended[i] ? (int64_t)in_ring((int64_t)first + count, p.n_pages) + given : (int64_t)first + asked - need[i];
+      plan.at[s0 + i] = ok ? (int)(a % p.n_pages) : ~0;
+      if (ended[i]) atomicOr(&plan.ended[(s0 + i) >> 5], 1u << ((s0 + i) & 31));
+      // the last sequence served a page has the largest sum that the ring suffices for
+      if (ok && need[i]) atomicMax(&taken_s, (int)asked);
+      refused |= !ok;
+      given += ended[i] ? old[i] : 0;
+      start += grow[i];
+      if (!ok) grow[i] = 0;  // (it keeps its length)
+    }
+  if (n_mine && s0 + n_mine == p.B) plan.start[p.B] = (int)min(start, (int64_t)INT32_MAX);
   __syncthreads();
-  if (tid == 0) {
-    const int64_t taken = taken_s;
-    p.free_state_out[0] = (int)((first + taken) % p.n_pages);
-    p.free_state_out[1] = (int)min(count - taken + all_back, (int64_t)p.n_pages);
-  }
-  if (refused) atomicOr(p.status, PPD_DEV_NO_PAGES);
-  if (bad || (tid == 0 && count + all_back > p.n_pages)) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
-}
-
-// slots of rows [i0, n) by steps of `step`, and the new pages' table entries;
-// pages given back, a wave a sequence
-__device__ void tables_fill(const PagedTablesLaunch &p, const int *start, int i0, int step, int w0, int w_step) {
-  const int n = min(start[p.B], p.n_slots), P = 1 << p.lp;
-  for (int i = i0; i < n; i += step) {
-    int lo = 0, hi = p.B - 1;  // the last sequence that starts at or before i
+  const int taken = taken_s;
+  if (tid == 0)
+    last_s = gridDim.x == 1 || __hip_atomic_fetch_add(p.ctr, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  // ---- slots, four rows a thread
+  const int n = min(plan.start[p.B], p.n_slots);
+  const bool wide = ((uintptr_t)p.slots & 15) == 0;
+  for (int64_t i0 = 4 * ((int64_t)blockIdx.x * TT + tid); i0 < n; i0 += 4 * (int64_t)gridDim.x * TT) {
+    int lo = 0, hi = p.B - 1;  // the last sequence that starts at or before i0
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (start[mid] <= i)
+      if (plan.start[mid] <= i0)
         lo = mid;
       else
         hi = mid - 1;
     }
-    const int4 q = p.plan[lo];
-    if (q.w != kServed) {
-      p.slots[i] = -1;
-      continue;
+    int s = -1, j = -1, page = 0, x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = (int)i0 + e;
+      while (lo < p.B - 1 && plan.start[lo + 1] <= i) ++lo;
+      x[e] = -1;
+      if (i < n && plan.at[lo] >= 0) {
+        const int pos = plan.len[lo] + (i - plan.start[lo]), q = pos >> p.lp;  // below max_pages pages
+        if (lo != s || q != j) {
+          s = lo, j = q;
+          const int before = (int)pages_of(plan.len[lo], p.lp);
+          int32_t *row = p.table + (size_t)lo * p.max_pages;
+          page = q < before ? row[q] : p.free_pages[in_ring((int64_t)plan.at[lo] + (q - before), p.n_pages)];
+          if (q >= before && (pos & (P - 1)) == 0) row[q] = page;
+        }
+        x[e] = page * P + (pos & (P - 1));
+      }
     }
-    const int pos = q.x + (i - start[lo]), j = pos >> p.lp;  // below max_pages pages
-    int32_t *row = p.table + (size_t)lo * p.max_pages;
-    int page;
-    if (j < q.y) {
-      page = row[j];
+    if (wide && i0 + 4 <= n) {
+      *(int4 *)(p.slots + i0) = int4{x[0], x[1], x[2], x[3]};
     } else {
-      page = p.free_pages[((int64_t)q.z + (j - q.y)) % p.n_pages];
-      if ((pos & (P - 1)) == 0) row[j] = page;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (i0 + e < n) p.slots[i0 + e] = x[e];
     }
-    p.slots[i] = page * P + (pos & (P - 1));
   }
-  for (int s = w0; s < p.B; s += w_step) {
-    const int4 q = p.plan[s];
-    if (q.w != kEnded) continue;
-    for (int j = threadIdx.x & 63; j < q.y; j += 64)
-      p.free_pages[((int64_t)q.z + j) % p.n_pages] = p.table[(size_t)s * p.max_pages + j];
+  // ---- pages given back, a wave a sequence
+  if (all_back)
+    for (int s = (blockIdx.x * TT + tid) >> 6; s < p.B; s += gridDim.x * (TT / 64)) {
+      if (!(plan.ended[s >> 5] >> (s & 31) & 1)) continue;
+      const int m = (int)pages_of(plan.len[s], p.lp);
+      for (int j = tid & 63; j < m; j += 64)
+        p.free_pages[in_ring((int64_t)plan.at[s] + j, p.n_pages)] = p.table[(size_t)s * p.max_pages + j];
+    }
+  if (blockIdx.x == 0) {
+    for (int s = tid; s <= p.B; s += TT) p.start[s] = plan.start[s];
+    if (refused) atomicOr(p.status, PPD_DEV_NO_PAGES);
+    if (bad || (tid == 0 && count + all_back > p.n_pages)) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   }
-}
-
-// everything in one workgroup
-__global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
-  __shared__ int start_s[PPD_PAGED_SEQS_MAX + 1];
-  tables_plan(p);
-  __threadfence_block();
   __syncthreads();
-  for (int s = threadIdx.x; s <= p.B; s += TT) start_s[s] = p.start[s];
-  __syncthreads();
-  tables_fill(p, start_s, threadIdx.x, TT, threadIdx.x >> 6, TT / 64);
-}
-
-__global__ __launch_bounds__(TT) void paged_plan_kernel(PagedTablesLaunch p) { tables_plan(p); }
-
-__global__ __launch_bounds__(256) void paged_fill_kernel(PagedTablesLaunch p) {
-  __shared__ int start_s[PPD_PAGED_SEQS_MAX + 1];
-  for (int s = threadIdx.x; s <= p.B; s += 256) start_s[s] = p.start[s];
-  __syncthreads();
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  tables_fill(p, start_s, i, gridDim.x * 256, i >> 6, gridDim.x * 4);
+  if (!last_s) return;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (i < n_mine) p.len_out[s0 + i] = ended[i] ? 0 : len[i] + grow[i];
+  if (tid == 0) {
+    p.free_state_out[0] = in_ring((int64_t)first + taken, p.n_pages);
+    p.free_state_out[1] = (int)min(count - taken + all_back, (int64_t)p.n_pages);
+    __hip_atomic_store(p.ctr, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -470,17 +471,10 @@ __global__ __launch_bounds__(64 * SW) void paged_fill_rows_kernel(PagedStoreLaun
 }  // namespace
 
 hipError_t launch_paged_tables(const PagedTablesLaunch &p, hipStream_t s) {
-  // one workgroup while a thread of it has a few rows; else its sums first, the
-  // rows over the device
-  if (p.n_slots <= 8 * TT) {
-    hipLaunchKernelGGL(paged_tables_kernel, dim3(1), dim3(TT), 0, s, p);
-    return hipGetLastError();
-  }
-  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(TT), 0, s, p);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int grid = (int)std::min<int64_t>(1024, ((int64_t)p.n_slots + 1023) / 1024);
-  hipLaunchKernelGGL(paged_fill_kernel, dim3(grid), dim3(256), 0, s, p);
+  // four rows a thread, a sequence a wave (for pages given back)
+  const int64_t rows = ((int64_t)p.n_slots + 4 * TT - 1) / (4 * TT), seqs = (p.B + TT / 64 - 1) / (TT / 64);
+  const int grid = (int)std::min<int64_t>(256, std::max(rows, seqs));
+  hipLaunchKernelGGL(p.B <= TT ? paged_tables_kernel<1> : paged_tables_kernel<PPD_PAGED_SEQS_MAX / TT>, dim3(grid), dim3(TT), 0, s, p);
   return hipGetLastError();
 }
 

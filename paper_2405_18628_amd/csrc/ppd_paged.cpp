@@ -148,7 +148,7 @@ size_t ppd_paged_tables_workspace_bytes(int32_t n_seqs) {
     ppd_fail(PPD_EINVAL, "n_seqs=%d outside [1, %d]", n_seqs, PPD_PAGED_SEQS_MAX);
     return 0;
   }
-  return kHeader + (size_t)n_seqs * sizeof(int4);
+  return kHeader;  // (the status words and a counter)
 }
 
 ppd_status ppd_paged_tables(const ppd_page_tables *pt, const int32_t *add, int32_t *len_out, int32_t *free_state_out,
@@ -174,7 +174,7 @@ ppd_status ppd_paged_tables(const ppd_page_tables *pt, const int32_t *add, int32
   p.n_pages = pt->n_pages;
   p.lp = log2_of(pt->page);
   p.n_slots = n_slots;
-  p.plan = (int4 *)((char *)ws + kHeader);
+  p.ctr = (uint32_t *)ws + 4;
   p.status = (uint32_t *)ws;
   PPD_TRY_HIP(launch_paged_tables(p, (hipStream_t)stream));
   return PPD_OK;

@@ -76,6 +76,23 @@ __device__ __forceinline__ int64_t wave_total(int64_t v) {
   for (int i = 0; i < 2; ++i) sum += (int64_t)wave_all((uint32_t)(v >> 24 * i) & 0xffffffu, add) << 24 * i;
   return sum;
 }
+__device__ __forceinline__ int64_t wave_incl64(int64_t v) {
+  auto step = [&](auto move) {
+    const uint32_t lo = (uint32_t)move((int)v), hi = (uint32_t)move((int)(v >> 32));
+    v += (int64_t)((uint64_t)hi << 32 | lo);
+  };
+  step([](int x) { return lane_move<0x111>(x); });
+  step([](int x) { return lane_move<0x112>(x); });
+  step([](int x) { return lane_move<0x114>(x); });
+  step([](int x) { return lane_move<0x118>(x); });
+  step([](int x) { return lane_move<0x142, 0xa>(x); });
+  step([](int x) { return lane_move<0x143, 0xc>(x); });
+  return v;
+}
+__device__ __forceinline__ int64_t lane_of64(int64_t v, int lane) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
+                   (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
+}
 __device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
 // The sequence of a row: the last one whose rows start at or before it.  Called
@@ -94,7 +111,7 @@ struct PagedTablesLaunch {
   const int32_t *len, *free_state, *add;
   int32_t *len_out, *free_state_out, *start, *slots;
   int B, max_pages, n_pages, lp, n_slots;
-  int4 *plan;        // [B]: length, pages held, first of the ring's entries, what becomes of it
+  uint32_t *ctr;  // workgroups that have read their inputs; zero between launches
   uint32_t *status;
 };
 hipError_t launch_paged_tables(const PagedTablesLaunch &p, hipStream_t s);

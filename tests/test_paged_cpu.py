@@ -33,7 +33,7 @@ def test_sizes():
     assert 0 < small < big
     for bad in ((0, 1, 1, 1), (4, 3, 1, 1), (4, 4, 0, 1), (4, 4, 4097, 1), (4, 4, 1, 0), (1024, 8, 1, 4097)):
         assert L.ppd_paged_attention_workspace_bytes(*bad) == 0 and ppd.ppd_last_error()
-    assert ppd.ppd_paged_tables_workspace_bytes(1) < ppd.ppd_paged_tables_workspace_bytes(4096)
+    assert 0 < ppd.ppd_paged_tables_workspace_bytes(1) <= ppd.ppd_paged_tables_workspace_bytes(4096)
     for bad in (0, -1, 4097):
         assert L.ppd_paged_tables_workspace_bytes(bad) == 0
     assert ppd.ppd_paged_select_workspace_bytes(8, 4, 100) >= 8 * 4 * 100 * 8
@@ -63,7 +63,7 @@ def test_tables_refuse():
     for kw in (dict(add=None), dict(len_out=None), dict(state=None), dict(start=None), dict(slots=None), dict(n=0),
                dict(n=-1), dict(ws=F + 4)):
         assert call(**kw) == ppd.PPD_EINVAL, kw
-    assert call(ws=None) == call(size=256 + 3 * 16 - 1) == ppd.PPD_EWORKSPACE
+    assert call(ws=None) == call(size=ppd.ppd_paged_tables_workspace_bytes(3) - 1) == ppd.PPD_EWORKSPACE
 
 
 def test_store_refuses():
