@@ -205,16 +205,15 @@ __device__ __forceinline__ float factor_of(float2 ml, float M) {
   return ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - M);
 }
 
-// two floats of a partial row; FAR: to and from where every XCD sees them
-template <bool FAR>
-__device__ __forceinline__ void put_part(float *p, float2 v) {
-  if constexpr (FAR)
-    __hip_atomic_store((uint64_t *)p, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  else
-    *(float2 *)p = v;
+// Partial rows that another workgroup adds are written and read past this XCD's
+// caches (sc1, the cache policy of agent scope), so no cache has to be written
+// back or dropped for them.
+constexpr int kFar = 16;
+__device__ __forceinline__ void put_far(__amdgpu_buffer_rsrc_t r, size_t at, floatx4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, (int)(at * sizeof(float)), 0, kFar);
 }
-__device__ __forceinline__ float2 get_part(const float *p) {
-  return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+__device__ __forceinline__ floatx4 get_far(__amdgpu_buffer_rsrc_t r, size_t at) {
+  return __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(at * sizeof(float)), 0, kFar));
 }
 
 // ONCE: no other wave of the call reads it
@@ -518,7 +517,8 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   }
   __syncthreads();
   const int n_rows = min(R - row0, RW);
-  float *part = p.part + (size_t)my_part * RW * OROW;  // (only with several splits)
+  const size_t part0_at = (size_t)my_part * RW * OROW;  // (only with several splits)
+  const __amdgpu_buffer_rsrc_t far = rsrc_of(p.part, JOIN ? 2 * SLOTS * RW * OROW * (uint32_t)sizeof(float) : 0);
   if (tid < n_rows) {
     float2 ml[PARS];
     float M = -INFINITY, l = 0.f;
@@ -537,7 +537,10 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
 #pragma unroll
     for (int w = 0; w < PARS; ++w) fac_s[tid][w] = f[w] * inv;
     if (KS > 1) {
-      put_part<JOIN>(part + (size_t)tid * OROW + 128, float2{M, l});
+      if constexpr (JOIN)
+        put_far(far, part0_at + (size_t)tid * OROW + 128, floatx4{M, l, 0.f, 0.f});
+      else
+        *(float2 *)(p.part + part0_at + (size_t)tid * OROW + 128) = float2{M, l};
     } else if (p.lse) {
       const int r = row0 + tid;
       p.lse[(size_t)(t0 + r / G) * p.nh + kvh * G + r % G] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
@@ -551,8 +554,10 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
 #pragma unroll
     for (int w = 0; w < PARS; ++w) o += fac_s[rl][w] * *(const floatx4 *)(rows_s[w][rl] + d4);
     if (KS > 1) {
-      put_part<JOIN>(part + (size_t)rl * OROW + d4, float2{o[0], o[1]});
-      put_part<JOIN>(part + (size_t)rl * OROW + d4 + 2, float2{o[2], o[3]});
+      if constexpr (JOIN)
+        put_far(far, part0_at + (size_t)rl * OROW + d4, o);
+      else
+        *(floatx4 *)(p.part + part0_at + (size_t)rl * OROW + d4) = o;
     } else {
       const int r = row0 + rl;
       store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, o);
@@ -560,9 +565,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   }
   if constexpr (JOIN) {
     if (KS == 1) return;
-    // ---- the last of the splits to arrive adds them all, in order.  Their rows
-    // are written and read past the XCDs' caches, so no cache is written back
-    // or dropped for them.
+    // ---- the last of the splits to arrive adds them all, in a fixed order
     __shared__ int last_s;
     __builtin_amdgcn_s_waitcnt(0);  // this thread's rows are in memory
     __syncthreads();
@@ -575,74 +578,83 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
     }
     __syncthreads();
     if (!last_s) return;
-    part = p.part + (size_t)(my_part - ks) * RW * OROW;
+    const size_t first_at = (size_t)(my_part - ks) * RW * OROW;
     constexpr size_t stride = (size_t)RW * OROW;
-    // a split's factor for a row, in LDS
+    // 32 threads a row; of few rows several such groups share one (ways), of more
+    // than eight a group takes two.  A round of splits is requested for both, and
+    // beside the first the splits' maxima and sums, of which LDS gets the factors
+    constexpr int GR = NT / 32, N = 8;
+    static_assert(2 * GR >= RW, "two rows a group");
+    const int ways = n_rows >= 5 ? 1 : n_rows >= 3 ? GR / 4 : n_rows == 2 ? GR / 2 : GR;
+    const int group = tid >> 5, sub = group % ways, rl = group / ways;
+    const bool two = ways == 1 && rl + GR < n_rows;
+    floatx4 x[N], y[N];
+    auto request = [&](int s0) {
+#pragma unroll
+      for (int v = 0; v < N; ++v)
+        x[v] = get_far(far, first_at + min(s0 + v * ways, KS - 1) * stride + (size_t)min(rl, n_rows - 1) * OROW + d4);
+      if (two)
+#pragma unroll
+        for (int v = 0; v < N; ++v) y[v] = get_far(far, first_at + min(s0 + v, KS - 1) * stride + (size_t)(rl + GR) * OROW + d4);
+    };
     float(*wt_s)[kPagedSplits] = (float(*)[kPagedSplits])rows_s;
+    floatx4 *sum_s = (floatx4 *)((char *)rows_s + sizeof(float) * RW * kPagedSplits);  // [GR][32]
     constexpr int TR = NT / RW;  // threads a row
-    static_assert(TR <= 64 && kPagedSplits % TR == 0 && sizeof(float) * RW * kPagedSplits <= sizeof(rows_s), "weights fit");
+    static_assert(TR <= 64 && kPagedSplits % TR == 0 && sizeof(float) * RW * kPagedSplits + GR * 512 <= sizeof(rows_s), "they fit");
     {
-      const int rl = tid / TR, j0 = tid % TR;
-      float2 ml[kPagedSplits / TR];
+      const int row = tid / TR, j0 = tid % TR;
+      floatx4 ml[kPagedSplits / TR];
       float M = -INFINITY, l = 0.f;
-      if (rl < n_rows) {
 #pragma unroll
-        for (int j = 0; j < kPagedSplits / TR; ++j)
-          ml[j] = j0 + TR * j < KS ? get_part(part + (j0 + TR * j) * stride + (size_t)rl * OROW + 128) : float2{-INFINITY, 0.f};
+      for (int j = 0; j < kPagedSplits / TR; ++j)
+        ml[j] = row < n_rows && j0 + TR * j < KS ? get_far(far, first_at + (j0 + TR * j) * stride + (size_t)row * OROW + 128)
+                                                : floatx4{-INFINITY, 0.f, 0.f, 0.f};
+      request(sub);
 #pragma unroll
-        for (int j = 0; j < kPagedSplits / TR; ++j) M = fmaxf(M, ml[j].x);
+      for (int j = 0; j < kPagedSplits / TR; ++j) M = fmaxf(M, ml[j][0]);
 #pragma unroll
-        for (int o = TR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+      for (int o = TR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
 #pragma unroll
-        for (int j = 0; j < kPagedSplits / TR; ++j) {
-          const float f = factor_of(ml[j], M);
-          l += f * ml[j].y;
-          if (j0 + TR * j < KS) wt_s[rl][j0 + TR * j] = f;
-        }
+      for (int j = 0; j < kPagedSplits / TR; ++j) {
+        const float f = factor_of(float2{ml[j][0], ml[j][1]}, M);
+        l += f * ml[j][1];
+        if (j0 + TR * j < KS) wt_s[row][j0 + TR * j] = f;
+      }
 #pragma unroll
-        for (int o = TR / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-        if (j0 == 0) {
-          fac_s[rl][0] = l == 0.f ? 0.f : 1.f / l;
-          const int r = row0 + rl;
-          if (p.lse) p.lse[(size_t)(t0 + r / G) * p.nh + kvh * G + r % G] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
-        }
+      for (int o = TR / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+      if (j0 == 0 && row < n_rows) {
+        fac_s[row][0] = l == 0.f ? 0.f : 1.f / l;
+        const int r = row0 + row;
+        if (p.lse) p.lse[(size_t)(t0 + r / G) * p.nh + kvh * G + r % G] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
       }
     }
     __syncthreads();
-    // rows' sums: 32 threads a row; of few rows several such groups share one
-    constexpr int GR = NT / 32;
-    const int ways = n_rows >= 5 ? 1 : n_rows >= 3 ? GR / 4 : n_rows == 2 ? GR / 2 : GR;
-    floatx4 *sum_s = (floatx4 *)((char *)rows_s + sizeof(float) * RW * kPagedSplits);  // [GR][32]
-    static_assert(sizeof(float) * RW * kPagedSplits + GR * 512 <= sizeof(rows_s), "sums fit");
-    const int grp32 = tid >> 5, sub = grp32 % ways;
-    for (int rl = grp32 / ways; rl < n_rows; rl += GR / ways) {
-      constexpr int N = 16;  // splits in flight
-      floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
-      for (int s0 = sub; s0 < KS; s0 += N * ways) {
-        float2 x[N][2];
+    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f}, o2 = o;
+    const int row = min(rl, n_rows - 1);
+    for (int s0 = sub; s0 < KS; s0 += N * ways) {
+      if (s0 != sub) request(s0);
 #pragma unroll
-        for (int v = 0; v < N; ++v) {
-          const float *row = part + min(s0 + v * ways, KS - 1) * stride + (size_t)rl * OROW + d4;
-          x[v][0] = get_part(row);
-          x[v][1] = get_part(row + 2);
-        }
+      for (int v = 0; v < N; ++v)
+        if (s0 + v * ways < KS) o += wt_s[row][s0 + v * ways] * x[v];
+      if (two)
 #pragma unroll
         for (int v = 0; v < N; ++v)
-          if (s0 + v * ways < KS) o += wt_s[rl][s0 + v * ways] * floatx4{x[v][0].x, x[v][0].y, x[v][1].x, x[v][1].y};
-      }
-      if (ways > 1) sum_s[grp32 * 32 + (tid & 31)] = o;
-      if (ways == 1) {
-        const int r = row0 + rl;
-        store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, o * fac_s[rl][0]);
-      }
+          if (s0 + v < KS) o2 += wt_s[rl + GR][s0 + v] * y[v];
     }
-    if (ways == 1) return;
+    auto store = [&](int row, floatx4 v) {
+      const int r = row0 + row;
+      store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, v * fac_s[row][0]);
+    };
+    if (ways == 1) {
+      if (rl < n_rows) store(rl, o);
+      if (two) store(rl + GR, o2);
+      return;
+    }
+    sum_s[group * 32 + (tid & 31)] = o;
     __syncthreads();
-    if (sub == 0 && grp32 / ways < n_rows) {
-      const int rl = grp32 / ways, r = row0 + rl;
-      floatx4 o = sum_s[grp32 * 32 + (tid & 31)];
-      for (int w = 1; w < ways; ++w) o += sum_s[(grp32 + w) * 32 + (tid & 31)];
-      store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, o * fac_s[rl][0]);
+    if (sub == 0 && rl < n_rows) {
+      for (int w = 1; w < ways; ++w) o += sum_s[(group + w) * 32 + (tid & 31)];
+      store(rl, o);
     }
   }
 }
