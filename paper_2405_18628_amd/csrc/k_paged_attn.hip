@@ -96,13 +96,14 @@ __device__ __forceinline__ Load load_of(const PagedAttnLaunch &p, int s, const P
   w.units = w.grps * p.nkv;
   return w;
 }
-// Blocks of a workgroup at most: all of them over the call's slots, LEAST at least.
-// With c of them, a row group of n blocks is cut into ceil(n / c) splits: at most
-// units + SLOTS workgroups in all, at most 2 SLOTS of them of groups that have
-// several, of which there are less than SLOTS (each holds more than c blocks).
-template <int SLOTS, int LEAST>
-__device__ __forceinline__ int blocks_each(int64_t total) {
-  return (int)max((total + SLOTS - 1) / SLOTS, (int64_t)LEAST);
+// Blocks of a workgroup at most, LEAST at least.  With c of them a row group of n
+// blocks is cut into ceil(n / c) splits.  Where c is not below total / (S slots),
+// there are at most units + S workgroups, at most 2 S of them in groups of several
+// splits and less than S such groups (each holds more than c blocks); S is
+// 1.5 kPagedSlots at most below.
+template <int LEAST>
+__device__ __forceinline__ int blocks_each(int64_t total, int slots) {
+  return (int)max((total + slots - 1) / slots, (int64_t)LEAST);
 }
 __device__ __forceinline__ int splits_of(const Load &w, int c) {
   c = max(c, (w.nblk + kPagedSplits - 1) / kPagedSplits);
@@ -116,13 +117,15 @@ struct Place {
 };
 // the workgroup's sequence and place in it; false: it has no part.  A wave's lanes
 // take a sequence each.
-template <int RW, int SLOTS, int LEAST>
+template <int RW, int LEAST>
 __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, Place *out, bool *bad) {
   if (p.sq.B == 1) {  // alike in all lanes
     out->sq = out->part0 = 0;
     out->q = paged_seq(p.sq, 0, bad);
     out->w = load_of(p, 0, out->q, RW, bad);
-    out->KS = splits_of(out->w, blocks_each<SLOTS, LEAST>((int64_t)out->w.units * out->w.nblk));
+    // (as many for each row group: no compute unit gets one workgroup more than the others)
+    const int even = max(1, kPagedSlots / max(1, out->w.units));
+    out->KS = splits_of(out->w, max((out->w.nblk + even - 1) / even, LEAST));
     out->local = slot;
     return slot < out->w.units * out->KS;
   }
@@ -139,8 +142,18 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, P
     }
   }
   total = wave_total(total);
-  // (of many groups, each is rounded up: over three quarters of the slots, most fit at once)
-  const int c = blocks_each<SLOTS * 3 / 4, LEAST>(total);
+  const int units = (int)wave_total(p.sq.B <= 64 ? w.units : 0);  // (more sequences: more groups than slots anyway)
+  int c;
+  if (units == 0 || units > kPagedSlots) {  // several rounds of workgroups: only long groups are cut
+    c = blocks_each<2 * LEAST>(total, kPagedSlots * 3 / 2);
+  } else {  // one round: each is rounded up, so fewer until they fit
+    c = blocks_each<LEAST>(total, kPagedSlots);
+    for (int i = 0; i < 4; ++i) {
+      const int n = (int)wave_total((int64_t)w.units * splits_of(w, c));
+      if (n <= kPagedSlots) break;
+      c = (int)(((int64_t)c * n + kPagedSlots - 1) / kPagedSlots);
+    }
+  }
   int slots0 = 0, parts0 = 0;
   for (int base = 0; base < p.sq.B; base += 64) {
     const int s = base + lane;
@@ -234,7 +247,6 @@ template <int NQ, int QW, int PARS, int QT>
 __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(PagedAttnLaunch p) {
   constexpr int NT = 64 * QW * PARS;
   constexpr bool JOIN = NQ * QW == 1;  // the last of a row group's splits adds them
-  constexpr int SLOTS = paged_slots(NQ * QW);
   constexpr int RW = QW * NQ * 16;  // rows of the workgroup
   constexpr int QP = q_parts(QT), PP = p_parts(QT);
   constexpr bool QLDS = NQ > 1 || QP > 2;  // no registers left for the queries
@@ -250,7 +262,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   const int lr = lane & 15, lg = lane >> 4;
   Place pl;
   bool bad = false;
-  const bool mine = find_place<RW, SLOTS, kLeast * PARS>(p, blockIdx.x, &pl, &bad);
+  const bool mine = find_place<RW, kLeast * PARS>(p, blockIdx.x, &pl, &bad);
   if (bad && blockIdx.x == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   if (!mine) return;
   const int sq = __builtin_amdgcn_readfirstlane(pl.sq), KS = __builtin_amdgcn_readfirstlane(pl.KS);
@@ -518,7 +530,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   __syncthreads();
   const int n_rows = min(R - row0, RW);
   const size_t part0_at = (size_t)my_part * RW * OROW;  // (only with several splits)
-  const __amdgpu_buffer_rsrc_t far = rsrc_of(p.part, JOIN ? 2 * SLOTS * RW * OROW * (uint32_t)sizeof(float) : 0);
+  const __amdgpu_buffer_rsrc_t far = rsrc_of(p.part, JOIN ? 3 * kPagedSlots * RW * OROW * (uint32_t)sizeof(float) : 0);
   if (tid < n_rows) {
     float2 ml[PARS];
     float M = -INFINITY, l = 0.f;
@@ -735,7 +747,7 @@ static int paged_tiles(int nh, int nkv, int B, int n_rows) {
 
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows) {
   const Shape sh = paged_shape(paged_tiles(nh, nkv, B, n_rows));
-  return 2 * (size_t)paged_slots(sh.nq * sh.qw) * sh.rows() * OROW * sizeof(float);
+  return 3 * (size_t)kPagedSlots * sh.rows() * OROW * sizeof(float);
 }
 
 void paged_attn_shape(PagedAttnLaunch &a) {
@@ -755,7 +767,7 @@ static hipError_t launch_attn(const PagedAttnLaunch &a, hipStream_t s) {
   // row groups of all sequences at most, and the splits of those that have several
   const int64_t rows = (int64_t)a.sq.n_rows * (a.nh / a.nkv);
   const int64_t units = a.nkv * (std::min<int64_t>(a.sq.B, a.sq.n_rows) + rows / rw);
-  const dim3 grid((unsigned)(units + (a.may_split ? paged_slots(sh.nq * sh.qw) : 0))), block(64 * sh.qw * sh.pars);
+  const dim3 grid((unsigned)(units + (a.may_split ? 3 * kPagedSlots / 2 : 0))), block(64 * sh.qw * sh.pars);
   const bool merge = a.may_split && sh.nq * sh.qw > 1;
   const hipEvent_t ev0 = (hipEvent_t)a.ev_start, ev1 = (hipEvent_t)a.ev_stop;
   if (ev0)

@@ -143,7 +143,7 @@ struct PagedAttnLaunch {
   const int32_t *sel, *n_sel;  // [B][nkv][budget], [B], or null
   int budget;
   int nh, nkv;
-  float *part;                 // [2 paged_slots][rows of a workgroup][PPD_ATTN_OROW]
+  float *part;                 // [3 kPagedSlots][rows of a workgroup][PPD_ATTN_OROW]
   int2 *rec;                   // [B]: splits, first of the partial rows' workgroups
   uint32_t *ctr;               // arrivals of row groups' splits, a byte each: zero between launches
   uint32_t *status;
@@ -152,11 +152,10 @@ struct PagedAttnLaunch {
   int may_split;               // a sequence can be long enough for more than one workgroup
   void *ev_start, *ev_stop;
 };
-// Workgroups that a call's keys are divided among, by the tiles of one: as many as
-// are on the device together
-constexpr int paged_slots(int tiles) { return tiles == 1 ? 512 : 256; }
+// Workgroups that a call's keys are divided among: one a compute unit
+constexpr int kPagedSlots = 256;
 constexpr int kPagedSplits = 128;  // most splits of a row group (a byte counts them)
-constexpr size_t kPagedCounters = 512;  // bytes of them: paged_slots(1) row groups at most have several
+constexpr size_t kPagedCounters = 512;  // bytes of them: below 1.5 kPagedSlots row groups have several
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows);
 void paged_attn_shape(PagedAttnLaunch &a);  // fills tiles, may_split
 hipError_t launch_paged_attn(const PagedAttnLaunch &a, hipStream_t s);
