@@ -271,13 +271,13 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   const int n4 = __builtin_amdgcn_readfirstlane(pl.w.n4), nblk = __builtin_amdgcn_readfirstlane(pl.w.nblk);
   const int n_grp = __builtin_amdgcn_readfirstlane(pl.w.grps);
   const int part0 = __builtin_amdgcn_readfirstlane(pl.part0);
-  int local = __builtin_amdgcn_readfirstlane(pl.local);
+  const int local = __builtin_amdgcn_readfirstlane(pl.local);
   if (!JOIN && local == 0 && tid == 0) p.rec[sq] = int2{KS, part0};
-  const int my_part = part0 + local;  // the workgroup's place among those that leave partial rows
   const int G = p.nh / p.nkv, R = T * G;
-  const int ks = local % KS;
-  local /= KS;
-  const int grp = local % n_grp, kvh = local / n_grp;
+  // row groups that read the same keys are nkv KS workgroups apart: mostly on one
+  // XCD, whose cache then holds them
+  const int ranges = p.nkv * KS, grp = local / ranges, kvh = local % ranges / KS, ks = local % KS;
+  const int my_part = part0 + (kvh * n_grp + grp) * KS + ks;  // its place among those that leave partial rows
   const int chunk = (nblk + KS - 1) / KS;  // (the last splits may be left without blocks)
   const int b0 = min(nblk, ks * chunk), b1 = min(nblk, b0 + chunk);
   const int row0 = grp * RW;
@@ -288,17 +288,19 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   const unsigned char *pages = p.pages + (size_t)kvh * ((size_t)kPBytes << lb);
   const size_t page_bytes = (size_t)p.nkv * ((size_t)kPBytes << lb);
 
-  // a block of the prefix: its page's place in the table, then its address.  Past
-  // the wave's blocks the first one again (the same loads on every path)
-  const int end4 = min(b1, n4);
+  // the workgroup's blocks: n_pre of the prefix, from b0 on, then n_new of new rows
+  const int n_pre = max(0, min(b1, n4) - b0), n_new = b1 - b0 - n_pre, first_new = max(0, b0 - n4);
+  auto block_at = [&](int j) {  // past the last: the first again (the same loads on every path)
+    return min(b0, max(0, n4 - 1)) + (j < n_pre ? j : 0);
+  };
+  // a block's page by its place in the table, then the block's address
   auto place_of = [&](int blk) {
-    const int i = (blk < end4 ? blk : min(b0, max(0, n4 - 1))) >> lb;
+    const int i = blk >> lb;
     return sel ? max(0, min(uniform_load(sel, i), last_page)) : i;
   };
   auto address_of = [&](int blk, int place) {
-    const int b = blk < end4 ? blk : min(b0, max(0, n4 - 1));
     const int page = paged_clamp(uniform_load(table, place), n_pages);
-    return pages + (size_t)page * page_bytes + (size_t)(b & ((1 << lb) - 1)) * kPBytes;
+    return pages + (size_t)page * page_bytes + (size_t)(blk & ((1 << lb) - 1)) * kPBytes;
   };
   u32x4 kf[2][4], vf[8];
   auto load_keys = [&](const unsigned char *src) {
@@ -311,13 +313,12 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) vf[dt] = load_page<QW == 1>(src + 2 * kPElems + dt * 1024 + lane * 16);
   };
-  int blk = b0 + par;
-  int place = 0, next_place = 0;
-  const unsigned char *addr = pages, *next_addr = pages;
+  int j = par;  // of the workgroup's blocks
+  int blk = block_at(j), next = block_at(j + PARS), place = 0, next_place = 0;
   if (n4 > 0) {
     place = place_of(blk);
-    next_place = place_of(blk + PARS);
-    addr = address_of(blk, place);
+    next_place = place_of(next);
+    const unsigned char *addr = address_of(blk, place);
     load_keys(addr);
     load_values(addr);
   }
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
       return as_bf16x8(q_s[(((qw + QW * i) * 4 + ds) * QP + part) * 64 + lane]);
   };
   const float c = p.scale_log2;
-  // S^T of the keys in kf, smallest parts first
+  // S^T of a block's keys, smallest parts first
   auto scores = [&](float (&sv)[NQ][8]) {
     floatx4 acc[NQ][2];
 #pragma unroll
@@ -391,7 +392,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
 #pragma unroll
       for (int u = 0; u < 8; ++u) sv[i][u] = acc[i][u >> 2][u & 3];
   };
-  // O^T += V^T P^T of the values in vf
+  // O^T += V^T P^T of its values
   auto products = [&](const u32x4 (&pf)[NQ][PP]) {
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt)
@@ -403,14 +404,14 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   };
 
   if (n_live > 0) {
-    for (; blk < end4; blk += PARS) {
-      // the block after next's place, the next one's address
-      next_addr = address_of(blk + PARS, next_place);
-      const int after = place_of(blk + 2 * PARS);
+    for (; j < n_pre; j += PARS) {
+      // the next block's address, the place of the one after it
+      const unsigned char *addr = address_of(next, next_place);
+      const int after = block_at(j + 2 * PARS), after_place = place_of(after);
       float sv[NQ][8];
       scores(sv);
       __builtin_amdgcn_sched_barrier(0);
-      load_keys(next_addr);
+      load_keys(addr);
       __builtin_amdgcn_sched_barrier(0);
       const int pos = (place << p.sq.lp) + (blk & ((1 << lb) - 1)) * kPB;
       const int vis = L - pos - 8 * lg;  // the lane's keys below the length
@@ -434,15 +435,17 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
       __builtin_amdgcn_sched_barrier(0);
       products(pf);
       __builtin_amdgcn_sched_barrier(0);
-      load_values(next_addr);
+      load_values(addr);
       __builtin_amdgcn_sched_barrier(0);
+      blk = next;
+      next = after;
       place = next_place;
-      next_place = after;
+      next_place = after_place;
     }
     // the new rows, straight from the tail
     const bf16_t *tk = p.tk + (size_t)kvh * p.tcap * 128, *tv = p.tv + (size_t)kvh * 128 * p.tcap;
-    for (; blk < b1; blk += PARS) {
-      const int k0 = (blk - n4) * kPB;
+    for (; j < n_pre + n_new; j += PARS) {
+      const int k0 = (first_new + j - n_pre) * kPB;
       const int j0 = k0 + 8 * lg, keep_n = max(0, min(8, T - j0));  // keys of the lane that exist
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -463,6 +466,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
 #pragma unroll
           for (int w = 0; w < 4; ++w)
             vf[dt][w] = row[min(c0 + 2 * w, p.tcap - 1)] | (uint32_t)row[min(c0 + 2 * w + 1, p.tcap - 1)] << 16;
+          if (dt & 1) __builtin_amdgcn_sched_barrier(0);  // (registers: 16 elements at a time)
         }
       }
       float sv[NQ][8];
@@ -736,14 +740,18 @@ struct Shape {
   int rows() const { return 16 * nq * qw; }
 };
 static Shape paged_shape(int tiles) {
-  return tiles <= 1 ? Shape{1, 1, 4} : tiles <= 2 ? Shape{2, 1, 8} : tiles <= 4 ? Shape{2, 2, 4} : Shape{2, 4, 2};
+  return tiles <= 1 ? Shape{1, 1, 4} : tiles <= 2 ? Shape{2, 1, 4} : tiles <= 4 ? Shape{2, 2, 4} : Shape{2, 4, 2};
 }
-// (a rule on the rows of an average sequence: how many a single one has is only
-// known on the device, and any shape serves any number)
+// 16-row tiles of a kv head's rows (of an average sequence: how many a single one
+// has is only known on the device, and any shape serves any number)
 static int paged_tiles(int nh, int nkv, int B, int n_rows) {
   const int64_t rows = std::min<int64_t>((n_rows + B - 1) / B, PPD_T_MAX) * (nh / nkv);
   return (int)std::min<int64_t>(64, (rows + 15) / 16);
 }
+// Blocks that a workgroup reads where each takes a tile of its own, at most: while
+// they are few the tiles of a kv head read its keys from the XCD's cache beside
+// one another, which is less than what several tiles in a workgroup cost.
+constexpr int64_t kOwnTileBlocks = 64;
 
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows) {
   const Shape sh = paged_shape(paged_tiles(nh, nkv, B, n_rows));
@@ -753,13 +761,15 @@ size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows) {
 void paged_attn_shape(PagedAttnLaunch &a) {
   a.tiles = paged_tiles(a.nh, a.nkv, a.sq.B, a.sq.n_rows);
   const int most = a.sel ? std::min(a.budget, a.sq.max_pages) : a.sq.max_pages;
+  const int64_t blocks = ((int64_t)most << (a.sq.lp - 5)) + 1;
+  if (blocks * a.nkv * std::min(a.sq.B, a.sq.n_rows) * a.tiles <= kOwnTileBlocks * kPagedSlots) a.tiles = 1;
   a.may_split = ((int64_t)most << (a.sq.lp - 5)) + PPD_T_MAX / kPB > kLeast * paged_shape(a.tiles).pars;
 }
 
 template <int QT>
 static hipError_t launch_attn(const PagedAttnLaunch &a, hipStream_t s) {
   auto kernel = a.tiles <= 1   ? paged_attention_kernel<1, 1, 4, QT>
-                : a.tiles <= 2 ? paged_attention_kernel<2, 1, 8, QT>
+                : a.tiles <= 2 ? paged_attention_kernel<2, 1, 4, QT>
                 : a.tiles <= 4 ? paged_attention_kernel<2, 2, 4, QT>
                                : paged_attention_kernel<2, 4, 2, QT>;
   const Shape sh = paged_shape(a.tiles);

@@ -201,9 +201,11 @@ class Pool:
                         self.bounds[l, p, h, 0], self.bounds[l, p, h, 1] = x.amin(0).to(BF), x.amax(0).to(BF)
         self.lens = np.asarray(lens, np.int32)
 
-    def on_gpu(self, tk, tv):
+    def on_gpu(self, tk, tv, width=0):
+        """width: columns of the tables at least (by it a call chooses its kernel)."""
         t = torch.zeros(self.n_pages, dtype=I32, device="cuda")
-        pt = ppd.PageTables(dev(self.table), dev(self.lens), t, t[:2].clone(), self.page)
+        table = np.pad(self.table, ((0, 0), (0, max(0, width - self.table.shape[1]))), constant_values=-7)
+        pt = ppd.PageTables(dev(table), dev(self.lens), t, t[:2].clone(), self.page)
         return ppd.PagedCache(self.pages.cuda(), self.bounds.cuda(), ppd.KVCache(tk.cuda(), tv.cuda())), pt
 
 
@@ -241,15 +243,17 @@ CASES = [  # lens, T, heads, kv heads, page, rows behind the last sequence
     ([3000], [5], 3, 1, 64, 0), ([77], [100], 16, 2, 32, 0), ([10] * 70, [1] * 70, 2, 1, 32, 0)]
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [BF, torch.float32])
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_attention(case, dtype):
+def test_attention(case, dtype, wide):
+    """wide: tables of 2^19 positions, with which several tiles share a workgroup."""
     lens, T, nh, nkv, page, extra = CASES[case]
     r = np.random.default_rng(case)
     pool = Pool(lens, nkv, page, layers=2, seed=case)
     rows = sum(T) + extra
     tk, tv = new_rows(nkv, (rows + 15) // 8 * 8, sum(T), layers=2)
-    kv, pt = pool.on_gpu(tk, tv)
+    kv, pt = pool.on_gpu(tk, tv, (1 << 19) // page if wide else 0)
     g = torch.Generator().manual_seed(case)
     q = torch.randn((rows, nh, 128), generator=g).to(dtype)
     m = np.concatenate((tree_masks(r, T), np.full((extra, 2), 2 ** 64 - 1, np.uint64)))
@@ -266,15 +270,16 @@ def test_attention(case, dtype):
         assert torch.equal(again[0], out)
 
 
-def test_attention_of_a_row_that_sees_nothing_and_of_odd_values():
+@pytest.mark.parametrize("wide", [False, True])
+def test_attention_of_a_row_that_sees_nothing_and_of_odd_values(wide):
     """Infinities and NaN in new rows reach the rows that see them and no others;
     queries and keys of large and tiny magnitude."""
-    T, nkv, nh = [6, 6], 1, 2
+    T, nkv, nh = [6, 6], 1, 8
     pool = Pool([0, 70], nkv, 32)
     tk, tv = new_rows(nkv, 16, 12)
     tv[0, 0, 5, 2], tv[0, 0, 6, 3], tk[0, 0, 4, 0] = math.inf, NAN, NAN
     tv[0, 0, 0, 11] = -math.inf
-    kv, pt = pool.on_gpu(tk, tv)
+    kv, pt = pool.on_gpu(tk, tv, 1 << 19 if wide else 0)
     m = np.zeros((12, 2), np.uint64)
     for i in range(6):
         m[i, 0] = 1 << i        # itself alone
