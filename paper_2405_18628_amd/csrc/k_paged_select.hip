@@ -126,11 +126,10 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
   }
 }
 
-constexpr int KT = 1024;  // threads of the selection
-constexpr int REG = 8;    // keys a thread holds; of more, the passes read them again
-constexpr int KW = KT / 64;
-
+// KT threads, REG keys of each in registers; of more, the passes read them again
+template <int KT, int REG>
 __global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
+  constexpr int KW = KT / 64;
   __shared__ uint32_t red_s[2][KW];
   __shared__ u64 list_s[64], pick_s;
   __shared__ unsigned hist_s[256];
@@ -168,7 +167,7 @@ __global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
   all = wave_all(all, [](uint32_t a, uint32_t b) { return a & b; });
   any = wave_all(any, [](uint32_t a, uint32_t b) { return a | b; });
   if (lane == 0) red_s[0][wave] = all, red_s[1][wave] = any;
-  if (tid < 256) hist_s[tid] = 0;
+  if (KT == 256 || tid < 256) hist_s[tid] = 0;
   if (tid == 0) n_list = 0;
   __syncthreads();
 #pragma unroll
@@ -249,14 +248,12 @@ __global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
       if (lane == 0) cnt_s[0][j][wave] = __popcll(tb[j]), cnt_s[1][j][wave] = __popcll(ab[j]);
     }
     __syncthreads();
-    // counts before each (round, wave): lane: round lane / 16 (+ 4), wave lane % 16
-    int t0 = 0, t1 = 0, a0 = 0, a1 = 0;
-    {
-      const int j = lane >> 4, w = lane & 15;
-      t0 = cnt_s[0][j][w], t1 = cnt_s[0][j + 4][w];
-      a0 = cnt_s[1][j][w], a1 = cnt_s[1][j + 4][w];
-    }
-    static_assert(REG == 8 && KW == 16, "two counts a lane");
+    // counts before each (round, wave): lane: entries lane and 64 + lane
+    constexpr int E = REG * KW;
+    static_assert(E <= 128 && (E < 64 || E % 64 == 0), "two counts a lane");
+    const int *tie_n = &cnt_s[0][0][0], *over_n = &cnt_s[1][0][0];
+    const int t0 = lane < E ? tie_n[min(lane, E - 1)] : 0, t1 = E > 64 ? tie_n[64 % E + lane % (E / 2)] : 0;
+    const int a0 = lane < E ? over_n[min(lane, E - 1)] : 0, a1 = E > 64 ? over_n[64 % E + lane % (E / 2)] : 0;
     const int ti0 = wave_incl(t0), ti1 = wave_incl(t1) + lane_of(ti0, 63);
     // of a group of ties, those below `left` are taken
     auto taken = [&](int upto, int n_ties) { return max(0, min(n_ties, left - (ties + upto - n_ties))); };
@@ -265,9 +262,9 @@ __global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
 #pragma unroll
     for (int j = 0; j < REG; ++j) {
       if (r0 + j >= rounds) break;
-      const int from = (j & 3) * 16 + __builtin_amdgcn_readfirstlane(wave);
-      const int t_before = ties + lane_of(j < 4 ? ti0 - t0 : ti1 - t1, from);
-      int at = done + lane_of(j < 4 ? bi0 - b0 : bi1 - b1, from);
+      const int from = j * KW % 64 + __builtin_amdgcn_readfirstlane(wave);
+      const int t_before = ties + lane_of(j * KW < 64 ? ti0 - t0 : ti1 - t1, from);
+      int at = done + lane_of(j * KW < 64 ? bi0 - b0 : bi1 - b1, from);
       const u64 below = (1ull << lane) - 1;
       const int my_ties = __popcll(tb[j] & below);
       const bool tie = tb[j] >> lane & 1, take = (ab[j] >> lane & 1) || (tie && t_before + my_ties < left);
@@ -294,6 +291,9 @@ hipError_t launch_paged_select(const PagedSelectLaunch &p, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(paged_pick_kernel, dim3(p.nkv * p.sq.B), dim3(KT), 0, s, p);
+  // (fewer threads start and meet sooner: 125 pages 4.9 us with 256, 6.3 with 1024;
+  // of more than a few keys each they take longer: 4097 pages 8.5 us with 512, 7.0 with 1024)
+  const bool few = p.sq.max_pages <= 4 * 256;
+  hipLaunchKernelGGL((few ? paged_pick_kernel<256, 8> : paged_pick_kernel<1024, 8>), dim3(p.nkv * p.sq.B), dim3(few ? 256 : 1024), 0, s, p);
   return hipGetLastError();
 }
