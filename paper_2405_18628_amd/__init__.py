@@ -410,10 +410,13 @@ class PagedCache:
         if bounds is not None:
             if bounds.shape != (*pages.shape[:3], 2, 128) or bounds.dtype != torch.bfloat16 or not bounds.is_contiguous():
                 raise ValueError("bounds must be contiguous bf16 [layers][n_pages][kv_heads][2][128]")
+        self.device = pages.get_device()
         if tail is not None:
             KVQCache._check_rows(tail, (self.n_layers, self.n_kv_heads), "tail")
+        for t, name in ((bounds, "bounds"), (tail.k if tail is not None else None, "tail")):
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"{name} must be on the pages' device")
         self.pages, self.bounds, self.tail = pages, bounds, tail
-        self.device = pages.get_device()
         self.desc = ppd_paged(_ptr(pages), _ptr(bounds) or None, self.n_layers, self.n_kv_heads, self.n_pages, self.page,
                               tail.desc if tail is not None else ppd_kv())
 
@@ -431,11 +434,6 @@ class PagedCache:
         return cls(new(n_layers, n_pages, n_kv_heads, page // PPD_PAGED_BLOCK, 2, 4096),
                    new(n_layers, n_pages, n_kv_heads, 2, 128) if bounds else None, tail)
 
-    def _on_device(self, *checks):
-        """The cache, and the call's other tensors, are on the current device."""
-        tail = self.tail
-        _tensors(self.device, (self.pages, None, "pages"), (self.bounds, None, "bounds"),
-                 (tail.k if tail is not None else None, None, "tail"), *checks)
 
 
 class PageTables:
@@ -465,8 +463,27 @@ class PageTables:
         return cls(torch.zeros((n_seqs, max_pages), **i32), torch.zeros(n_seqs, **i32), torch.arange(n_pages, **i32),
                    torch.tensor([0, n_pages], **i32), page)
 
-    def _on_device(self, *checks):
-        _tensors(self.device, (self.table, None, "table"), *checks)
+
+def _paged_tensors(dev, objs, checks):
+    """_tensors for the calls on pages: `objs`, the caches and tables of the call,
+    looked their tensors over when they were made and have to be of the current
+    device, dev; (tensor or None, dtype or None, name) of the others."""
+    if dev >= 0 and _torch is None:
+        _stream(None)  # sets _torch
+    ok = dev >= 0 and _torch._C._cuda_getDevice() == dev
+    for o in objs:
+        ok = ok and o.device == dev
+    if ok:
+        for t, dtype, _ in checks:
+            if t is not None and not (t.get_device() == dev and t.is_contiguous() and (dtype is None or t.dtype is dtype)):
+                ok = False
+                break
+    if not ok:  # names the fault
+        for o in objs:
+            t = o.pages if isinstance(o, PagedCache) else o.table
+            _tensors(dev, (t, None, "pages" if isinstance(o, PagedCache) else "table"))
+        _tensors(dev, *checks)
+        raise ValueError("a call's caches, tables and tensors must be of one device, the current one")
 
 
 # ---------------------------------------------------------------------------
@@ -670,7 +687,7 @@ def _dtypes():
     t = _torch
     if t is None:
         import torch as t
-    return t.bfloat16, t.float32
+    return t.bfloat16, t.float32, t.int32
 
 
 def _kvq_batch(kvs, counts, checks=()):
@@ -691,7 +708,7 @@ def ppd_kvq_attention(kvs: Sequence[KVQCache], layer: int, L: Sequence[int], T: 
                       lse=None, stream=None):
     """Tree attention of one layer: q, out bf16 [tokens][heads][128], lse float32
     [tokens][heads] (optional), mask int64 / uint64 [tokens][2]."""
-    bf16, f32 = _dtypes()
+    bf16, f32, _ = _dtypes()
     B, descs, Ls, Ts = _kvq_batch(kvs, (L, T), ((q, bf16, "q"), (out, bf16, "out"), (lse, f32, "lse"), (mask, None, "mask"),
                                                 (ws, None, "ws")))
     n = int(Ts[0]) if B == 1 else int(Ts.sum())
@@ -813,11 +830,11 @@ def ppd_paged_tables(pt: PageTables, add, start, slots, ws, len_out=None, free_s
     """Pages for add [n_seqs] more tokens of every sequence (negative: it has
     ended); start [n_seqs + 1] and slots get the rows' offsets and places.
     Lengths and the ring's state are written to pt unless given elsewhere."""
-    i32 = _i32_dtype()
+    i32 = _dtypes()[2]
     len_out = pt.len if len_out is None else len_out
     free_state_out = pt.free_state if free_state_out is None else free_state_out
-    pt._on_device((add, i32, "add"), (start, i32, "start"), (slots, i32, "slots"), (ws, None, "ws"),
-                  (len_out, i32, "len_out"), (free_state_out, i32, "free_state_out"))
+    _paged_tensors(pt.device, (pt,), ((add, i32, "add"), (start, i32, "start"), (slots, i32, "slots"), (ws, None, "ws"),
+                                      (len_out, i32, "len_out"), (free_state_out, i32, "free_state_out")))
     n = pt.n_seqs
     if add.numel() != n or len_out.numel() != n or start.numel() != n + 1 or free_state_out.numel() != 2:
         raise ValueError(f"add and len_out must be [{n}], start [{n + 1}], free_state_out [2]")
@@ -828,10 +845,10 @@ def ppd_paged_tables(pt: PageTables, add, start, slots, ws, len_out=None, free_s
 def ppd_paged_store(kv: PagedCache, src: KVCache, start, row_start, path, slots, stream=None):
     """Rows of src into pages: row start[s] + k to slots[start[s] + k], from src's
     row row_start[s] + path[row_start[s] + k] (path None: row_start[s] + k)."""
-    i32 = _i32_dtype()
+    i32 = _dtypes()[2]
     KVQCache._check_rows(src, (kv.n_layers, kv.n_kv_heads), "src")
-    kv._on_device((src.k, None, "src"), (start, i32, "start"), (row_start, i32, "row_start"), (path, i32, "path"),
-                  (slots, i32, "slots"))
+    _paged_tensors(kv.device, (kv,), ((src.k, None, "src"), (start, i32, "start"), (row_start, i32, "row_start"),
+                                      (path, i32, "path"), (slots, i32, "slots")))
     n = start.numel() - 1
     if row_start.numel() < n:
         raise ValueError(f"row_start holds {row_start.numel()} offsets, not {n}")
@@ -843,27 +860,18 @@ def ppd_paged_attention_workspace_bytes(n_heads: int, n_kv_heads: int, n_seqs: i
     return _bytes(lib().ppd_paged_attention_workspace_bytes(int(n_heads), int(n_kv_heads), int(n_seqs), int(n_rows)))
 
 
-def _i32_dtype():
-    t = _torch
-    if t is None:
-        import torch as t
-    return t.int32
-
-
-def _paged_rows(kv, pt, row_start, q, sel, n_sel, budget, *checks):
-    """The checks that attention and selection share; the rows' type as PPD_F32 or PPD_BF16."""
-    i32 = _i32_dtype()
-    bf16, f32 = _dtypes()
-    kv._on_device((pt.table, None, "table"), (row_start, i32, "row_start"), (q, None, "q"), (sel, i32, "sel"),
-                  (n_sel, i32, "n_sel"), *checks)
+def _paged_rows(kv, pt, row_start, q, sel, n_sel, budget):
+    """The checks that attention and selection share; rows and heads of q, its type as PPD_F32 or PPD_BF16."""
+    bf16, f32, _ = _dtypes()
     n = pt.n_seqs
     if row_start.numel() != n + 1:
         raise ValueError(f"row_start must be [{n + 1}]")
-    if q.dim() != 3 or q.shape[2] != 128 or q.dtype not in (bf16, f32):
+    shape, dt = q.shape, q.dtype
+    if len(shape) != 3 or shape[2] != 128 or (dt is not bf16 and dt is not f32):
         raise ValueError("q must be bf16 or float32 [rows][heads][128]")
     if sel is not None and (sel.shape != (n, kv.n_kv_heads, budget) or n_sel is None or n_sel.numel() != n):
         raise ValueError(f"sel must be [{n}][{kv.n_kv_heads}][budget], n_sel [{n}]")
-    return PPD_F32 if q.dtype is f32 else PPD_BF16
+    return shape[0], shape[1], PPD_F32 if dt is f32 else PPD_BF16
 
 
 def ppd_paged_attention(kv: PagedCache, layer: int, pt: PageTables, row_start, q, mask, out, ws, lse=None, sel=None,
@@ -873,9 +881,10 @@ def ppd_paged_attention(kv: PagedCache, layer: int, pt: PageTables, row_start, q
     uint64 [rows][2] (None: a row sees its sequence's rows up to itself), lse
     float32 [rows][heads] (optional)."""
     budget = sel.shape[2] if sel is not None and sel.dim() == 3 else 0
-    dt = _paged_rows(kv, pt, row_start, q, sel, n_sel, budget, (out, q.dtype, "out"), (lse, _dtypes()[1], "lse"),
-                     (mask, None, "mask"), (ws, None, "ws"))
-    n, nh, _ = q.shape
+    _, f32, i32 = _dtypes()
+    _paged_tensors(kv.device, (kv, pt), ((row_start, i32, "row_start"), (q, None, "q"), (out, q.dtype, "out"), (mask, None, "mask"),
+                                         (ws, None, "ws"), (lse, f32, "lse"), (sel, i32, "sel"), (n_sel, i32, "n_sel")))
+    n, nh, dt = _paged_rows(kv, pt, row_start, q, sel, n_sel, budget)
     if out.shape != q.shape or (lse is not None and lse.shape != (n, nh)):
         raise ValueError(f"out must be [{n}][{nh}][128], lse [{n}][{nh}]")
     if mask is not None and mask.numel() * mask.element_size() < 16 * n:
@@ -894,8 +903,11 @@ def ppd_paged_select(kv: PagedCache, layer: int, pt: PageTables, row_start, q, b
                      n_sel, ws, stream=None):
     """The pages that matter most to each sequence's rows, a list for each kv head:
     sel int32 [n_seqs][kv_heads][budget], n_sel int32 [n_seqs]."""
-    dt = _paged_rows(kv, pt, row_start, q, sel, n_sel, budget, (ws, None, "ws"))
-    _check(lib().ppd_paged_select(q.shape[1], C.byref(kv.desc), int(layer), C.byref(pt.desc), _ptr(row_start), q.shape[0],
+    i32 = _dtypes()[2]
+    _paged_tensors(kv.device, (kv, pt), ((row_start, i32, "row_start"), (q, None, "q"), (sel, i32, "sel"), (n_sel, i32, "n_sel"),
+                                         (ws, None, "ws")))
+    n, nh, dt = _paged_rows(kv, pt, row_start, q, sel, n_sel, budget)
+    _check(lib().ppd_paged_select(nh, C.byref(kv.desc), int(layer), C.byref(pt.desc), _ptr(row_start), n,
                                   _ptr(q), dt, int(budget), int(n_first), int(n_last), _ptr(sel), _ptr(n_sel), _ptr(ws),
                                   ws.numel() * ws.element_size(), _stream(stream)))
 
@@ -910,8 +922,8 @@ def ppd_verify_batch_paged(model: Model, kv: PagedCache, pt: PageTables, row_sta
     budget > 0: attention to the pages that ppd_paged_select picks."""
     import torch
     i32 = torch.int32
-    kv._on_device((pt.table, None, "table"), (row_start, i32, "row_start"), (ids, i32, "ids"), (depth, i32, "depth"),
-                  (mask, None, "mask"), (ws, None, "ws"), (logits, torch.float32, "logits"), (pred, i32, "pred"))
+    _paged_tensors(kv.device, (kv, pt), ((row_start, i32, "row_start"), (ids, i32, "ids"), (depth, i32, "depth"), (mask, None, "mask"),
+                                         (ws, None, "ws"), (logits, torch.float32, "logits"), (pred, i32, "pred")))
     n = ids.numel()
     if row_start.numel() != pt.n_seqs + 1:
         raise ValueError(f"row_start must be [{pt.n_seqs + 1}]")
