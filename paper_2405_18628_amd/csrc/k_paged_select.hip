@@ -51,7 +51,7 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
   const int tid = threadIdx.x, lane = tid & 63;
   const int c = blockIdx.x % chunks, kvh = blockIdx.x / chunks % p.nkv, sq = blockIdx.x / chunks / p.nkv;
   const int page0 = c * CH + (tid >> 6) * PAGES;
-  // ---- this wave's bounds (the table's entries are requested beside the length)
+  // (the table's entries are requested beside the length)
   const int32_t *table = p.sq.table + (size_t)sq * p.sq.max_pages;
   const int entry = table[min(page0 + (lane & (PAGES - 1)), p.sq.max_pages - 1)];
   bool bad = false;
@@ -59,6 +59,24 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
   if (bad && c == 0 && tid == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   const int n = (s.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
   if (n <= p.budget || c * CH >= n) return;  // all are taken
+  // ---- sums of the queries' positive and negative parts; the first rows and then the
+  // bounds are requested before either is used
+  const int G = p.nh / p.nkv, R = s.T * G, wave = tid >> 6;
+  const uint32_t inv = G > 1 ? 0xffffffffu / G + 1 : 0;
+  constexpr int QB = 16;  // rows of a wave in flight
+  float2 x[QB];
+  auto request = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < QB; ++u) {
+      const int r = r0 + u * (ST / 64);
+      if (r >= R) break;
+      int t = G > 1 ? (int)__umulhi((uint32_t)r, inv) : r;  // r / G
+      t -= t * G > r;
+      x[u] = query2<QT>(p, s.t0 + t, kvh * G + r - t * G, 2 * lane);
+    }
+  };
+  request(wave);
+  __builtin_amdgcn_sched_barrier(0);
   const int phys = paged_clamp(entry, p.sq.n_pages);
   u32x4 w[PAGES / 2];
 #pragma unroll
@@ -66,16 +84,18 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
     const int page = __shfl(phys, 2 * i + (lane >> 5), 64);
     w[i] = *(const u32x4 *)(p.bounds + ((size_t)page * p.nkv + kvh) * 256 + (lane & 31) * 8);
   }
-  // ---- sums of the queries' positive and negative parts
-  const int G = p.nh / p.nkv, R = s.T * G, wave = tid >> 6;
+  __builtin_amdgcn_sched_barrier(0);
   double qp[2] = {0.0, 0.0}, qm[2] = {0.0, 0.0};
-#pragma unroll 8
-  for (int r = wave; r < R; r += ST / 64) {
-    const float2 x = query2<QT>(p, s.t0 + r / G, kvh * G + r % G, 2 * lane);
-    qp[0] += (double)(x.x <= 0.f ? 0.f : x.x);  // (a NaN stays one)
-    qp[1] += (double)(x.y <= 0.f ? 0.f : x.y);
-    qm[0] += (double)(x.x >= 0.f ? 0.f : x.x);
-    qm[1] += (double)(x.y >= 0.f ? 0.f : x.y);
+  for (int r0 = wave; r0 < R; r0 += QB * (ST / 64)) {
+    if (r0 != wave) request(r0);
+#pragma unroll
+    for (int u = 0; u < QB; ++u) {
+      if (r0 + u * (ST / 64) >= R) break;
+      qp[0] += (double)(x[u].x <= 0.f ? 0.f : x[u].x);  // (a NaN stays one)
+      qp[1] += (double)(x[u].y <= 0.f ? 0.f : x[u].y);
+      qm[0] += (double)(x[u].x >= 0.f ? 0.f : x[u].x);
+      qm[1] += (double)(x[u].y >= 0.f ? 0.f : x[u].y);
+    }
   }
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
@@ -116,13 +136,13 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
     }
     i = 2 * i + up;
   }
-  double x = v[0];
+  double score = v[0];
 #pragma unroll
-  for (int o = 16 / NV; o > 0; o /= 2) x += __shfl_xor(x, o, 64);
+  for (int o = 16 / NV; o > 0; o /= 2) score += __shfl_xor(score, o, 64);
   const int page = page0 + 2 * i + (lane >> 5);
   if (lane % (32 / NV) == 0 && page < n) {
     const bool kept = page < p.n_first || page >= n - p.n_last;
-    p.keys[((size_t)sq * p.nkv + kvh) * p.sq.max_pages + page] = kept ? kKept : key_of(x);
+    p.keys[((size_t)sq * p.nkv + kvh) * p.sq.max_pages + page] = kept ? kKept : key_of(score);
   }
 }
 
