@@ -591,10 +591,12 @@ ppd_status ppd_paged_tables(const ppd_page_tables *pt, const int32_t *add, int32
  * slots[start[s] + k] from row
  *   row_start[s] + path[row_start[s] + k]   of src (accepted nodes of a tree), or
  *   row_start[s] + k                        where path is NULL (a prompt)
- * Rows at and behind n_rows, and slots outside the pages, are left out; source rows
- * are clamped to src.  A page's bounds start anew with its first position
- * and else widen; a NaN has no part in them.  Rows of one sequence have rising
- * positions, and no page is written for two sequences.
+ * The slots of a sequence's rows are those of neighbouring positions, as
+ * ppd_paged_tables gives them, and no page is written for two sequences.  Rows
+ * at and behind n_rows, and runs of slots that start outside the pages, are left
+ * out; rows outside src read some row of it.  A page's bounds start anew with its
+ * first position and else widen; a NaN has no part in them (of NaN alone,
+ * infinities are left).
  *   src        the tail or another bfloat16 cache of the same layers and heads
  *   row_start  device int32[n_seqs]; path device int32 (n_path entries) or NULL
  *   slots      device int32[n_rows]

@@ -26,6 +26,7 @@ constexpr int NT = 512;              // threads of the second launch
 constexpr int kLeast = 2;            // blocks of a wave, at least, where a prefix is split
 constexpr int OROW = PPD_ATTN_OROW;  // partial row: 128 dims, m, l, padding (floats)
 constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kNoSplit = PPD_CAPACITY_MAX;  // more blocks than a sequence has
 
 // parts of a query and of a probability on the matrix cores: bfloat16 outputs
 // round to 2^-9, two parts of a probability leave 2^-17 of it; float32 calls
@@ -103,7 +104,7 @@ __device__ __forceinline__ Load load_of(const PagedAttnLaunch &p, int s, const P
 // 1.5 kPagedSlots at most below.
 template <int LEAST>
 __device__ __forceinline__ int blocks_each(int64_t total, int slots) {
-  return (int)max((total + slots - 1) / slots, (int64_t)LEAST);
+  return (int)min(max((total + slots - 1) / slots, (int64_t)LEAST), (int64_t)kNoSplit);
 }
 __device__ __forceinline__ int splits_of(const Load &w, int c) {
   c = max(c, (w.nblk + kPagedSplits - 1) / kPagedSplits);
@@ -151,7 +152,7 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, P
     for (int i = 0; i < 4; ++i) {
       const int n = (int)wave_total((int64_t)w.units * splits_of(w, c));
       if (n <= kPagedSlots) break;
-      c = (int)(((int64_t)c * n + kPagedSlots - 1) / kPagedSlots);
+      c = (int)min(((int64_t)c * n + kPagedSlots - 1) / kPagedSlots, (int64_t)kNoSplit);
     }
   }
   int slots0 = 0, parts0 = 0;

@@ -154,6 +154,35 @@ def test_store(page, layers, nkv, B, tree, off, bounds):
             assert torch.equal(kv.bounds.cpu().nan_to_num(77.0), bd.nan_to_num(77.0)), step
 
 
+@pytest.mark.parametrize("tree", [False, True])
+def test_store_of_many_sequences(tree):
+    """300 sequences, some without rows; slots that are not 16-byte aligned."""
+    r = np.random.default_rng(3)
+    B, page, T = 300, 32, 3
+    pt = ppd.PageTables.empty(B, 3, 700, page)
+    pt.free_pages.copy_(dev(r.permutation(700)))
+    kv = ppd.PagedCache.empty(1, 2, 700, page, 8)
+    kv.pages.zero_(), kv.bounds.zero_()
+    ws = workspace(ppd.ppd_paged_tables_workspace_bytes(B))
+    pages, bd = kv.pages.cpu(), kv.bounds.cpu()
+    for step in range(3):
+        add = r.integers(0, T + 1 if tree else 30, B).astype(np.int32)
+        rows, start = int(add.sum()), torch.zeros(B + 1, dtype=I32, device="cuda")
+        slots = torch.full((rows + 5,), -9, dtype=I32, device="cuda")[1:]
+        before = [t.cpu().numpy() for t in (pt.table, pt.len, pt.free_pages, pt.free_state)]
+        ppd.ppd_paged_tables(pt, dev(add), start, slots, ws)
+        want = R.tables(before[0], before[1], add, before[2], before[3], page, rows + 4, np.full(rows + 4, -9, np.int32))
+        assert np.array_equal(slots.cpu().numpy(), want[5]) and np.array_equal(start.cpu().numpy(), want[4])
+        assert np.array_equal(pt.table.cpu().numpy(), want[0]) and ppd.ppd_device_status(ws) == 0
+        row_start = offsets([T] * B) if tree else offsets(add)
+        path = np.tile(np.arange(T, dtype=np.int32)[::-1], B) if tree else None
+        cap = (int(row_start[-1]) + 7) // 8 * 8 + 8
+        k, v = torch.randn((1, 2, cap, 128), device="cuda").to(BF), torch.randn((1, 2, 128, cap), device="cuda").to(BF)
+        ppd.ppd_paged_store(kv, ppd.KVCache(k, v), start, dev(row_start), None if path is None else dev(path), slots)
+        R.store(pages, bd, k.cpu(), v.cpu(), want[4].tolist(), row_start.tolist(), path, want[5][:rows], page)
+        assert torch.equal(kv.pages.cpu(), pages) and torch.equal(kv.bounds.cpu(), bd), step
+
+
 def test_store_leaves_out_what_lies_outside():
     kv = ppd.PagedCache.empty(1, 1, 2, 32, 8)
     kv.pages.zero_(), kv.bounds.zero_()
@@ -299,6 +328,33 @@ def test_attention_of_a_row_that_sees_nothing_and_of_odd_values(wide):
         got = out.cpu().double()
         ref.out[~keep] = got[~keep] = 0.0
         ref.check(got, lse)
+
+
+@pytest.mark.parametrize("nkv", [1, 2])
+def test_attention_and_selection_of_many_sequences(nkv):
+    """300 sequences, most without rows or without a prefix, some that share all pages."""
+    r = np.random.default_rng(nkv)
+    lens = np.where(r.random(300) < 0.4, 0, r.integers(1, 200, 300)).tolist()
+    lens[123] = 3000
+    T = np.where(r.random(300) < 0.7, 0, r.integers(1, 4, 300))
+    T[123], T[7], lens[7] = 2, 1, 150
+    for s in range(200, 220):
+        lens[s], T[s] = 0, 1
+    pool = Pool(lens, nkv, 32, seed=nkv)
+    for s in range(200, 220):                           # these read sequence 7's pages
+        pool.table[s], pool.lens[s] = pool.table[7], 150 - (s - 200)
+    rows = int(T.sum())
+    tk, tv = new_rows(nkv, (rows + 15) // 8 * 8, rows)
+    kv, pt = pool.on_gpu(tk, tv)
+    q = torch.randn((rows, 2 * nkv, 128), generator=torch.Generator().manual_seed(1)).to(BF)
+    row_start = offsets(T)
+    out, lse, ws = attend(kv, pt, dev(row_start), q.cuda(), None)
+    assert ppd.ppd_device_status(ws) == 0
+    table = torch.from_numpy(pool.table)
+    R.Attention(pool.pages, table, pool.lens, tk, tv, 0, row_start, q, None, 32).check(out, lse)
+    sel, n_sel = run_select(pool, kv, pt, row_start, q, 3, 1, 1)
+    out, lse, _ = attend(kv, pt, dev(row_start), q.cuda(), None, sel=sel, n_sel=n_sel)
+    R.Attention(pool.pages, table, pool.lens, tk, tv, 0, row_start, q, None, 32, sel.cpu(), n_sel.cpu()).check(out, lse)
 
 
 @pytest.mark.parametrize("page,lens,T,nh,nkv,budget", [(32, [500, 90, 20], [1, 4, 2], 4, 2, 5), (64, [3000], [20], 4, 1, 17),

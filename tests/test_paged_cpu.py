@@ -1,6 +1,7 @@
 """The paged cache without a GPU: refusals of the C ABI and of the binding, sizes,
 and the reference forms against their definitions."""
 import ctypes as C
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -8,6 +9,7 @@ import torch
 
 import paged_reference as R
 import paper_2405_18628_amd as ppd
+from test_kernel_resources_cpu import _kernels
 
 F = 0x10000  # a pointer that is never followed
 L = ppd.lib()
@@ -204,3 +206,50 @@ def test_a_pages_score_bounds_its_keys():
     lo, hi = k.amin(0), k.amax(0)
     up = q.clamp(min=0).sum(0) @ hi + q.clamp(max=0).sum(0) @ lo
     assert bool(((q @ k.t()).sum(0) <= up).all())
+
+
+class On:
+    """A contiguous device tensor of device d, as far as the checks look."""
+    is_cuda = True
+
+    def __init__(self, d, dtype=torch.int32):
+        self.d, self.dtype = d, dtype
+
+    def get_device(self):
+        return self.d
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return 4
+
+
+def test_calls_refuse_another_device(monkeypatch):
+    """Tensors, tables or caches of device 1 with device 0 current, and the other way round."""
+    monkeypatch.setattr(ppd, "_torch", SimpleNamespace(
+        _C=SimpleNamespace(_cuda_getDevice=lambda: 0), bfloat16=torch.bfloat16, float32=torch.float32, int32=torch.int32))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    bf = torch.bfloat16
+    kv = ppd.PagedCache(torch.zeros((1, 3, 4, 2, 2, 4096), dtype=bf), torch.zeros((1, 3, 4, 2, 128), dtype=bf))
+    pt = ppd.PageTables.empty(3, 5, 3, 64, device="cpu")
+    kv.pages, pt.table = On(0, bf), On(0)
+    for cache, table, tensor in ((1, 1, 1), (0, 1, 0), (1, 0, 0), (0, 0, 1)):
+        kv.device, pt.device, kv.pages.d, pt.table.d = cache, table, cache, table
+        t, f = On(tensor), On(tensor, torch.float32)
+        f.shape = (4, 8, 128)
+        with pytest.raises(ValueError):
+            ppd.ppd_paged_select(kv, 0, pt, t, f, 2, 0, 0, t, t, t)
+        with pytest.raises(ValueError):
+            ppd.ppd_paged_attention(kv, 0, pt, t, f, None, f, t)
+        if (cache, table, tensor) != (1, 0, 0):
+            with pytest.raises(ValueError):
+                ppd.ppd_paged_tables(pt, t, t, t, t, t, t)
+
+
+def test_kernels_use_no_scratch_memory():
+    mine = [k for k in _kernels() if "paged_" in k[".name"]]
+    for part in ("paged_tables_kernel", "paged_put_kernel", "paged_fill_rows_kernel", "paged_attention_kernel", "paged_merge_kernel",
+                 "paged_score_kernel", "paged_pick_kernel"):
+        assert any(part in k[".name"] for k in mine), part
+    assert not [k[".name"] for k in mine if k[".private_segment_fixed_size"]]
