@@ -247,7 +247,7 @@ __device__ __forceinline__ int uniform_load(const int32_t *p, int64_t i) {
 template <int NQ, int QW, int PARS, int QT>
 __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(PagedAttnLaunch p) {
   constexpr int NT = 64 * QW * PARS;
-  constexpr bool JOIN = NQ * QW == 1;  // the last of a row group's splits adds them
+  constexpr bool JOIN = QW == 1;  // the last of a row group's splits adds them
   constexpr int RW = QW * NQ * 16;  // rows of the workgroup
   constexpr int QP = q_parts(QT), PP = p_parts(QT);
   constexpr bool QLDS = NQ > 1 || QP > 2;  // no registers left for the queries
@@ -598,19 +598,20 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
     const size_t first_at = (size_t)(my_part - ks) * RW * OROW;
     constexpr size_t stride = (size_t)RW * OROW;
     // 32 threads a row; of few rows several such groups share one (ways), of more
-    // than eight a group takes two.  A round of splits is requested for both, and
-    // beside the first the splits' maxima and sums, of which LDS gets the factors
+    // than eight a group takes two at a time.  A round of splits is requested for
+    // both, and beside the first the splits' maxima and sums, of which LDS gets the
+    // factors
     constexpr int GR = NT / 32, N = 8;
-    static_assert(2 * GR >= RW, "two rows a group");
     const int ways = n_rows >= 5 ? 1 : n_rows >= 3 ? GR / 4 : n_rows == 2 ? GR / 2 : GR;
-    const int group = tid >> 5, sub = group % ways, rl = group / ways;
-    const bool two = ways == 1 && rl + GR < n_rows;
+    const int group = tid >> 5, sub = group % ways;
+    int rl = group / ways;
     floatx4 x[N], y[N];
+    auto two = [&] { return ways == 1 && rl + GR < n_rows; };
     auto request = [&](int s0) {
 #pragma unroll
       for (int v = 0; v < N; ++v)
         x[v] = get_far(far, first_at + min(s0 + v * ways, KS - 1) * stride + (size_t)min(rl, n_rows - 1) * OROW + d4);
-      if (two)
+      if (two())
 #pragma unroll
         for (int v = 0; v < N; ++v) y[v] = get_far(far, first_at + min(s0 + v, KS - 1) * stride + (size_t)(rl + GR) * OROW + d4);
     };
@@ -646,32 +647,35 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
       }
     }
     __syncthreads();
-    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f}, o2 = o;
-    const int row = min(rl, n_rows - 1);
-    for (int s0 = sub; s0 < KS; s0 += N * ways) {
-      if (s0 != sub) request(s0);
-#pragma unroll
-      for (int v = 0; v < N; ++v)
-        if (s0 + v * ways < KS) o += wt_s[row][s0 + v * ways] * x[v];
-      if (two)
-#pragma unroll
-        for (int v = 0; v < N; ++v)
-          if (s0 + v < KS) o2 += wt_s[rl + GR][s0 + v] * y[v];
-    }
     auto store = [&](int row, floatx4 v) {
       const int r = row0 + row;
       store_out4<QT>(p, t0 + r / G, kvh * G + r % G, d4, v * fac_s[row][0]);
     };
-    if (ways == 1) {
-      if (rl < n_rows) store(rl, o);
-      if (two) store(rl + GR, o2);
+    for (bool first = true; first || rl < n_rows; first = false, rl += 2 * GR) {
+      floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f}, o2 = o;
+      const int row = min(rl, n_rows - 1);
+      for (int s0 = sub; s0 < KS; s0 += N * ways) {
+        if (!first || s0 != sub) request(s0);
+#pragma unroll
+        for (int v = 0; v < N; ++v)
+          if (s0 + v * ways < KS) o += wt_s[row][s0 + v * ways] * x[v];
+        if (two())
+#pragma unroll
+          for (int v = 0; v < N; ++v)
+            if (s0 + v < KS) o2 += wt_s[rl + GR][s0 + v] * y[v];
+      }
+      if (ways == 1) {
+        if (rl < n_rows) store(rl, o);
+        if (two()) store(rl + GR, o2);
+        continue;
+      }
+      sum_s[group * 32 + (tid & 31)] = o;  // (a single round: few rows)
+      __syncthreads();
+      if (sub == 0 && rl < n_rows) {
+        for (int w = 1; w < ways; ++w) o += sum_s[(group + w) * 32 + (tid & 31)];
+        store(rl, o);
+      }
       return;
-    }
-    sum_s[group * 32 + (tid & 31)] = o;
-    __syncthreads();
-    if (sub == 0 && rl < n_rows) {
-      for (int w = 1; w < ways; ++w) o += sum_s[(group + w) * 32 + (tid & 31)];
-      store(rl, o);
     }
   }
 }
@@ -735,13 +739,13 @@ __global__ __launch_bounds__(NT) void paged_merge_kernel(PagedAttnLaunch p, int 
 
 }  // namespace
 
-// 16-row tiles a wave holds and waves side by side, by the tiles of a kv head
+// tiles a wave holds, waves side by side and over blocks, by the tiles of a workgroup
 struct Shape {
   int nq, qw, pars;
   int rows() const { return 16 * nq * qw; }
 };
 static Shape paged_shape(int tiles) {
-  return tiles <= 1 ? Shape{1, 1, 4} : tiles <= 2 ? Shape{2, 1, 4} : tiles <= 4 ? Shape{2, 2, 4} : Shape{2, 4, 2};
+  return tiles == 1 ? Shape{1, 1, 4} : tiles == 2 ? Shape{2, 1, 4} : tiles == 4 ? Shape{2, 2, 4} : Shape{2, 4, 2};
 }
 // 16-row tiles of a kv head's rows (of an average sequence: how many a single one
 // has is only known on the device, and any shape serves any number)
@@ -749,29 +753,39 @@ static int paged_tiles(int nh, int nkv, int B, int n_rows) {
   const int64_t rows = std::min<int64_t>((n_rows + B - 1) / B, PPD_T_MAX) * (nh / nkv);
   return (int)std::min<int64_t>(64, (rows + 15) / 16);
 }
-// Blocks that a workgroup reads where each takes a tile of its own, at most: while
-// they are few the tiles of a kv head read its keys from the XCD's cache beside
-// one another, which is less than what several tiles in a workgroup cost.
-constexpr int64_t kOwnTileBlocks = 64;
+// Tiles of a workgroup, by the blocks that one would read with a tile or two of its
+// own.  While they are few the tiles of a kv head read its keys from the XCD's
+// cache beside one another, which is less than what more tiles in a workgroup cost
+// in registers, LDS and meeting; with many a compute unit's load path (it holds 32
+// KB of loads, some 50 GB/s) is the bound, and wide workgroups read every block once.
+// us, by tiles of a workgroup 1, 2, 4 or 8: 32 heads of 64 nodes, 1024 positions 16.0,
+// 18.1, 19.9; 4096 29.3, 26.1, 29.5; 32768 166, 121, 111; of 128 nodes 2048 25.3, 24.8,
+// 28.9; 8192 74, 60, 52; of 32 nodes 2000 16.0, 20.5; 8192 33.4, 35.7
+constexpr int64_t kOwnTileBlocks = 48, kTwoTileBlocks = 96;
+static int paged_width(int tiles, int64_t blocks_of_a_tile) {
+  const int64_t two = blocks_of_a_tile * ((tiles + 1) / 2), one = blocks_of_a_tile * tiles;
+  if (tiles == 1 || one <= kOwnTileBlocks * kPagedSlots) return 1;
+  return tiles == 2 || two <= kTwoTileBlocks * kPagedSlots ? 2 : tiles <= 4 ? 4 : 8;
+}
 
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows) {
-  const Shape sh = paged_shape(paged_tiles(nh, nkv, B, n_rows));
+  const int tiles = paged_tiles(nh, nkv, B, n_rows);  // (of the widest workgroup it may become)
+  const Shape sh = paged_shape(tiles <= 2 ? tiles : tiles <= 4 ? 4 : 8);
   return 3 * (size_t)kPagedSlots * sh.rows() * OROW * sizeof(float);
 }
 
 void paged_attn_shape(PagedAttnLaunch &a) {
-  a.tiles = paged_tiles(a.nh, a.nkv, a.sq.B, a.sq.n_rows);
   const int most = a.sel ? std::min(a.budget, a.sq.max_pages) : a.sq.max_pages;
   const int64_t blocks = ((int64_t)most << (a.sq.lp - 5)) + 1;
-  if (blocks * a.nkv * std::min(a.sq.B, a.sq.n_rows) * a.tiles <= kOwnTileBlocks * kPagedSlots) a.tiles = 1;
-  a.may_split = ((int64_t)most << (a.sq.lp - 5)) + PPD_T_MAX / kPB > kLeast * paged_shape(a.tiles).pars;
+  a.tiles = paged_width(paged_tiles(a.nh, a.nkv, a.sq.B, a.sq.n_rows), blocks * a.nkv * std::min(a.sq.B, a.sq.n_rows));
+  a.may_split = blocks + PPD_T_MAX / kPB > kLeast * paged_shape(a.tiles).pars;
 }
 
 template <int QT>
 static hipError_t launch_attn(const PagedAttnLaunch &a, hipStream_t s) {
-  auto kernel = a.tiles <= 1   ? paged_attention_kernel<1, 1, 4, QT>
-                : a.tiles <= 2 ? paged_attention_kernel<2, 1, 4, QT>
-                : a.tiles <= 4 ? paged_attention_kernel<2, 2, 4, QT>
+  auto kernel = a.tiles == 1   ? paged_attention_kernel<1, 1, 4, QT>
+                : a.tiles == 2 ? paged_attention_kernel<2, 1, 4, QT>
+                : a.tiles == 4 ? paged_attention_kernel<2, 2, 4, QT>
                                : paged_attention_kernel<2, 4, 2, QT>;
   const Shape sh = paged_shape(a.tiles);
   const int rw = sh.rows();
@@ -779,7 +793,7 @@ static hipError_t launch_attn(const PagedAttnLaunch &a, hipStream_t s) {
   const int64_t rows = (int64_t)a.sq.n_rows * (a.nh / a.nkv);
   const int64_t units = a.nkv * (std::min<int64_t>(a.sq.B, a.sq.n_rows) + rows / rw);
   const dim3 grid((unsigned)(units + (a.may_split ? 3 * kPagedSlots / 2 : 0))), block(64 * sh.qw * sh.pars);
-  const bool merge = a.may_split && sh.nq * sh.qw > 1;
+  const bool merge = a.may_split && sh.qw > 1;
   const hipEvent_t ev0 = (hipEvent_t)a.ev_start, ev1 = (hipEvent_t)a.ev_stop;
   if (ev0)
     hipExtLaunchKernelGGL(kernel, grid, block, 0, s, ev0, merge ? (hipEvent_t) nullptr : ev1, 0, a);

@@ -148,7 +148,7 @@ struct PagedAttnLaunch {
   uint32_t *ctr;               // arrivals of row groups' splits, a byte each: zero between launches
   uint32_t *status;
   float scale_log2;
-  int tiles;                   // 16-row tiles of a kv head's rows, by which the kernel's shape is chosen
+  int tiles;                   // 16-row tiles of a workgroup: 1, 2, 4 or 8
   int may_split;               // a sequence can be long enough for more than one workgroup
   void *ev_start, *ev_stop;
 };
