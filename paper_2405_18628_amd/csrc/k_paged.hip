@@ -18,7 +18,6 @@ namespace {
 // state may be written where they are read: the last workgroup to have read
 // them does it.
 
-constexpr int TT = 1024;
 enum { kEnded = -1, kRefused = 0, kServed = 1 };
 
 struct TablesPlan {
@@ -29,7 +28,7 @@ struct TablesPlan {
 };
 
 // inclusive sums over the workgroup's threads; all: of all of them
-template <int N>
+template <int TT, int N>
 __device__ __forceinline__ void block_scan(int64_t (&v)[N], int64_t (&all)[N], int64_t (*waves)[N]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
@@ -50,7 +49,7 @@ __device__ __forceinline__ int64_t pages_of(int64_t n, int lp) { return (n + (1 
 // i of a ring of n, i < 2 n
 __device__ __forceinline__ int in_ring(int64_t i, int n) { return (int)(i >= n ? i - n : i); }
 
-template <int PER>  // sequences of a thread
+template <int TT, int PER>  // threads, sequences of a thread
 __global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
   __shared__ TablesPlan plan;
   __shared__ int64_t sums_s[2][TT / 64][2];
@@ -81,7 +80,7 @@ __global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) v[0] += grow[i], v[1] += ended[i] ? old[i] : 0;
   const int64_t rows = v[0], back = v[1];
-  block_scan<2>(v, all, sums_s[0]);
+  block_scan<TT, 2>(v, all, sums_s[0]);
   int64_t start = v[0] - rows, given = v[1] - back;
   const int64_t all_back = all[1];
   // new pages of those that fit
@@ -97,7 +96,7 @@ __global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
     at += grow[i];
   }
   const int64_t wanted = mine[0];
-  block_scan<1>(mine, all_need, (int64_t(*)[1])sums_s[1]);
+  block_scan<TT, 1>(mine, all_need, (int64_t(*)[1])sums_s[1]);
   int64_t asked = mine[0] - wanted;
   bool refused = false;
 #pragma unroll
@@ -472,9 +471,16 @@ __global__ __launch_bounds__(64 * SW) void paged_fill_rows_kernel(PagedStoreLaun
 
 hipError_t launch_paged_tables(const PagedTablesLaunch &p, hipStream_t s) {
   // four rows a thread, a sequence a wave (for pages given back)
-  const int64_t rows = ((int64_t)p.n_slots + 4 * TT - 1) / (4 * TT), seqs = (p.B + TT / 64 - 1) / (TT / 64);
-  const int grid = (int)std::min<int64_t>(256, std::max(rows, seqs));
-  hipLaunchKernelGGL(p.B <= TT ? paged_tables_kernel<1> : paged_tables_kernel<PPD_PAGED_SEQS_MAX / TT>, dim3(grid), dim3(TT), 0, s, p);
+  auto parts = [&](int threads) {
+    const int64_t rows = ((int64_t)p.n_slots + 4 * threads - 1) / (4 * threads), seqs = (p.B + threads / 64 - 1) / (threads / 64);
+    return (int)std::min<int64_t>(256, std::max(rows, seqs));
+  };
+  if (p.B <= 256 && p.n_slots <= 4096)  // (few threads start and meet sooner)
+    hipLaunchKernelGGL((paged_tables_kernel<256, 1>), dim3(parts(256)), dim3(256), 0, s, p);
+  else if (p.B <= 1024)
+    hipLaunchKernelGGL((paged_tables_kernel<1024, 1>), dim3(parts(1024)), dim3(1024), 0, s, p);
+  else
+    hipLaunchKernelGGL((paged_tables_kernel<1024, PPD_PAGED_SEQS_MAX / 1024>), dim3(parts(1024)), dim3(1024), 0, s, p);
   return hipGetLastError();
 }
 
