@@ -616,7 +616,10 @@ ppd_status ppd_paged_store(const ppd_paged *kv, const ppd_kv *src, int32_t n_seq
  * rows up to t), scale 1 / sqrt(128).  Sums are float32; probabilities and
  * float32 queries enter the products as two bfloat16 parts (bfloat16 calls) or
  * three (float32 calls).  A row that sees nothing gets zeros, and minus
- * infinity in lse; NaN and infinities reach only rows that see them.
+ * infinity in lse; NaN and infinities reach only rows that see them.  Limits: values
+ * of up to 2^95 in magnitude, and products of a query's and a key's elements of
+ * up to 2^118, keep every sum finite; past that finite rows can give infinities
+ * or NaN to the rows that see them.
  *   n_rows   rows that the buffers hold (rows behind row_start[n_seqs] are left
  *            as they were); n_rows <= tail.capacity
  *   q, out   device [n_rows][n_heads][128] of type dtype (PPD_BF16 or PPD_F32),

@@ -6,16 +6,36 @@
 // Products (v_mfma_f32_16x16x32_bf16): S^T = K Q^T with the 32 keys of a block as
 // two 16-row A operands, O^T += V^T P^T with 16 dims as the A operand.  Pages hold
 // blocks in the order of these operands: 16 loads of 1 KB, straight into the
-// registers of the wave that multiplies them.  A wave's rows of S^T are the keys
-// that its lanes hold as the B operand of the second product.
+// registers of the wave that multiplies them, the next block's keys requested
+// when a block's are multiplied, its values when its values are.  A wave's rows of
+// S^T are the keys that its lanes hold as the B operand of the second product.
 //
 // Work decomposition.  A workgroup takes a sequence, a kv head, up to RW rows and
-// one of KS key splits; its eight waves are QW side by side over tiles, NQ tiles
-// each, and PARS over blocks, with no barrier in the loop.  The grid is fixed by
-// what the host knows (sequences, rows); which part a workgroup takes it finds
-// from the lengths, every wave for itself: a sequence's share of kPagedSlots
-// workgroups follows its blocks, and sequences that get more than one leave
-// partial rows that a second launch adds in order.
+// one of KS key splits; its waves are QW side by side over tiles, NQ tiles each,
+// and PARS over blocks, with no barrier in the loop: (NQ, QW, PARS) = (1, 1, 4),
+// (2, 1, 4), (2, 2, 4) or (2, 4, 2), by paged_width.  The grid is fixed by what the
+// host knows (sequences, rows, the tables' width); which part a workgroup takes
+// every wave finds for itself from the lengths, so a captured call follows them.
+// Splits are such that a compute unit has one workgroup, of one sequence exactly as
+// many for every row group: where 9 splits of 32 groups put two workgroups on 32
+// units, 16 rows over 2048 positions took 20.1 us, with 8 16.5; twice as many
+// workgroups throughout, 131072 positions 93 us, 88 as it is.  Row groups of the
+// same keys are workgroups of one XCD; started at places of their own instead of
+// side by side they took 29 us for 20 (64 rows, 2048 positions).  Splits of one
+// or two tiles are added by the last of them to arrive, through memory past
+// the caches; wider ones by a second launch, since their rows are too many for
+// one compute unit.
+//
+// Bounds.  A compute unit has at most 32 KB of loads in flight (its L1), and four
+// waves keep it there: with eight a workgroup 32 heads over 2000 positions took 17.3 us
+// for 15.6 and 64 sequences 104 for 101, with two blocks requested ahead 64
+// sequences 101 for 96 (each beside the kernel of its time).  131072 positions 88 us (6.1
+// TB/s of reads; a copy 5.0), 64 sequences of up to 8192 positions 95 (5.3 TB/s, by
+// the last workgroups' unevenness), 128 of 2000 positions 167 (6.1).  64 rows over
+// 2048 positions 19.4: a unit loads 540 KB, each block for four tiles.  200 positions
+// 6.0: launch, lengths, table, keys, waves' meeting, one after another; splits
+// add about 4 (rows out, arrival, rows in).  Streaming (non-temporal) loads of pages
+// that one wave alone reads: 131072 positions 108 -> 97 us then.
 #include <algorithm>
 
 #include "ppd_paged.h"
@@ -28,9 +48,9 @@ constexpr int OROW = PPD_ATTN_OROW;  // partial row: 128 dims, m, l, padding (fl
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kNoSplit = PPD_CAPACITY_MAX;  // more blocks than a sequence has
 
-// parts of a query and of a probability on the matrix cores: bfloat16 outputs
-// round to 2^-9, two parts of a probability leave 2^-17 of it; float32 calls
-// carry three parts of both, 2^-25
+// parts of a query and of a probability on the matrix cores: a bfloat16 output is
+// rounded by up to 2^-8 of itself, a probability of two parts by 2^-16 (one would
+// double the output's error); float32 calls carry three parts of both, 2^-24
 __host__ __device__ constexpr int q_parts(int qt) { return qt == PAGED_Q_BF16 ? 1 : qt == PAGED_Q_F32 ? 3 : 2; }
 __host__ __device__ constexpr int p_parts(int qt) { return qt == PAGED_Q_F32 ? 3 : 2; }
 
@@ -57,10 +77,15 @@ __device__ __forceinline__ void split8(const float (&v)[8], u32x4 (&out)[PARTS])
 }
 
 // One block's scores (unscaled, hidden keys at -inf) into the running softmax:
-// the reference moves only when a maximum passes it by 8 (log2), P in pv.
+// the reference moves only when a maximum passes it by 8 (log2), P in pv.  Scaled
+// scores are rounded before the reference is taken off: a fused product would
+// leave the reference's own rounding, past 128 (and infinity) from scores of 2^31 on.
 __device__ __forceinline__ void softmax_step(PTile &R, const float (&sv)[8], float c, float (&pv)[8]) {
-  const float lmax = c * fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])),
-                               fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+#pragma clang fp contract(off)
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = sv[e] * c;
+  const float lmax = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
   if (__ballot(lmax > R.m_run + 8.f)) {
     const float bmax = quad_max(lmax);
     const bool need = bmax > R.m_run + 8.f;
@@ -73,7 +98,7 @@ __device__ __forceinline__ void softmax_step(PTile &R, const float (&sv)[8], flo
   const float m_eff = R.m_run == -INFINITY ? 0.f : R.m_run;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    pv[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], c, -m_eff));
+    pv[e] = __builtin_amdgcn_exp2f(x[e] - m_eff);
     R.l_run += pv[e];
   }
 }

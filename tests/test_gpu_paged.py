@@ -330,6 +330,41 @@ def test_attention_of_a_row_that_sees_nothing_and_of_odd_values(wide):
         ref.check(got, lse)
 
 
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+@pytest.mark.parametrize("L", [200, 3000])
+def test_attention_at_the_limits_of_magnitude(L, dtype):
+    """Values of up to 2^95; then scores of up to 2^125 too, whole multiples of 2^119
+    before the scale (exact in float32), so that a row is the mean of its best
+    keys' values: those weights are equal and the others zero."""
+    T, nkv, nh = 5, 1, 4
+    pool = Pool([L], nkv, 64, seed=L)
+    tk, tv = new_rows(nkv, 8, T)
+    pool.pages[:, :, :, :, 1] = (pool.pages[:, :, :, :, 1] * 2.0 ** 93).clamp(-2.0 ** 95, 2.0 ** 95)
+    tv = (tv * 2.0 ** 93).clamp(-2.0 ** 95, 2.0 ** 95)
+    q = torch.randn((T, nh, 128), generator=torch.Generator().manual_seed(L)).to(dtype)
+    kv, pt = pool.on_gpu(tk, tv)
+    out, lse, _ = attend(kv, pt, dev([0, T]), q.cuda(), None)
+    assert bool(torch.isfinite(out).all())
+    R.Attention(pool.pages, torch.from_numpy(pool.table), pool.lens, tk, tv, 0, [0, T], q, None, 64).check(out, lse)
+
+    pool.pages[:, :, :, :, 0] = torch.sign(pool.pages[:, :, :, :, 0]) * 2.0 ** 59
+    tk, q = torch.sign(tk) * 2.0 ** 59, torch.sign(q) * 2.0 ** 59
+    kv, pt = pool.on_gpu(tk, tv)
+    out, lse, _ = attend(kv, pt, dev([0, T]), q.cuda(), None)
+    k, v = R.rows_of(pool.pages, torch.from_numpy(pool.table), 0, 0, 0, L, 64)
+    k, v = torch.cat((k, tk[0, 0, :T])).double(), torch.cat((v, tv[0, 0, :, :T].t())).double()
+    half, part = (2.0 ** -8, 2.0 ** -16) if dtype == BF else (2.0 ** -24, 2.0 ** -24)
+    for t in range(T):
+        y = q[t].double() @ k[:L + t + 1].t()                    # whole multiples of 2^119
+        for h in range(nh):
+            best = v[:L + t + 1][y[h] == y[h].max()]
+            want, mag = best.mean(0), best.abs().mean(0)
+            err = (out[t, h].cpu().double() - want).abs()
+            assert bool((err <= half * want.abs() + (part + 2 * (L + 64) * 2.0 ** -24) * mag).all())
+            top = float(y[h].max()) / math.sqrt(128)
+            assert abs(float(lse[t, h]) - top) <= abs(top) * 2.0 ** -21
+
+
 @pytest.mark.parametrize("nkv", [1, 2])
 def test_attention_and_selection_of_many_sequences(nkv):
     """300 sequences, most without rows or without a prefix, some that share all pages."""
