@@ -16,7 +16,9 @@ namespace {
 // bisection of the starts, and the first row of a new page writes the table's
 // entry, so every new page is written by exactly one row.  Lengths and the ring's
 // state may be written where they are read: the last workgroup to have read
-// them does it.
+// them does it.  16 sequences with 60 rows 5.5 us, 512 with 0.8 million rows 10.6 (two
+// launches, the sums in the first: 17.0): launch, counts, two sums, bisection, ring and
+// slots one after another, a few KB to 3 MB.
 
 enum { kEnded = -1, kRefused = 0, kServed = 1 };
 
@@ -198,6 +200,12 @@ __global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
 // a block of 32 positions each, values 16 bytes at a time -- of a source that is
 // not aligned by eights two neighbouring pieces shifted into one -- and the waves'
 // bounds joined in LDS.
+//
+// Prompts of 4 sequences, 24 layers of 8 heads 206 to 212 us (4.7 TB/s of rows in and
+// out; a copy 5.0), pages of 256 positions 234 us for 904 MB, a
+// source off by three rows 183 for 700 MB.  Accepted rows of four sequences, 32 layers of 32
+// heads 15 us: 22 MB in and 22 MB out in lines touched in part, for 18 MB.  One kernel
+// for both took 250 and 27.
 
 constexpr int SW = 4;     // waves of a workgroup
 constexpr int SB = 255;   // sequences whose offsets fit its LDS
