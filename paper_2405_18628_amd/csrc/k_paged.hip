@@ -196,16 +196,16 @@ __global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
 // Accepted rows and single tokens (paged_put_kernel): a wave a run, eight rows at
 // a time, values element by element, a lane two dims; keys, values and bounds
 // requested together, since a call takes round trips and the lines it touches
-// in part rather than bytes.  Prompts (paged_fill_kernel): up to four waves a run,
+// in part rather than bytes.  Prompts (paged_fill_rows_kernel): up to four waves a run,
 // a block of 32 positions each, values 16 bytes at a time -- of a source that is
 // not aligned by eights two neighbouring pieces shifted into one -- and the waves'
 // bounds joined in LDS.
 //
-// Prompts of 4 sequences, 24 layers of 8 heads 206 to 212 us (4.7 TB/s of rows in and
-// out; a copy 5.0), pages of 256 positions 234 us for 904 MB, a
-// source off by three rows 183 for 700 MB.  Accepted rows of four sequences, 32 layers of 32
-// heads 15 us: 22 MB in and 22 MB out in lines touched in part, for 18 MB.  One kernel
-// for both took 250 and 27.
+// Prompts of four sequences, 24 layers of 8 heads 206 to 212 us (4.7 TB/s of rows in and
+// out; a copy 5.0), in pages of 256 positions 234, from a source off by three rows 183
+// (700 of 904 MB).  Accepted rows of four sequences, 32 layers of 32 heads 15 us: 22 MB
+// in and 22 MB out, in lines touched in part, for 18 MB.  One kernel for both took
+// 250 and 27.
 
 constexpr int SW = 4;     // waves of a workgroup
 constexpr int SB = 255;   // sequences whose offsets fit its LDS

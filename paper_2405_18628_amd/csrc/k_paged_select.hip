@@ -33,7 +33,7 @@ constexpr int CH = PAGES * (ST / 64);
 
 constexpr u64 kKept = ~0ull;  // the key of a page that is always taken: no number's
 
-// the order of numbers as unsigned keys; NaN first of all
+// the order of numbers as unsigned keys; NaN below every number
 __device__ __forceinline__ u64 key_of(double v) {
   if (v != v) return 0;
   const u64 b = __builtin_bit_cast(u64, v + 0.0);  // -0 as 0
