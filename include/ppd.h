@@ -623,7 +623,7 @@ ppd_status ppd_paged_store(const ppd_paged *kv, const ppd_kv *src, int32_t n_seq
  *   n_rows   rows that the buffers hold (rows behind row_start[n_seqs] are left
  *            as they were); n_rows <= tail.capacity
  *   q, out   device [n_rows][n_heads][128] of type dtype (PPD_BF16 or PPD_F32),
- *            16-byte aligned, not the same buffer
+ *            16-byte aligned, not overlapping
  *   lse      device float32 [n_rows][n_heads]: ln sum exp of the row's scores, or NULL
  *   sel, n_sel   pages by their place in the table, device int32
  *            [n_seqs][n_kv_heads][budget] and how many of them count, device
@@ -632,7 +632,9 @@ ppd_status ppd_paged_store(const ppd_paged *kv, const ppd_kv *src, int32_t n_seq
  *            ppd_paged_attention_workspace_bytes(n_heads, n_kv_heads, n_seqs, n_rows),
  *            one for each stream that calls may overlap on, prepared once with
  *            ppd_workspace_init (its header the status word, then counters that
- *            every call leaves zero)
+ *            every call leaves zero).  One large enough serves ppd_paged_tables,
+ *            ppd_paged_select and ppd_paged_attention in turn; other calls' scratch
+ *            would overwrite the counters
  */
 size_t ppd_paged_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t n_rows);
 ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,

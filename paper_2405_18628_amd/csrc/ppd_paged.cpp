@@ -18,7 +18,9 @@ namespace {
 constexpr int kMaxHeads = 1 << 20;   // layers x kv heads
 constexpr int kMaxRows = 1 << 22;    // new rows x heads: workgroups and threads are counted in 32 bits
 constexpr int64_t kMaxKeys = 1 << 29;  // sequences x kv heads x pages that are ranked
-constexpr size_t kHeader = 256;      // the status word
+// the status word and the counter of the tables, then the counters of the attention's
+// splits: alike in all workspaces here, so that calls in turn may share one
+constexpr size_t kHeader = 256, kFront = kHeader + kPagedCounters;
 
 int log2_of(int page) {
   int lp = 5;
@@ -219,7 +221,7 @@ size_t ppd_paged_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, 
              PPD_PAGED_SEQS_MAX, kMaxRows);
     return 0;
   }
-  return kHeader + kPagedCounters + (size_t)PPD_PAGED_SEQS_MAX * sizeof(int2) + paged_attn_part_bytes(n_heads, n_kv_heads, n_seqs, n_rows);
+  return kFront + (size_t)PPD_PAGED_SEQS_MAX * sizeof(int2) + paged_attn_part_bytes(n_heads, n_kv_heads, n_seqs, n_rows);
 }
 
 ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,
@@ -232,6 +234,9 @@ ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t lay
   if ((st = paged_check_rows(kv, row_start, n_rows)) != PPD_OK) return st;
   if (!out || (sel != nullptr) != (n_sel != nullptr)) return ppd_fail(PPD_EINVAL, "NULL argument");
   if ((uintptr_t)out % 16) return ppd_fail(PPD_EINVAL, "out must be 16-byte aligned");
+  const uintptr_t span = (uintptr_t)n_rows * n_heads * 128 * (dtype == PPD_F32 ? 4 : 2);
+  if ((uintptr_t)out - (uintptr_t)q < span || (uintptr_t)q - (uintptr_t)out < span)
+    return ppd_fail(PPD_EINVAL, "q and out must not overlap");
   if (sel && budget < 1) return ppd_fail(PPD_EINVAL, "budget=%d must be positive", budget);
   if ((st = check_work(ws, ws_bytes, ppd_paged_attention_workspace_bytes(n_heads, kv->n_kv_heads, pt->n_seqs, n_rows))) != PPD_OK)
     return st;
@@ -254,7 +259,7 @@ ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t lay
   a.nkv = kv->n_kv_heads;
   a.status = (uint32_t *)ws;
   a.ctr = (uint32_t *)((char *)ws + kHeader);  // (zeroed by ppd_workspace_init)
-  a.rec = (int2 *)((char *)ws + kHeader + kPagedCounters);
+  a.rec = (int2 *)((char *)ws + kFront);
   a.part = (float *)(a.rec + PPD_PAGED_SEQS_MAX);
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt(128.0));
   paged_attn_shape(a);
@@ -269,7 +274,7 @@ size_t ppd_paged_select_workspace_bytes(int32_t n_kv_heads, int32_t n_seqs, int3
     ppd_fail(PPD_EINVAL, "n_kv_heads, n_seqs=%d or max_pages=%d out of range", n_seqs, max_pages);
     return 0;
   }
-  return kHeader + paged_select_key_bytes(n_kv_heads, n_seqs, max_pages);
+  return kFront + paged_select_key_bytes(n_kv_heads, n_seqs, max_pages);
 }
 
 ppd_status ppd_paged_select(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,
@@ -293,7 +298,7 @@ ppd_status ppd_paged_select(int32_t n_heads, const ppd_paged *kv, int32_t layer,
   p.budget = budget;
   p.n_first = n_first;
   p.n_last = n_last;
-  p.keys = (unsigned long long *)((char *)ws + kHeader);
+  p.keys = (unsigned long long *)((char *)ws + kFront);
   p.sel = sel;
   p.n_sel = n_sel;
   p.status = (uint32_t *)ws;

@@ -548,6 +548,46 @@ def test_calls_on_another_stream():
     side.synchronize()
 
 
+def test_two_streams_at_once():
+    """Chains of selection and attention of two batches side by side, each stream with
+    a workspace that its calls share, beside the same calls one after another."""
+    nh, nkv, T, budget = 8, 2, 3, 9
+    runs = []
+    for i, lens in enumerate(([5000, 40, 0], [777, 3000, 1200])):
+        pool = Pool(lens, nkv, 64, seed=i)
+        tk, tv = new_rows(nkv, 16, 3 * T, seed=i)
+        kv, pt = pool.on_gpu(tk, tv)
+        q = torch.randn((3 * T, nh, 128), generator=torch.Generator().manual_seed(i)).to(BF).cuda()
+        width = pt.table.shape[1]
+        need = max(ppd.ppd_paged_attention_workspace_bytes(nh, nkv, 3, 3 * T), ppd.ppd_paged_select_workspace_bytes(nkv, 3, width))
+        sel = torch.zeros((3, nkv, budget), dtype=I32, device="cuda")
+        runs.append(dict(kv=kv, pt=pt, q=q, rows=dev(offsets([T] * 3)), ws=workspace(need), sel=sel, n=torch.zeros(3, dtype=I32, device="cuda"),
+                         out=[torch.zeros_like(q) for _ in range(2)], stream=torch.cuda.Stream()))
+
+    def chain(r, stream):
+        ppd.ppd_paged_select(r["kv"], 0, r["pt"], r["rows"], r["q"], budget, 1, 2, r["sel"], r["n"], r["ws"], stream=stream)
+        ppd.ppd_paged_attention(r["kv"], 0, r["pt"], r["rows"], r["q"], None, r["out"][0], r["ws"], None, r["sel"], r["n"], stream=stream)
+        ppd.ppd_paged_attention(r["kv"], 0, r["pt"], r["rows"], r["q"], None, r["out"][1], r["ws"], stream=stream)
+
+    torch.cuda.synchronize()
+    want = []
+    for r in runs:
+        chain(r, None)
+        torch.cuda.synchronize()
+        want.append([x.clone() for x in (*r["out"], r["sel"], r["n"])])
+    for _ in range(20):
+        for r in runs:
+            for x in r["out"]:
+                x.zero_()
+        torch.cuda.synchronize()
+        for r in runs:
+            chain(r, r["stream"])
+        torch.cuda.synchronize()
+        for r, w in zip(runs, want):
+            assert all(torch.equal(a, b) for a, b in zip((*r["out"], r["sel"], r["n"]), w))
+            assert ppd.ppd_device_status(r["ws"]) == 0
+
+
 def test_a_captured_chain_follows_the_lengths():
     """Select, attention, tables and store captured once and replayed while the
     sequences grow, end and start again, beside eager calls; two graphs share the

@@ -81,7 +81,7 @@ def test_store_refuses():
         assert call(**kw) == ppd.PPD_EINVAL, kw
 
 
-def _attend(nh=8, kv=None, layer=0, pt=None, row_start=F, n=4, q=F, dt=ppd.PPD_BF16, mask=None, out=F, sel=None, n_sel=None,
+def _attend(nh=8, kv=None, layer=0, pt=None, row_start=F, n=4, q=F, dt=ppd.PPD_BF16, mask=None, out=2 * F, sel=None, n_sel=None,
             budget=0, ws=F, size=BIG):
     return L.ppd_paged_attention(nh, C.byref(kv or _cache()), layer, C.byref(pt or _tables()), row_start, n, q, dt, mask, out, None,
                                  sel, n_sel, budget, ws, size, None)
@@ -108,7 +108,9 @@ def test_attention_and_select_refuse():
     for tail, code in BAD_TAILS:
         assert _attend(kv=_cache(tail=tail)) == code, tail
     assert _attend(n=129) == ppd.PPD_ECAPACITY
-    for kw in (dict(out=None), dict(out=F + 4), dict(sel=F), dict(n_sel=F), dict(sel=F, n_sel=F, budget=0)):
+    # (four rows of eight heads are 8192 bytes, in float32 16384)
+    for kw in (dict(out=None), dict(out=2 * F + 4), dict(out=F), dict(out=F + 8176), dict(out=F - 8176),
+               dict(out=F + 8192, dt=ppd.PPD_F32), dict(sel=F), dict(n_sel=F), dict(sel=F, n_sel=F, budget=0)):
         assert _attend(**kw) == ppd.PPD_EINVAL, kw
     assert _select(kv=_cache(bounds=None)) == ppd.PPD_EINVAL
     for kw in (dict(budget=0), dict(first=-1), dict(last=-1), dict(first=3, last=2), dict(sel=None), dict(n_sel=None)):
