@@ -30,8 +30,8 @@
 // waves keep it there: with eight a workgroup 32 heads over 2000 positions took 17.3 us
 // for 15.6 and 64 sequences 104 for 101, with two blocks requested ahead 64
 // sequences 101 for 96 (each beside the kernel of its time).  131072 positions 88 us (6.1
-// TB/s of reads; a copy 5.0), 64 sequences of up to 8192 positions 95 (5.3 TB/s, by
-// the last workgroups' unevenness), 128 of 2000 positions 167 (6.1).  64 rows over
+// TB/s of reads; a copy 5.0), 64 sequences of up to 8192 positions 89 (5.6 TB/s, by
+// uneven shares), 128 of 2000 positions 168 (6.0).  64 rows over
 // 2048 positions 19.4: a unit loads 540 KB, each block for four tiles.  200 positions
 // 6.0: launch, lengths, table, keys, waves' meeting, one after another; splits
 // add about 4 (rows out, arrival, rows in).  Streaming (non-temporal) loads of pages
@@ -141,9 +141,79 @@ struct Place {
   PagedSeq q;
   Load w;
 };
-// the workgroup's sequence and place in it; false: it has no part.  A wave's lanes
-// take a sequence each.
-template <int RW, int LEAST>
+// Where workgroups of several sequences start: those of groups that are cut first (so
+// a partial row's place is its workgroup's), and where not all start at once
+// the others by their length, in three classes, so that the last to start are short.
+// us in this order and in the sequences': 64 of up to 8192 positions 92 and 97, 200 of up
+// to 4000 147 and 169, 32 of up to 3000 with four rows 46 and 49, 128 of 2000 174 both
+constexpr int kClasses = 4;
+__device__ __forceinline__ int class_of(const Load &w, int KS, int c, bool at_once) {
+  return KS > 1 ? 0 : at_once || w.nblk > c >> 1 ? 1 : w.nblk > c >> 2 ? 2 : 3;
+}
+// More than 64 sequences: a thread takes every NT-th, the workgroup adds.  Every wave
+// by itself, 64 at a time, took 113 us for 94 with 1000 sequences of up to 1000
+// positions, 524 for 280 with 3000 of up to 300.
+template <int RW, int LEAST, int NT>
+__device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int slot, Place *out, bool *bad) {
+  constexpr int NW = NT / 64;
+  __shared__ int64_t total_s[NW];
+  __shared__ int count_s[NW][kClasses];
+  __shared__ Place place_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int64_t total = 0;
+#pragma unroll 4
+  for (int s = tid; s < p.sq.B; s += NT) {
+    const Load w = load_of(p, s, paged_seq(p.sq, s, bad), RW, bad);
+    total += (int64_t)w.units * w.nblk;
+  }
+  total = wave_total(total);
+  if (lane == 0) total_s[wave] = total;
+  if (tid == 0) place_s.sq = -1;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int v = 0; v < NW; ++v) total += total_s[v];
+  const int c = blocks_each<2 * LEAST>(total, kPagedSlots * 3 / 2);
+  int n[kClasses] = {}, upto[kClasses];
+#pragma unroll 4
+  for (int s = tid; s < p.sq.B; s += NT) {
+    const Load w = load_of(p, s, paged_seq(p.sq, s, bad), RW, bad);
+    const int KS = splits_of(w, c), cls = class_of(w, KS, c, false);
+#pragma unroll
+    for (int k = 0; k < kClasses; ++k) n[k] += cls == k ? w.units * KS : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < kClasses; ++k) {
+    upto[k] = wave_incl(n[k]);
+    if (lane == 63) count_s[wave][k] = upto[k];
+  }
+  __syncthreads();
+  int base = 0;
+  for (int k = 0; k < kClasses; ++k) {
+    int at = base + upto[k] - n[k];
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      at += v < wave ? count_s[v][k] : 0;
+      base += count_s[v][k];
+    }
+    if (slot < at || slot >= at + n[k]) continue;
+    for (int s = tid; s < p.sq.B; s += NT) {  // one of this thread's
+      const PagedSeq q = paged_seq(p.sq, s, bad);
+      const Load w = load_of(p, s, q, RW, bad);
+      const int KS = splits_of(w, c), m = class_of(w, KS, c, false) == k ? w.units * KS : 0;
+      if (slot < at + m) {
+        place_s = Place{s, slot - at, KS, at, q, w};
+        break;
+      }
+      at += m;
+    }
+  }
+  __syncthreads();
+  *out = place_s;
+  return out->sq >= 0;
+}
+// the workgroup's sequence and place in it; false: it has no part
+template <int RW, int LEAST, int NT>
 __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, Place *out, bool *bad) {
   if (p.sq.B == 1) {  // alike in all lanes
     out->sq = out->part0 = 0;
@@ -155,22 +225,20 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, P
     out->local = slot;
     return slot < out->w.units * out->KS;
   }
+  if (p.sq.B > 64) return find_place_of_many<RW, LEAST, NT>(p, slot, out, bad);
+  // a wave's lanes take a sequence each
   const int lane = threadIdx.x & 63;
-  int64_t total = 0;
   PagedSeq q{};
   Load w{};
-  for (int base = 0; base < p.sq.B; base += 64) {
-    const int s = base + lane;
-    if (s < p.sq.B) {
-      q = paged_seq(p.sq, s, bad);
-      w = load_of(p, s, q, RW, bad);
-      total += (int64_t)w.units * w.nblk;
-    }
+  if (lane < p.sq.B) {
+    q = paged_seq(p.sq, lane, bad);
+    w = load_of(p, lane, q, RW, bad);
   }
-  total = wave_total(total);
-  const int units = (int)wave_total(p.sq.B <= 64 ? w.units : 0);  // (more sequences: more groups than slots anyway)
+  const int64_t total = wave_total((int64_t)w.units * w.nblk);
+  const int units = (int)wave_total((int64_t)w.units);
+  const bool at_once = units <= kPagedSlots;
   int c;
-  if (units == 0 || units > kPagedSlots) {  // several rounds of workgroups: only long groups are cut
+  if (!at_once) {  // several rounds of workgroups: only long groups are cut
     c = blocks_each<2 * LEAST>(total, kPagedSlots * 3 / 2);
   } else {  // one round: each is rounded up, so fewer until they fit
     c = blocks_each<LEAST>(total, kPagedSlots);
@@ -180,32 +248,22 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, P
       c = (int)min(((int64_t)c * n + kPagedSlots - 1) / kPagedSlots, (int64_t)kNoSplit);
     }
   }
-  int slots0 = 0, parts0 = 0;
-  for (int base = 0; base < p.sq.B; base += 64) {
-    const int s = base + lane;
-    int KS = 0;
-    if (s < p.sq.B) {
-      if (p.sq.B > 64) {
-        q = paged_seq(p.sq, s, bad);
-        w = load_of(p, s, q, RW, bad);
-      }
-      KS = splits_of(w, c);
-    }
-    const int mine = s < p.sq.B ? w.units * KS : 0, parted = KS > 1 ? mine : 0;
-    const int upto = slots0 + wave_incl(mine), parts = parts0 + wave_incl(parted);
+  const int KS = splits_of(w, c), cls = class_of(w, KS, c, at_once);
+  int base = 0;
+  for (int k = 0; k < (at_once ? 2 : kClasses); ++k) {
+    const int mine = cls == k ? w.units * KS : 0, upto = base + wave_incl(mine);
     const uint64_t hit = __ballot(slot < upto);
     if (hit) {
       const int at = __builtin_ctzll(hit);
-      out->sq = base + at;
-      out->local = slot - lane_of(upto - mine, at);
+      out->sq = at;
+      out->part0 = lane_of(upto - mine, at);
+      out->local = slot - out->part0;
       out->KS = lane_of(KS, at);
-      out->part0 = lane_of(parts - parted, at);
       out->q = PagedSeq{lane_of(q.t0, at), lane_of(q.T, at), lane_of(q.L, at)};
       out->w = Load{lane_of(w.n4, at), lane_of(w.nblk, at), lane_of(w.grps, at), lane_of(w.units, at)};
       return true;
     }
-    slots0 = lane_of(upto, 63);
-    parts0 = lane_of(parts, 63);
+    base = lane_of(upto, 63);
   }
   return false;
 }
@@ -288,7 +346,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   const int lr = lane & 15, lg = lane >> 4;
   Place pl;
   bool bad = false;
-  const bool mine = find_place<RW, kLeast * PARS>(p, blockIdx.x, &pl, &bad);
+  const bool mine = find_place<RW, kLeast * PARS, NT>(p, blockIdx.x, &pl, &bad);
   if (bad && blockIdx.x == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   if (!mine) return;
   const int sq = __builtin_amdgcn_readfirstlane(pl.sq), KS = __builtin_amdgcn_readfirstlane(pl.KS);

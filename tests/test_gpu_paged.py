@@ -365,6 +365,31 @@ def test_attention_at_the_limits_of_magnitude(L, dtype):
             assert abs(float(lse[t, h]) - top) <= abs(top) * 2.0 ** -21
 
 
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("B,nkv,long", [(64, 5, 700), (65, 1, 3000), (100, 3, 2100), (600, 1, 1500)])
+def test_attention_of_many_lengths(B, nkv, long, wide):
+    """More groups of rows than compute units, or more sequences than a wave's lanes: a
+    few long ones that are cut among short and empty ones, in any order."""
+    r = np.random.default_rng(B)
+    lens = np.where(r.random(B) < 0.2, 0, (30 * np.exp(r.random(B) * 2.5)).astype(int))
+    lens[r.integers(0, B, 3)] = [long, long // 2, long - 31]
+    T = r.integers(0, 3, B)
+    T[[0, B - 1]] = 1
+    T[r.integers(B)] = 40
+    nh, n = 2 * nkv, int(T.sum())
+    pool = Pool(lens.tolist(), nkv, 32, seed=B)
+    tk, tv = new_rows(nkv, (n + 15) // 8 * 8, n)
+    kv, pt = pool.on_gpu(tk, tv, 1 << 19 if wide else 0)
+    q = torch.randn((n, nh, 128), generator=torch.Generator().manual_seed(B)).to(BF)
+    row_start = offsets(T.tolist())
+    out, lse, ws = attend(kv, pt, dev(row_start), q.cuda(), None)
+    assert ppd.ppd_device_status(ws) == 0
+    ref = R.Attention(pool.pages, torch.from_numpy(pool.table), pool.lens, tk, tv, 0, row_start, q, None, 32)
+    ref.check(out, lse)
+    again = attend(kv, pt, dev(row_start), q.cuda(), None, ws=ws)
+    assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
 @pytest.mark.parametrize("nkv", [1, 2])
 def test_attention_and_selection_of_many_sequences(nkv):
     """300 sequences, most without rows or without a prefix, some that share all pages."""
