@@ -131,10 +131,12 @@ template <int LEAST>
 __device__ __forceinline__ int blocks_each(int64_t total, int slots) {
   return (int)min(max((total + slots - 1) / slots, (int64_t)LEAST), (int64_t)kNoSplit);
 }
-__device__ __forceinline__ int splits_of(const Load &w, int c) {
-  c = max(c, (w.nblk + kPagedSplits - 1) / kPagedSplits);
-  return w.units ? (w.nblk + c - 1) / c : 0;
+__device__ __forceinline__ int splits_of(int units, int nblk, int c) {
+  if (nblk <= c) return units ? 1 : 0;
+  c = max(c, (nblk + kPagedSplits - 1) / kPagedSplits);
+  return units ? (nblk + c - 1) / c : 0;
 }
+__device__ __forceinline__ int splits_of(const Load &w, int c) { return splits_of(w.units, w.nblk, c); }
 
 struct Place {
   int sq, local, KS, part0;
@@ -147,24 +149,32 @@ struct Place {
 // us in this order and in the sequences': 64 of up to 8192 positions 92 and 97, 200 of up
 // to 4000 147 and 169, 32 of up to 3000 with four rows 46 and 49, 128 of 2000 174 both
 constexpr int kClasses = 4;
-__device__ __forceinline__ int class_of(const Load &w, int KS, int c, bool at_once) {
-  return KS > 1 ? 0 : at_once || w.nblk > c >> 1 ? 1 : w.nblk > c >> 2 ? 2 : 3;
+__device__ __forceinline__ int class_of(int nblk, int KS, int c, bool at_once) {
+  return KS > 1 ? 0 : at_once || nblk > c >> 1 ? 1 : nblk > c >> 2 ? 2 : 3;
 }
 // More than 64 sequences: a thread takes every NT-th, the workgroup adds.  Every wave
-// by itself, 64 at a time, took 113 us for 94 with 1000 sequences of up to 1000
-// positions, 524 for 280 with 3000 of up to 300.
+// by itself, 64 at a time, took 113 us for 81 with 1000 sequences of up to 1000
+// positions, 524 for 195 with 3000 of up to 300; with the lengths read again for the
+// second sum in place of LDS 94 and 280.
 template <int RW, int LEAST, int NT>
-__device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int slot, Place *out, bool *bad) {
+__device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int slot, int2 *list, Place *out, bool *bad) {
   constexpr int NW = NT / 64;
   __shared__ int64_t total_s[NW];
   __shared__ int count_s[NW][kClasses];
   __shared__ Place place_s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int64_t total = 0;
-#pragma unroll 4
-  for (int s = tid; s < p.sq.B; s += NT) {
-    const Load w = load_of(p, s, paged_seq(p.sq, s, bad), RW, bad);
-    total += (int64_t)w.units * w.nblk;
+  for (int s0 = tid; s0 < p.sq.B; s0 += 4 * NT) {  // (past the last: the last again)
+    PagedSeq q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = paged_seq(p.sq, min(s0 + i * NT, p.sq.B - 1), bad);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (s0 + i * NT < p.sq.B) {
+        const Load w = load_of(p, s0 + i * NT, q[i], RW, bad);
+        list[s0 + i * NT] = int2{w.units, w.nblk};
+        total += (int64_t)w.units * w.nblk;
+      }
   }
   total = wave_total(total);
   if (lane == 0) total_s[wave] = total;
@@ -177,10 +187,10 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
   int n[kClasses] = {}, upto[kClasses];
 #pragma unroll 4
   for (int s = tid; s < p.sq.B; s += NT) {
-    const Load w = load_of(p, s, paged_seq(p.sq, s, bad), RW, bad);
-    const int KS = splits_of(w, c), cls = class_of(w, KS, c, false);
+    const int2 w = list[s];
+    const int KS = splits_of(w.x, w.y, c), cls = class_of(w.y, KS, c, false);
 #pragma unroll
-    for (int k = 0; k < kClasses; ++k) n[k] += cls == k ? w.units * KS : 0;
+    for (int k = 0; k < kClasses; ++k) n[k] += cls == k ? w.x * KS : 0;
   }
 #pragma unroll
   for (int k = 0; k < kClasses; ++k) {
@@ -198,11 +208,11 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
     }
     if (slot < at || slot >= at + n[k]) continue;
     for (int s = tid; s < p.sq.B; s += NT) {  // one of this thread's
-      const PagedSeq q = paged_seq(p.sq, s, bad);
-      const Load w = load_of(p, s, q, RW, bad);
-      const int KS = splits_of(w, c), m = class_of(w, KS, c, false) == k ? w.units * KS : 0;
+      const int2 w = list[s];
+      const int KS = splits_of(w.x, w.y, c), m = class_of(w.y, KS, c, false) == k ? w.x * KS : 0;
       if (slot < at + m) {
-        place_s = Place{s, slot - at, KS, at, q, w};
+        const PagedSeq q = paged_seq(p.sq, s, bad);
+        place_s = Place{s, slot - at, KS, at, q, load_of(p, s, q, RW, bad)};
         break;
       }
       at += m;
@@ -212,9 +222,10 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
   *out = place_s;
   return out->sq >= 0;
 }
-// the workgroup's sequence and place in it; false: it has no part
+// the workgroup's sequence and place in it; false: it has no part.  list: LDS for all
+// sequences' work
 template <int RW, int LEAST, int NT>
-__device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, Place *out, bool *bad) {
+__device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, int2 *list, Place *out, bool *bad) {
   if (p.sq.B == 1) {  // alike in all lanes
     out->sq = out->part0 = 0;
     out->q = paged_seq(p.sq, 0, bad);
@@ -225,7 +236,7 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, P
     out->local = slot;
     return slot < out->w.units * out->KS;
   }
-  if (p.sq.B > 64) return find_place_of_many<RW, LEAST, NT>(p, slot, out, bad);
+  if (p.sq.B > 64) return find_place_of_many<RW, LEAST, NT>(p, slot, list, out, bad);
   // a wave's lanes take a sequence each
   const int lane = threadIdx.x & 63;
   PagedSeq q{};
@@ -248,7 +259,7 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, P
       c = (int)min(((int64_t)c * n + kPagedSlots - 1) / kPagedSlots, (int64_t)kNoSplit);
     }
   }
-  const int KS = splits_of(w, c), cls = class_of(w, KS, c, at_once);
+  const int KS = splits_of(w, c), cls = class_of(w.nblk, KS, c, at_once);
   int base = 0;
   for (int k = 0; k < (at_once ? 2 : kClasses); ++k) {
     const int mine = cls == k ? w.units * KS : 0, upto = base + wave_incl(mine);
@@ -338,6 +349,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   __shared__ __attribute__((aligned(16))) float rows_s[PARS][RW][OROW];
   u32x4 *q_s = (u32x4 *)rows_s;  // [tile][ds][part][lane]
   static_assert((size_t)QW * NQ * 4 * QP * 1024 <= sizeof(rows_s), "queries fit");
+  static_assert(PPD_PAGED_SEQS_MAX * sizeof(int2) <= sizeof(rows_s), "the sequences' work fits");
   __shared__ float fac_s[RW][PARS];  // what a row's waves are added with
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -346,7 +358,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   const int lr = lane & 15, lg = lane >> 4;
   Place pl;
   bool bad = false;
-  const bool mine = find_place<RW, kLeast * PARS, NT>(p, blockIdx.x, &pl, &bad);
+  const bool mine = find_place<RW, kLeast * PARS, NT>(p, blockIdx.x, (int2 *)rows_s, &pl, &bad);
   if (bad && blockIdx.x == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   if (!mine) return;
   const int sq = __builtin_amdgcn_readfirstlane(pl.sq), KS = __builtin_amdgcn_readfirstlane(pl.KS);
