@@ -609,8 +609,9 @@ ppd_status ppd_paged_store(const ppd_paged *kv, const ppd_kv *src, int32_t n_seq
  * Attention of one layer: the new rows of every sequence -- one token, or the
  * nodes of a tree -- over its pages and its own rows in kv->tail.  Sequence s has
  * rows [row_start[s], row_start[s + 1]) of q, mask, out, lse and the tail
- * (device int32[n_seqs + 1], not falling; up to PPD_T_MAX rows a sequence,
- * none allowed).  Row t of head h attends to positions [0, len[s]) of kv head h /
+ * (device int32[n_seqs + 1], not falling: of offsets that fall anywhere every
+ * row is left as it was and PPD_DEV_BAD_LENGTH is set; up to PPD_T_MAX rows a
+ * sequence, none allowed).  Row t of head h attends to positions [0, len[s]) of kv head h /
  * (n_heads / n_kv_heads), or those of them in the listed pages, and to the
  * sequence's rows whose mask bit is set (bits over its own rows; mask NULL: its
  * rows up to t), scale 1 / sqrt(128).  Sums are float32; probabilities and

@@ -164,6 +164,7 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
   __shared__ Place place_s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int64_t total = 0;
+  bool falls = false;
   for (int s0 = tid; s0 < p.sq.B; s0 += 4 * NT) {  // (past the last: the last again)
     PagedSeq q[4];
 #pragma unroll
@@ -174,15 +175,21 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
         const Load w = load_of(p, s0 + i * NT, q[i], RW, bad);
         list[s0 + i * NT] = int2{w.units, w.nblk};
         total += (int64_t)w.units * w.nblk;
+        falls |= q[i].falls;
       }
   }
   total = wave_total(total);
+  if (__ballot(falls)) total = -1;
   if (lane == 0) total_s[wave] = total;
   if (tid == 0) place_s.sq = -1;
   __syncthreads();
   total = 0;
 #pragma unroll
-  for (int v = 0; v < NW; ++v) total += total_s[v];
+  for (int v = 0; v < NW; ++v) {
+    falls |= total_s[v] < 0;
+    total += total_s[v];
+  }
+  if (falls) return false;  // (alike in all threads: a wave with a fall has -1 there)
   const int c = blocks_each<2 * LEAST>(total, kPagedSlots * 3 / 2);
   int n[kClasses] = {}, upto[kClasses];
 #pragma unroll 4
@@ -222,8 +229,10 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
   *out = place_s;
   return out->sq >= 0;
 }
-// the workgroup's sequence and place in it; false: it has no part.  list: LDS for all
-// sequences' work
+// the workgroup's sequence and place in it; false: it has no part.  Offsets that fall
+// give no workgroup one: the rows could ask for more workgroups than the grid has,
+// and a split that is never run leaves the others' arrivals in the counters, where
+// the workspace's next call would find them.  list: LDS for all sequences' work
 template <int RW, int LEAST, int NT>
 __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, int2 *list, Place *out, bool *bad) {
   if (p.sq.B == 1) {  // alike in all lanes
@@ -245,6 +254,7 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, i
     q = paged_seq(p.sq, lane, bad);
     w = load_of(p, lane, q, RW, bad);
   }
+  if (__ballot(q.falls)) return false;
   const int64_t total = wave_total((int64_t)w.units * w.nblk);
   const int units = (int)wave_total((int64_t)w.units);
   const bool at_once = units <= kPagedSlots;
@@ -360,7 +370,12 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   bool bad = false;
   const bool mine = find_place<RW, kLeast * PARS, NT>(p, blockIdx.x, (int2 *)rows_s, &pl, &bad);
   if (bad && blockIdx.x == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
-  if (!mine) return;
+  if (!mine) {
+    // (of a call without work: what the second launch reads of each sequence)
+    if (!JOIN && blockIdx.x == 0)
+      for (int s = tid; s < p.sq.B; s += NT) p.rec[s] = int2{0, 0};
+    return;
+  }
   const int sq = __builtin_amdgcn_readfirstlane(pl.sq), KS = __builtin_amdgcn_readfirstlane(pl.KS);
   const int t0 = __builtin_amdgcn_readfirstlane(pl.q.t0), T = __builtin_amdgcn_readfirstlane(pl.q.T);
   const int L = __builtin_amdgcn_readfirstlane(pl.q.L);

@@ -27,9 +27,12 @@ struct PagedSeqs {
 };
 
 // A sequence's own numbers, clamped so that no index that follows from them
-// leaves its buffer; *bad where one had to be.
+// leaves its buffer; *bad where one had to be.  Where offsets fall (falls of any
+// sequence) rows can be several sequences', and more than n_rows altogether: a call
+// that divides work among all of them has to leave it.
 struct PagedSeq {
   int t0, T, L;
+  bool falls;
 };
 __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs &p, int s, bool *bad) {
   const int n = p.len[s], a = p.row_start[s], b = p.row_start[s + 1];
@@ -37,7 +40,8 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs &p, int s, bool *b
   q.L = max(0, min((int64_t)n, (int64_t)p.max_pages << p.lp));
   q.t0 = max(0, min(a, p.n_rows));
   q.T = max(0, min(min(b, p.n_rows) - q.t0, PPD_T_MAX));
-  *bad |= n != q.L || a != q.t0 || b - a != q.T;
+  q.falls = b < a;
+  *bad |= n != q.L || a != q.t0 || (int64_t)b - a != q.T;
   return q;
 }
 __device__ __forceinline__ int paged_clamp(int page, int n_pages) { return max(0, min(page, n_pages - 1)); }
