@@ -61,9 +61,8 @@ __global__ __launch_bounds__(ST) void paged_score_kernel(PagedSelectLaunch p, in
   // (the table's entries are requested beside the length)
   const int32_t *table = p.sq.table + (size_t)sq * p.sq.max_pages;
   const int entry = table[min(page0 + (lane & (PAGES - 1)), p.sq.max_pages - 1)];
-  bool bad = false;
+  bool bad = false;  // (the selection, which every call launches, reports it)
   const PagedSeq s = paged_seq(p.sq, sq, &bad);
-  if (bad && c == 0 && tid == 0) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
   const int n = (s.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
   if (n <= p.budget || c * CH >= n) return;  // all are taken
   // ---- sums of the queries' positive and negative parts; the first rows and then the
@@ -171,7 +170,10 @@ __global__ __launch_bounds__(KT) void paged_pick_kernel(PagedSelectLaunch p) {
   const PagedSeq s = paged_seq(p.sq, sq, &bad);
   const int n = (s.L + (1 << p.sq.lp) - 1) >> p.sq.lp;
   int32_t *sel = p.sel + ((size_t)sq * p.nkv + kvh) * p.budget;
-  if (kvh == 0 && tid == 0) p.n_sel[sq] = min(n, p.budget);
+  if (kvh == 0 && tid == 0) {
+    p.n_sel[sq] = min(n, p.budget);
+    if (bad) atomicOr(p.status, PPD_DEV_BAD_LENGTH);
+  }
   if (n <= p.budget) {
     for (int i = tid; i < n; i += KT) sel[i] = i;
     return;

@@ -39,3 +39,27 @@ def test_offsets_that_fall_leave_the_workspace_as_it_was(B, rows, wide):
             out, lse, _ = attend(kv, pt, dev(good), q.cuda(), None, ws=ws)
             assert ppd.ppd_device_status(ws) == 0
             ref.check(out, lse, kept)
+
+
+@pytest.mark.parametrize("budget", [1, 3, 5, 9])
+def test_selection_reports_bad_numbers(budget):
+    """Tables of five pages, budgets below and above them (above: no scores are formed)."""
+    pool = Pool([150, 50], 2, 32)
+    pool.table = np.abs(pool.table[:, :5]) % pool.n_pages
+    tk, tv = new_rows(2, 8, 8)
+    kv, pt = pool.on_gpu(tk, tv)
+    assert pt.max_pages == 5
+    q = torch.randn((8, 2, 128), device="cuda").to(BF)
+    ws = workspace(ppd.ppd_paged_select_workspace_bytes(2, 2, 5))
+    sel, n_sel = torch.full((2, 2, budget), -8, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for length, rows in (([150, 50], [0, 4, 8]), ([-1, 50], [0, 4, 8]), ([150, 161], [0, 4, 8]), ([10 ** 9, 50], [0, 4, 8]),
+                         ([150, 50], [0, 4, 9]), ([150, 50], [-2 ** 31, 4, 2 ** 31 - 1]), ([150, 50], [6, 2, 8])):
+        pt.len.copy_(dev(length))
+        ppd.ppd_paged_select(kv, 0, pt, dev(rows), q, budget, 0, 1, sel, n_sel, ws)
+        bad = length != [150, 50] or rows != [0, 4, 8]
+        assert ppd.ppd_device_status(ws, clear=True) == (ppd.PPD_DEV_BAD_LENGTH if bad else 0), (length, rows)
+        want = [min(budget, -(-min(max(n, 0), 160) // 32)) for n in length]
+        assert n_sel.tolist() == want
+        for s, m in enumerate(want):
+            picked = sel[s, :, :m]
+            assert bool(((picked >= 0) & (picked < 5)).all()) and bool((picked[:, 1:] > picked[:, :-1]).all())
