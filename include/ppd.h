@@ -660,7 +660,8 @@ ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t lay
  *            selected ones are left as they were
  *   n_sel    device int32[n_seqs]
  *   ws       device workspace, 16-byte aligned, of
- *            ppd_paged_select_workspace_bytes(n_kv_heads, n_seqs, max_pages)
+ *            ppd_paged_select_workspace_bytes(n_kv_heads, n_seqs, max_pages), 0 past
+ *            2^21 heads x sequences or 2^29 heads x sequences x pages
  */
 size_t ppd_paged_select_workspace_bytes(int32_t n_kv_heads, int32_t n_seqs, int32_t max_pages);
 ppd_status ppd_paged_select(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,

@@ -897,7 +897,13 @@ size_t ppd_paged_workspace_bytes(const ppd_model *model, int32_t n_seqs, int32_t
     fail(PPD_EINVAL, "n_rows must be in [1, %d], budget >= 0, the model bf16", PPD_T_MAX);
     return 0;
   }
-  if (!ppd_paged_select_workspace_bytes(model->n_kv_heads, n_seqs, max_pages)) return 0;
+  if (n_seqs < 1 || n_seqs > PPD_PAGED_SEQS_MAX || max_pages < 1 || max_pages > PPD_CAPACITY_MAX / PPD_PAGED_BLOCK) {
+    fail(PPD_EINVAL, "n_seqs=%d outside [1, %d] or max_pages=%d outside [1, %d]", n_seqs, PPD_PAGED_SEQS_MAX, max_pages,
+         PPD_CAPACITY_MAX / PPD_PAGED_BLOCK);
+    return 0;
+  }
+  // (limits of the pages that are ranked: a step over all pages ranks none)
+  if (budget && !ppd_paged_select_workspace_bytes(model->n_kv_heads, n_seqs, max_pages)) return 0;
   return layout_of(model, n_rows).total + paged_layout(model, n_seqs, max_pages, n_rows, budget).total;
 }
 
