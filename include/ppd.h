@@ -92,7 +92,8 @@ typedef enum { PPD_F32 = 0, PPD_BF16 = 1 } ppd_dtype;
                                     step's outputs are then invalid          */
 #define PPD_DEV_NO_PAGES 32u    /* ppd_paged_tables refused a sequence its tokens */
 #define PPD_DEV_BAD_LENGTH 64u  /* a length, count or row offset on the device was
-                                    out of range and was clamped             */
+                                    out of range and was clamped, or row offsets
+                                    fall or leave rows of a step out         */
 
 /*
  * Llama-style decoder (the paper's MobileLLaMA / Vicuna family): pre-RMSNorm
@@ -672,8 +673,9 @@ ppd_status ppd_paged_select(int32_t n_heads, const ppd_paged *kv, int32_t layer,
 /*
  * ppd_verify_batch on pages: sequence s of pt has rows [row_start[s],
  * row_start[s + 1]) of ids, depth, mask, logits and pred (device int32[n_seqs +
- * 1], rising to n_rows = all tree tokens <= PPD_T_MAX; sequences without rows
- * sit the step out), its root at position len[s].  Lengths and offsets are read
+ * 1], rising from 0 to n_rows = all tree tokens <= PPD_T_MAX; sequences without
+ * rows sit the step out), its root at position len[s].  Rows that are no sequence's
+ * get no attention: their logits and pred mean nothing, and PPD_DEV_BAD_LENGTH is set.  Lengths and offsets are read
  * on the device: a captured step serves whatever they are when it is replayed.
  * The rows go to kv->tail.  budget > 0: every layer attends to the pages that
  * ppd_paged_select picks (budget, n_first, n_last as there); 0: to all.

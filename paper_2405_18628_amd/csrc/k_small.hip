@@ -43,6 +43,8 @@ __global__ __launch_bounds__(256) void embed_kernel(const WT *__restrict__ tok_e
         n += __popcll(__ballot(s < dev.B && dev.row_start[min(s, dev.B - 1)] <= t));
       }
       L = max(0, min(dev.len[max(0, n - 1)], PPD_CAPACITY_MAX));
+      // a row that no sequence has gets no attention
+      if (t < T && threadIdx.x == 0 && (n == 0 || dev.row_start[n] <= t)) atomicOr(status, PPD_DEV_BAD_LENGTH);
     }
     for (int i = threadIdx.x; i < d / 2; i += blockDim.x) {
       const double pos = t < T ? (double)L + (double)depth[t] : 0.0;

@@ -6,7 +6,10 @@ import torch
 
 import paged_reference as R
 import paper_2405_18628_amd as ppd
+from gpu_cases import make_case, tree_for
+from synth import workload
 from test_gpu_paged import BF, Pool, attend, dev, new_rows, workspace
+from test_gpu_paged_step import Paged, joined
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +66,30 @@ def test_selection_reports_bad_numbers(budget):
         for s, m in enumerate(want):
             picked = sel[s, :, :m]
             assert bool(((picked >= 0) & (picked < 5)).all()) and bool((picked[:, 1:] > picked[:, :-1]).all())
+
+
+@pytest.mark.parametrize("budget", [0, 3])
+def test_a_step_reports_rows_that_no_sequence_has(budget):
+    case = make_case(workload("small-gqa", cache_len=150))
+    trees = [tree_for(case, spec=s, seed_offset=i) for i, s in enumerate(("total:16", "chain:7"))]
+    T0, n = trees[0].T, sum(t.T for t in trees)
+    p = Paged(case, 2, 32, 20, 8, n, budget)
+    p.prompts(case.k, case.v, [150, 70])
+    tt = joined(trees)
+
+    def step(offsets):
+        p.logits.fill_(7.0)
+        p.verify(dev(offsets), tt, budget=budget, n_last=min(1, budget))
+        return p.logits.clone(), ppd.ppd_device_status(p.ws, clear=True)
+
+    right, status = step([0, T0, n])
+    assert status == 0
+    for offsets, rows in (([0, T0, n - 2], slice(0, n - 2)), ([0, T0, T0], slice(0, T0)), ([2, T0, n], slice(T0, n)),
+                          ([0, T0, n + 5], slice(0, n)), ([0, n, T0], slice(0, 0))):
+        logits, status = step(offsets)
+        assert status & ppd.PPD_DEV_BAD_LENGTH, offsets
+        assert not len(logits[rows]) or float((logits[rows] - right[rows]).abs().max()) < 1e-3, offsets
+    again, status = step([0, T0, n])
+    assert status == 0 and torch.equal(again, right)
+    again, status = step([0, 0, n])      # a sequence that sits out: every row is the other's
+    assert status == 0
