@@ -164,32 +164,35 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
   __shared__ Place place_s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int64_t total = 0;
-  bool falls = false;
+  int low = 0;
+  if (blockIdx.x == 0)  // bad numbers are reported by one workgroup (looked for in all 3000 sequences took 754 us for 741)
+    for (int s = tid; s < p.sq.B; s += NT) load_of(p, s, paged_seq(p.sq, s, bad), RW, bad);
+  bool unused = false;
   for (int s0 = tid; s0 < p.sq.B; s0 += 4 * NT) {  // (past the last: the last again)
     PagedSeq q[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = paged_seq(p.sq, min(s0 + i * NT, p.sq.B - 1), bad);
+    for (int i = 0; i < 4; ++i) q[i] = paged_seq(p.sq, min(s0 + i * NT, p.sq.B - 1), &unused, &low);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (s0 + i * NT < p.sq.B) {
-        const Load w = load_of(p, s0 + i * NT, q[i], RW, bad);
+        const Load w = load_of(p, s0 + i * NT, q[i], RW, &unused);
         list[s0 + i * NT] = int2{w.units, w.nblk};
         total += (int64_t)w.units * w.nblk;
-        falls |= q[i].falls;
       }
   }
   total = wave_total(total);
-  if (__ballot(falls)) total = -1;
+  if (__ballot(low < 0)) total = -1;  // (offsets fall)
   if (lane == 0) total_s[wave] = total;
   if (tid == 0) place_s.sq = -1;
   __syncthreads();
   total = 0;
+  bool falls = false;
 #pragma unroll
   for (int v = 0; v < NW; ++v) {
     falls |= total_s[v] < 0;
     total += total_s[v];
   }
-  if (falls) return false;  // (alike in all threads: a wave with a fall has -1 there)
+  if (falls) return false;
   const int c = blocks_each<2 * LEAST>(total, kPagedSlots * 3 / 2);
   int n[kClasses] = {}, upto[kClasses];
 #pragma unroll 4
@@ -218,8 +221,8 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
       const int2 w = list[s];
       const int KS = splits_of(w.x, w.y, c), m = class_of(w.y, KS, c, false) == k ? w.x * KS : 0;
       if (slot < at + m) {
-        const PagedSeq q = paged_seq(p.sq, s, bad);
-        place_s = Place{s, slot - at, KS, at, q, load_of(p, s, q, RW, bad)};
+        const PagedSeq q = paged_seq(p.sq, s, &unused);
+        place_s = Place{s, slot - at, KS, at, q, load_of(p, s, q, RW, &unused)};
         break;
       }
       at += m;
@@ -250,11 +253,12 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, i
   const int lane = threadIdx.x & 63;
   PagedSeq q{};
   Load w{};
+  int low = 0;
   if (lane < p.sq.B) {
-    q = paged_seq(p.sq, lane, bad);
+    q = paged_seq(p.sq, lane, bad, &low);
     w = load_of(p, lane, q, RW, bad);
   }
-  if (__ballot(q.falls)) return false;
+  if (__ballot(low < 0)) return false;
   const int64_t total = wave_total((int64_t)w.units * w.nblk);
   const int units = (int)wave_total((int64_t)w.units);
   const bool at_once = units <= kPagedSlots;

@@ -27,22 +27,26 @@ struct PagedSeqs {
 };
 
 // A sequence's own numbers, clamped so that no index that follows from them
-// leaves its buffer; *bad where one had to be.  Where offsets fall (falls of any
-// sequence) rows can be several sequences', and more than n_rows altogether: a call
-// that divides work among all of them has to leave it.
+// leaves its buffer; *bad where one had to be.  Where clamped offsets fall (*low below
+// zero) rows can be several sequences', and more than n_rows altogether: a call that
+// divides work among all of them has to leave it.
 struct PagedSeq {
   int t0, T, L;
-  bool falls;
 };
-__device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs &p, int s, bool *bad) {
+__device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs &p, int s, bool *bad, int *low) {
   const int n = p.len[s], a = p.row_start[s], b = p.row_start[s + 1];
   PagedSeq q;
   q.L = max(0, min((int64_t)n, (int64_t)p.max_pages << p.lp));
   q.t0 = max(0, min(a, p.n_rows));
-  q.T = max(0, min(min(b, p.n_rows) - q.t0, PPD_T_MAX));
-  q.falls = b < a;
-  *bad |= n != q.L || a != q.t0 || (int64_t)b - a != q.T;
+  const int end = max(0, min(b, p.n_rows)), rows = end - q.t0;  // (clamped first: no difference of offsets overflows)
+  q.T = max(0, min(rows, PPD_T_MAX));
+  *low = min(*low, rows);
+  *bad |= n != q.L || a != q.t0 || b != end || rows != q.T;
   return q;
+}
+__device__ __forceinline__ PagedSeq paged_seq(const PagedSeqs &p, int s, bool *bad) {
+  int low = 0;
+  return paged_seq(p, s, bad, &low);
 }
 __device__ __forceinline__ int paged_clamp(int page, int n_pages) { return max(0, min(page, n_pages - 1)); }
 

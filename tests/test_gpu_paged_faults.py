@@ -93,3 +93,33 @@ def test_a_step_reports_rows_that_no_sequence_has(budget):
     assert status == 0 and torch.equal(again, right)
     again, status = step([0, 0, n])      # a sequence that sits out: every row is the other's
     assert status == 0
+
+
+@pytest.mark.parametrize("B", [1, 2, 70])
+def test_offsets_at_the_ends_of_32_bits_stay_inside(B):
+    """A difference of offsets that passes 32 bits is no number of rows: what lies
+    behind the call's rows stays as it was."""
+    n, nh, low, high = 8, 2, -2 ** 31, 2 ** 31 - 1
+    pool = Pool([100], 1, 32)
+    pool.table, pool.lens = np.repeat(pool.table, B, 0), np.full(B, 100, np.int32)
+    tk, tv = new_rows(1, 8, n)
+    kv, pt = pool.on_gpu(tk, tv)
+    q = torch.randn((n + 256, nh, 128), generator=torch.Generator().manual_seed(B)).to(BF).cuda()
+    ws = workspace(max(ppd.ppd_paged_attention_workspace_bytes(nh, 1, B, n), ppd.ppd_paged_select_workspace_bytes(1, B, pt.max_pages)))
+    out, lse = torch.full_like(q, 7.0), torch.full((n + 256, nh), 7.0, device="cuda")
+    sel, n_sel = dev(np.zeros((B, 1, 2))), dev(np.zeros(B))
+    for ends in ((5, low), (low, high), (high, low), (low, 5), (3, high), (n, low), (0, low), (low, low), (high, high)):
+        offsets = np.concatenate((np.full(B, ends[0]), [ends[1]])) if B < 3 else np.concatenate((np.full(B // 2, ends[0]), np.full(B // 2 + 1, ends[1])))
+        rows = dev(offsets.astype(np.int64))
+        for listed in (False, True):
+            if listed:
+                ppd.ppd_paged_select(kv, 0, pt, rows, q[:n], 2, 0, 1, sel, n_sel, ws)
+                assert ppd.ppd_device_status(ws, clear=True) == ppd.PPD_DEV_BAD_LENGTH, ends
+            ppd.ppd_paged_attention(kv, 0, pt, rows, q[:n], None, out[:n], ws, lse[:n], *((sel, n_sel) if listed else ()))
+            assert ppd.ppd_device_status(ws, clear=True) == ppd.PPD_DEV_BAD_LENGTH, ends
+            assert bool((out[n:] == 7.0).all()) and bool((lse[n:] == 7.0).all()), ends
+    good = dev(np.minimum(np.arange(B + 1) * 4, n))
+    ppd.ppd_paged_attention(kv, 0, pt, good, q[:n], None, out[:n], ws, lse[:n])
+    assert ppd.ppd_device_status(ws) == 0
+    ref = R.Attention(pool.pages, torch.from_numpy(pool.table), pool.lens, tk, tv, 0, good.tolist(), q[:n].cpu(), None, 32)
+    ref.check(out[:n], lse[:n])
