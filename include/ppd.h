@@ -186,10 +186,11 @@ typedef struct {
  * nodes and caches of up to max_len positions.  0 on invalid input. */
 size_t ppd_workspace_bytes(const ppd_model *model, int32_t t_max, int32_t max_len);
 
-/* Zero the workspace's header, its first 256 bytes, which hold the status word,
- * and of what it has behind them 512 bytes more, the counters of a
- * ppd_paged_attention workspace (enqueued on `stream`).  Call once after allocating
- * a workspace; later calls never write the header except for status bits. */
+/* Zero the workspace's header, its first 256 bytes (enqueued on `stream`).  Call
+ * once after allocating a workspace.  It holds the status word, to which later calls
+ * add bits, and counters that ppd_paged_tables and ppd_paged_attention use and leave
+ * zero; no call's scratch covers it, so calls in turn may share a workspace that is
+ * large enough for each of them. */
 ppd_status ppd_workspace_init(void *ws, size_t ws_bytes, void *stream);
 
 /*
@@ -633,10 +634,7 @@ ppd_status ppd_paged_store(const ppd_paged *kv, const ppd_kv *src, int32_t n_seq
  *   ws       device workspace, 16-byte aligned, of
  *            ppd_paged_attention_workspace_bytes(n_heads, n_kv_heads, n_seqs, n_rows),
  *            one for each stream that calls may overlap on, prepared once with
- *            ppd_workspace_init (its header the status word, then counters that
- *            every call leaves zero).  One large enough serves ppd_paged_tables,
- *            ppd_paged_select and ppd_paged_attention in turn; other calls' scratch
- *            would overwrite the counters
+ *            ppd_workspace_init
  */
 size_t ppd_paged_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t n_seqs, int32_t n_rows);
 ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,

@@ -140,6 +140,7 @@ __device__ __forceinline__ int splits_of(const Load &w, int c) { return splits_o
 
 struct Place {
   int sq, local, KS, part0;
+  int bits;  // of a place's share of the counters
   PagedSeq q;
   Load w;
 };
@@ -222,7 +223,7 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
       const int KS = splits_of(w.x, w.y, c), m = class_of(w.y, KS, c, false) == k ? w.x * KS : 0;
       if (slot < at + m) {
         const PagedSeq q = paged_seq(p.sq, s, &unused);
-        place_s = Place{s, slot - at, KS, at, q, load_of(p, s, q, RW, &unused)};
+        place_s = Place{s, slot - at, KS, at, 2, q, load_of(p, s, q, RW, &unused)};
         break;
       }
       at += m;
@@ -240,6 +241,7 @@ template <int RW, int LEAST, int NT>
 __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, int2 *list, Place *out, bool *bad) {
   if (p.sq.B == 1) {  // alike in all lanes
     out->sq = out->part0 = 0;
+    out->bits = 6;
     out->q = paged_seq(p.sq, 0, bad);
     out->w = load_of(p, 0, out->q, RW, bad);
     // (as many for each row group: no compute unit gets one workgroup more than the others)
@@ -263,13 +265,17 @@ __device__ __forceinline__ bool find_place(const PagedAttnLaunch &p, int slot, i
   const int units = (int)wave_total((int64_t)w.units);
   const bool at_once = units <= kPagedSlots;
   int c;
+  out->bits = at_once ? 3 : 2;
   if (!at_once) {  // several rounds of workgroups: only long groups are cut
     c = blocks_each<2 * LEAST>(total, kPagedSlots * 3 / 2);
   } else {  // one round: each is rounded up, so fewer until they fit
     c = blocks_each<LEAST>(total, kPagedSlots);
     for (int i = 0; i < 4; ++i) {
       const int n = (int)wave_total((int64_t)w.units * splits_of(w, c));
-      if (n <= kPagedSlots) break;
+      if (n <= kPagedSlots) {
+        out->bits = 6;
+        break;
+      }
       c = (int)min(((int64_t)c * n + kPagedSlots - 1) / kPagedSlots, (int64_t)kNoSplit);
     }
   }
@@ -387,6 +393,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   const int n_grp = __builtin_amdgcn_readfirstlane(pl.w.grps);
   const int part0 = __builtin_amdgcn_readfirstlane(pl.part0);
   const int local = __builtin_amdgcn_readfirstlane(pl.local);
+  const int bits = __builtin_amdgcn_readfirstlane(pl.bits);
   if (!JOIN && local == 0 && tid == 0) p.rec[sq] = int2{KS, part0};
   const int G = p.nh / p.nkv, R = T * G;
   // row groups that read the same keys are nkv KS workgroups apart: mostly on one
@@ -649,7 +656,7 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
   __syncthreads();
   const int n_rows = min(R - row0, RW);
   const size_t part0_at = (size_t)my_part * RW * OROW;  // (only with several splits)
-  const __amdgpu_buffer_rsrc_t far = rsrc_of(p.part, JOIN ? 3 * kPagedSlots * RW * OROW * (uint32_t)sizeof(float) : 0);
+  const __amdgpu_buffer_rsrc_t far = rsrc_of(p.part, JOIN ? kPagedParts * RW * OROW * (uint32_t)sizeof(float) : 0);
   if (tid < n_rows) {
     float2 ml[PARS];
     float M = -INFINITY, l = 0.f;
@@ -701,11 +708,11 @@ __global__ __launch_bounds__(64 * QW * PARS, 2) void paged_attention_kernel(Page
     __builtin_amdgcn_s_waitcnt(0);  // this thread's rows are in memory
     __syncthreads();
     if (tid == 0) {
-      const int i = (my_part - ks) >> 1, shift = 8 * (i & 3);  // (two splits at least: no two groups share i)
-      uint32_t *ctr = p.ctr + (i >> 2);
-      const uint32_t n = __hip_atomic_fetch_add(ctr, 1u << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> shift & 0xffu;
+      const SplitCounter c = split_counter(my_part - ks, KS, bits);
+      uint32_t *ctr = p.ctr + c.word;
+      const uint32_t n = __hip_atomic_fetch_add(ctr, 1u << c.shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> c.shift & c.mask;
       last_s = n + 1 == (uint32_t)KS;
-      if (last_s) __hip_atomic_fetch_sub(ctr, (uint32_t)KS << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (last_s) __hip_atomic_fetch_sub(ctr, (uint32_t)KS << c.shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (!last_s) return;
@@ -885,7 +892,7 @@ static int paged_width(int tiles, int64_t blocks_of_a_tile) {
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows) {
   const int tiles = paged_tiles(nh, nkv, B, n_rows);  // (of the widest workgroup it may become)
   const Shape sh = paged_shape(tiles <= 2 ? tiles : tiles <= 4 ? 4 : 8);
-  return 3 * (size_t)kPagedSlots * sh.rows() * OROW * sizeof(float);
+  return (size_t)kPagedParts * sh.rows() * OROW * sizeof(float);
 }
 
 void paged_attn_shape(PagedAttnLaunch &a) {

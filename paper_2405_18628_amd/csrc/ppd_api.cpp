@@ -775,11 +775,9 @@ size_t ppd_workspace_bytes(const ppd_model *model, int32_t t_max, int32_t max_le
 }
 
 ppd_status ppd_workspace_init(void *ws, size_t ws_bytes, void *stream) {
-  const size_t need = align_up(16);  // the header: the status word
+  const size_t need = align_up(16);  // the header: the status word, the counters of the calls on pages
   if (!ws || ws_bytes < need) return fail(PPD_EWORKSPACE, "workspace needs at least %zu bytes", need);
-  // (with the counters of ppd_paged_attention's workspace)
-  const size_t bytes = std::min(ws_bytes, need + kPagedCounters) & ~(size_t)3;
-  PPD_TRY_HIP(launch_ws_init(ws, bytes / 4, (hipStream_t)stream));
+  PPD_TRY_HIP(launch_ws_init(ws, need / 4, (hipStream_t)stream));
   return PPD_OK;
 }
 

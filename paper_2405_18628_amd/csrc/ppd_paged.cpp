@@ -18,9 +18,10 @@ namespace {
 constexpr int kMaxHeads = 1 << 20;   // layers x kv heads
 constexpr int kMaxRows = 1 << 22;    // new rows x heads: workgroups and threads are counted in 32 bits
 constexpr int64_t kMaxKeys = 1 << 29;  // sequences x kv heads x pages that are ranked
-// the status word and the counter of the tables, then the counters of the attention's
-// splits: alike in all workspaces here, so that calls in turn may share one
-constexpr size_t kHeader = 256, kFront = kHeader + kPagedCounters;
+// the header of a workspace: the status word, from byte 16 on the counter of the tables,
+// from kCounters on those of the attention's splits
+constexpr size_t kHeader = 256, kCounters = 64;
+static_assert(kCounters + kPagedCounters <= kHeader, "the counters fit the header");
 
 int log2_of(int page) {
   int lp = 5;
@@ -150,7 +151,7 @@ size_t ppd_paged_tables_workspace_bytes(int32_t n_seqs) {
     ppd_fail(PPD_EINVAL, "n_seqs=%d outside [1, %d]", n_seqs, PPD_PAGED_SEQS_MAX);
     return 0;
   }
-  return kHeader;  // (the status words and a counter)
+  return kHeader;
 }
 
 ppd_status ppd_paged_tables(const ppd_page_tables *pt, const int32_t *add, int32_t *len_out, int32_t *free_state_out,
@@ -221,7 +222,7 @@ size_t ppd_paged_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, 
              PPD_PAGED_SEQS_MAX, kMaxRows);
     return 0;
   }
-  return kFront + (size_t)PPD_PAGED_SEQS_MAX * sizeof(int2) + paged_attn_part_bytes(n_heads, n_kv_heads, n_seqs, n_rows);
+  return kHeader + (size_t)PPD_PAGED_SEQS_MAX * sizeof(int2) + paged_attn_part_bytes(n_heads, n_kv_heads, n_seqs, n_rows);
 }
 
 ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,
@@ -258,8 +259,8 @@ ppd_status ppd_paged_attention(int32_t n_heads, const ppd_paged *kv, int32_t lay
   a.nh = n_heads;
   a.nkv = kv->n_kv_heads;
   a.status = (uint32_t *)ws;
-  a.ctr = (uint32_t *)((char *)ws + kHeader);  // (zeroed by ppd_workspace_init)
-  a.rec = (int2 *)((char *)ws + kFront);
+  a.ctr = (uint32_t *)((char *)ws + kCounters);  // (zeroed by ppd_workspace_init)
+  a.rec = (int2 *)((char *)ws + kHeader);
   a.part = (float *)(a.rec + PPD_PAGED_SEQS_MAX);
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt(128.0));
   paged_attn_shape(a);
@@ -274,7 +275,7 @@ size_t ppd_paged_select_workspace_bytes(int32_t n_kv_heads, int32_t n_seqs, int3
     ppd_fail(PPD_EINVAL, "n_kv_heads, n_seqs=%d or max_pages=%d out of range", n_seqs, max_pages);
     return 0;
   }
-  return kFront + paged_select_key_bytes(n_kv_heads, n_seqs, max_pages);
+  return kHeader + paged_select_key_bytes(n_kv_heads, n_seqs, max_pages);
 }
 
 ppd_status ppd_paged_select(int32_t n_heads, const ppd_paged *kv, int32_t layer, const ppd_page_tables *pt,
@@ -298,7 +299,7 @@ ppd_status ppd_paged_select(int32_t n_heads, const ppd_paged *kv, int32_t layer,
   p.budget = budget;
   p.n_first = n_first;
   p.n_last = n_last;
-  p.keys = (unsigned long long *)((char *)ws + kFront);
+  p.keys = (unsigned long long *)((char *)ws + kHeader);
   p.sel = sel;
   p.n_sel = n_sel;
   p.status = (uint32_t *)ws;

@@ -151,9 +151,9 @@ struct PagedAttnLaunch {
   const int32_t *sel, *n_sel;  // [B][nkv][budget], [B], or null
   int budget;
   int nh, nkv;
-  float *part;                 // [3 kPagedSlots][rows of a workgroup][PPD_ATTN_OROW]
+  float *part;                 // [kPagedParts][rows of a workgroup][PPD_ATTN_OROW]
   int2 *rec;                   // [B]: splits, first of the partial rows' workgroups
-  uint32_t *ctr;               // arrivals of row groups' splits, a byte each: zero between launches
+  uint32_t *ctr;               // arrivals of row groups' splits (SplitCounter): zero between launches
   uint32_t *status;
   float scale_log2;
   int tiles;                   // 16-row tiles of a workgroup: 1, 2, 4 or 8
@@ -162,8 +162,34 @@ struct PagedAttnLaunch {
 };
 // Workgroups that a call's keys are divided among: one a compute unit
 constexpr int kPagedSlots = 256;
-constexpr int kPagedSplits = 128;  // most splits of a row group (a byte counts them)
-constexpr size_t kPagedCounters = 512;  // bytes of them: below 1.5 kPagedSlots row groups have several
+constexpr int kPagedSplits = 128;  // most splits of a row group
+constexpr int kPagedParts = 3 * kPagedSlots;  // workgroups of row groups with several, at most
+constexpr size_t kPagedCounters = 2 * kPagedParts / 8;  // bytes of their counters
+// Where the splits of a row group, KS of them from place `first` on, count their
+// arrivals: `bits` of the workspace's header for each place (6 of up to kPagedSlots
+// places, 3 of twice and 2 of three times as many), which no call's scratch covers.
+// The group's counter holds up to KS and lies in one word, in the next where it would
+// cross into it.  Few groups share a word: arrivals at one are served one after
+// another (with 2 bits throughout, 16 rows over 2000 positions took 17.0 us for 15.9).
+struct SplitCounter {
+  int word, shift;
+  uint32_t mask;
+};
+__host__ __device__ constexpr SplitCounter split_counter(int first, int KS, int bits) {
+  const int need = 32 - __builtin_clz((unsigned)KS), at = bits * first;
+  const int from = at % 32 + need > 32 ? (at + 31) / 32 * 32 : at;
+  return SplitCounter{from / 32, from % 32, (1u << need) - 1};
+}
+constexpr bool split_counters_fit(int bits) {
+  for (int first = 0; first < 32; ++first)  // (later places: the same, whole words on)
+    for (int KS = 2; KS <= kPagedSplits; ++KS) {
+      const SplitCounter c = split_counter(first, KS, bits);
+      const int from = 32 * c.word + c.shift, need = 32 - __builtin_clz(c.mask);
+      if (from < bits * first || from + need > bits * (first + KS) || c.shift + need > 32 || (unsigned)KS > c.mask) return false;
+    }
+  return true;
+}
+static_assert(split_counters_fit(2) && split_counters_fit(3) && split_counters_fit(6), "in the group's own bits and one word, and hold KS");
 size_t paged_attn_part_bytes(int nh, int nkv, int B, int n_rows);
 void paged_attn_shape(PagedAttnLaunch &a);  // fills tiles, may_split
 hipError_t launch_paged_attn(const PagedAttnLaunch &a, hipStream_t s);

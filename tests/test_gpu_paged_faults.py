@@ -123,3 +123,37 @@ def test_offsets_at_the_ends_of_32_bits_stay_inside(B):
     assert ppd.ppd_device_status(ws) == 0
     ref = R.Attention(pool.pages, torch.from_numpy(pool.table), pool.lens, tk, tv, 0, good.tolist(), q[:n].cpu(), None, 32)
     ref.check(out[:n], lse[:n])
+
+
+def test_any_calls_in_turn_share_a_workspace():
+    """Split attention on a workspace whose scratch holds what other calls left there:
+    bytes of ones, a step's, a selection's, another batch's.  The header keeps nothing."""
+    case = make_case(workload("small-gqa", cache_len=150))
+    tree = tree_for(case, spec="total:16")
+    p = Paged(case, 1, 32, 20, 8, tree.T, 3)
+    p.prompts(case.k, case.v, [150])
+    runs = []
+    for i, (lens, nkv, nh, T) in enumerate((([3000, 900], 2, 4, [5, 1]), ([700] * 40, 1, 2, [1] * 40), ([5000], 3, 3, [20]))):
+        pool = Pool(lens, nkv, 64, seed=i)
+        tk, tv = new_rows(nkv, 40, sum(T), seed=i)
+        kv, pt = pool.on_gpu(tk, tv)
+        q = torch.randn((sum(T), nh, 128), generator=torch.Generator().manual_seed(i)).to(BF).cuda()
+        rows = dev(np.concatenate(([0], np.cumsum(T))))
+        out, lse, ws = attend(kv, pt, rows, q, None)
+        runs.append((kv, pt, rows, q, out, lse, ws.numel(), dev(np.zeros((len(lens), nkv, 2))), dev([0] * len(lens))))
+    size = max([r[6] for r in runs] + [p.ws.numel(), ppd.ppd_workspace_bytes(case.model, 16, case.k.shape[2])])
+    ws = workspace(size)
+    ws[256:] = 255
+    steps = (lambda r: None, lambda r: ppd.ppd_verify_batch_paged(case.model, p.kv, p.pt, dev([0, tree.T]), tt["ids"], tt["depth"],
+                                                                  tt["mask"], ws, p.logits, p.pred, budget=3, n_last=1),
+             lambda r: ppd.ppd_paged_select(r[0], 0, r[1], r[2], r[3], 2, 0, 1, r[7], r[8], ws),
+             lambda r: ppd.ppd_paged_tables(p.pt, dev([0]), p.start, dev([0]), ws),
+             lambda r: ppd.ppd_verify_step(case.model, ppd.KVCache(case.k, case.v), 150, tree.T, tt["ids"], tt["depth"], tt["mask"], ws,
+                                           p.logits, p.pred), lambda r: ws[256:].fill_(3))
+    tt = joined([tree])
+    for between in steps:
+        for r in runs:
+            between(r)
+            out, lse, _ = attend(*r[:4], None, ws=ws)
+            assert ppd.ppd_device_status(ws) == 0 and not ws[:256].any()
+            assert torch.equal(out, r[4]) and torch.equal(lse, r[5])
