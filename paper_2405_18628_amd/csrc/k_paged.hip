@@ -168,7 +168,8 @@ __global__ __launch_bounds__(TT) void paged_tables_kernel(PagedTablesLaunch p) {
       if (!(plan.ended[s >> 5] >> (s & 31) & 1)) continue;
       const int m = (int)pages_of(plan.len[s], p.lp);
       for (int j = tid & 63; j < m; j += 64)
-        p.free_pages[in_ring((int64_t)plan.at[s] + j, p.n_pages)] = p.table[(size_t)s * p.max_pages + j];
+        // (a length of more pages than there are is bad, but goes round the ring)
+        p.free_pages[(uint32_t)(plan.at[s] + j) % (uint32_t)p.n_pages] = p.table[(size_t)s * p.max_pages + j];
     }
   if (blockIdx.x == 0) {
     for (int s = tid; s <= p.B; s += TT) p.start[s] = plan.start[s];

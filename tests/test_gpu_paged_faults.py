@@ -157,3 +157,20 @@ def test_any_calls_in_turn_share_a_workspace():
             out, lse, _ = attend(*r[:4], None, ws=ws)
             assert ppd.ppd_device_status(ws) == 0 and not ws[:256].any()
             assert torch.equal(out, r[4]) and torch.equal(lse, r[5])
+
+
+@pytest.mark.parametrize("B", [1, 3, 400])
+def test_pages_given_back_stay_in_the_ring(B):
+    """Tables wider than the pool, and lengths on the device of more pages than it has."""
+    n, width = 6, 20
+    ring = torch.full((n + 64,), -9, dtype=torch.int32, device="cuda")
+    ring[:n] = torch.arange(n, dtype=torch.int32)
+    pt = ppd.PageTables(torch.zeros((B, width), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda"),
+                        ring[:n], dev([4, 3]), 32)
+    start, slots = torch.zeros(B + 1, dtype=torch.int32, device="cuda"), torch.zeros(8, dtype=torch.int32, device="cuda")
+    ws = workspace(ppd.ppd_paged_tables_workspace_bytes(B))
+    for length in (width * 32, 10 ** 9, 7 * 32):
+        pt.len.fill_(length)
+        ppd.ppd_paged_tables(pt, dev(np.full(B, -1)), start, slots, ws)
+        assert ppd.ppd_device_status(ws, clear=True) == ppd.PPD_DEV_BAD_LENGTH
+        assert bool((ring[n:] == -9).all()) and not pt.len.any() and 0 <= int(pt.free_state[1]) <= n
