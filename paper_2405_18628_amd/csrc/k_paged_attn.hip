@@ -155,7 +155,7 @@ __device__ __forceinline__ int class_of(int nblk, int KS, int c, bool at_once) {
 }
 // More than 64 sequences: a thread takes every NT-th, the workgroup adds.  Every wave
 // by itself, 64 at a time, took 113 us for 81 with 1000 sequences of up to 1000
-// positions, 524 for 195 with 3000 of up to 300; with the lengths read again for the
+// positions, 524 for 195 with 3000 of up to 300 (192 since one workgroup alone looks for bad numbers); with the lengths read again for the
 // second sum in place of LDS 94 and 280.
 template <int RW, int LEAST, int NT>
 __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int slot, int2 *list, Place *out, bool *bad) {
@@ -166,7 +166,7 @@ __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int64_t total = 0;
   int low = 0;
-  if (blockIdx.x == 0)  // bad numbers are reported by one workgroup (looked for in all 3000 sequences took 754 us for 741)
+  if (blockIdx.x == 0)  // (3000 sequences on 8 kv heads 728 us, looked for in all workgroups 754)
     for (int s = tid; s < p.sq.B; s += NT) load_of(p, s, paged_seq(p.sq, s, bad), RW, bad);
   bool unused = false;
   for (int s0 = tid; s0 < p.sq.B; s0 += 4 * NT) {  // (past the last: the last again)
@@ -344,10 +344,13 @@ __device__ __forceinline__ floatx4 get_far(__amdgpu_buffer_rsrc_t r, size_t at) 
   return __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(at * sizeof(float)), 0, kFar));
 }
 
-// ONCE: no other wave of the call reads it
-template <bool ONCE>
+// STREAM: past the caches (non-temporal), in workgroups of one tile or two.  Pages that
+// one row group reads gain by it (131072 positions, one row 91 us for 101); where
+// row groups share them neither is better throughout: 64 rows over 1024, 2048, 4096 and
+// 8192 positions 16.1, 20.8, 26.7, 39.0 us, through the caches 15.4, 21.2, 27.1, 38.6.
+template <bool STREAM>
 __device__ __forceinline__ u32x4 load_page(const unsigned char *p) {
-  if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4 *)p);
+  if constexpr (STREAM) return __builtin_nontemporal_load((const u32x4 *)p);
   return *(const u32x4 *)p;
 }
 
@@ -881,7 +884,12 @@ static int paged_tiles(int nh, int nkv, int B, int n_rows) {
 // KB of loads, some 50 GB/s) is the bound, and wide workgroups read every block once.
 // us, by tiles of a workgroup 1, 2, 4 or 8: 32 heads of 64 nodes, 1024 positions 16.0,
 // 18.1, 19.9; 4096 29.3, 26.1, 29.5; 32768 166, 121, 111; of 128 nodes 2048 25.3, 24.8,
-// 28.9; 8192 74, 60, 52; of 32 nodes 2000 16.0, 20.5; 8192 33.4, 35.7
+// 28.9; 8192 74, 60, 52; of 32 nodes 2000 16.3, 20.9; 4096 22.4, 26.3; 8192 34.3, 36.3;
+// 16384 58.3, 57.0.  The limits are alike for all numbers of tiles, so that 32 nodes get
+// two from 6100 positions on, where they lose 6 %: 64 nodes over 4096, which are as many
+// blocks, gain 10.  Blocks are those of the tables' width: short prefixes in wide tables
+// are read in the shape of long ones (32 nodes over 2048 positions 15.8 us, from a table of
+// 8192 on 20.4; 64 over 1024 15.6, from 4096 on 18.0, from 32768 on 18.9)
 constexpr int64_t kOwnTileBlocks = 48, kTwoTileBlocks = 96;
 static int paged_width(int tiles, int64_t blocks_of_a_tile) {
   const int64_t two = blocks_of_a_tile * ((tiles + 1) / 2), one = blocks_of_a_tile * tiles;

@@ -5,7 +5,8 @@
 // over the rows and heads that share the choice, with Qp and Qm the sums of their
 // positive and negative parts, it is one product of 256 elements a page whatever
 // the number of rows.  Its sums are float64: pages' scores lie close together,
-// and whole numbers hang on their order.
+// and whole numbers hang on their order (scores that differ by their roundings alone may
+// rank either way).
 //
 // Scores: a wave takes 16 pages, two at a time (512 bytes of bounds a page, 16
 // bytes a lane), the rows of queries and then the bounds requested before either is

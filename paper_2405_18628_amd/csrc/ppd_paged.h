@@ -76,7 +76,7 @@ __device__ __forceinline__ uint32_t wave_all(uint32_t v, F f) {
   auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   return f(b[0], b[1]);
 }
-// (whole numbers below 2^53; 24 bits at a time, so that 64 of them fit)
+// (whole numbers below 2^48; 24 bits at a time, so that 64 of them fit)
 __device__ __forceinline__ int64_t wave_total(int64_t v) {
   auto add = [](uint32_t a, uint32_t b) { return a + b; };
   int64_t sum = 0;
