@@ -155,8 +155,9 @@ __device__ __forceinline__ int class_of(int nblk, int KS, int c, bool at_once) {
 }
 // More than 64 sequences: a thread takes every NT-th, the workgroup adds.  Every wave
 // by itself, 64 at a time, took 113 us for 81 with 1000 sequences of up to 1000
-// positions, 524 for 195 with 3000 of up to 300 (192 since one workgroup alone looks for bad numbers); with the lengths read again for the
-// second sum in place of LDS 94 and 280.
+// positions, 524 for 195 with 3000 of up to 300 (192 since one workgroup alone looks
+// for bad numbers); with the lengths read again for the second sum in place of LDS 94
+// and 280.
 template <int RW, int LEAST, int NT>
 __device__ __forceinline__ bool find_place_of_many(const PagedAttnLaunch &p, int slot, int2 *list, Place *out, bool *bad) {
   constexpr int NW = NT / 64;
